@@ -67,6 +67,17 @@ class _Outputs(C.Structure):
                 ("blk_rank", C.c_void_p)]
 
 
+class _F8Matrix(C.Structure):
+    """sop_f8_matrix"""
+    _fields_ = [("codes", C.c_void_p), ("ld_codes", C.c_int64), ("scales", C.c_void_p), ("ld_scales", C.c_int64), ("format", C.c_int), ("block_rows", C.c_int)]
+
+
+class _Packed(C.Structure):
+    """sop_packed_weights"""
+    _fields_ = [("words", C.c_void_p), ("payload", C.c_void_p), ("N", C.c_int64), ("K", C.c_int64), ("g", C.c_int), ("n_bits", C.c_int),
+                ("fmt", ScaleFmt), ("k", C.c_int), ("table_a", C.POINTER(C.c_float)), ("entries_a", C.c_int), ("table_b", C.POINTER(C.c_float)), ("entries_b", C.c_int)]
+
+
 def lib_path() -> str:
     return os.path.join(_HERE, "libsop_hip.so")
 
@@ -132,6 +143,16 @@ def lib():
         L.sop_pack_blocks.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int, ScaleFmt, C.c_void_p, C.c_void_p, C.c_int,
                                       C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                                       C.POINTER(C.c_int), C.c_void_p]
+        L.sop_fp8_quantize.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.POINTER(_F8Matrix), C.c_void_p, C.c_int64, C.c_void_p]
+        L.sop_fp8_matmul.argtypes = [C.c_void_p, C.POINTER(_F8Matrix), C.POINTER(_F8Matrix), C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int,
+                                     C.c_int64, C.c_void_p]
+        L.sop_fp8_weight_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_F8Matrix), C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int,
+                                          C.c_int64, C.c_int, C.c_void_p]
+        L.sop_fp8_gated.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.POINTER(_F8Matrix),
+                                    C.POINTER(_F8Matrix), C.POINTER(_F8Matrix), C.c_void_p]
+        L.sop_fp8_gated_grad.argtypes = [C.c_void_p, C.POINTER(_F8Matrix), C.POINTER(_F8Matrix), C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64,
+                                         C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(_F8Matrix), C.POINTER(_F8Matrix), C.c_void_p]
+        L.sop_packed_matmul.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_Packed), C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
         L.sop_layer_shift.argtypes = [C.POINTER(C.c_int64), C.c_int64, ScaleFmt, C.POINTER(C.c_int), C.POINTER(C.c_double)]
         _lib = L
     return _lib
@@ -278,6 +299,94 @@ class Outputs:
     blk_cos: object = None
     blk_err: object = None
     blk_rank: object = None
+
+
+E4M3, E5M2 = 0, 1
+
+
+def _up(n, unit):
+    return -(-n // unit) * unit
+
+
+def _spaced(t, unit, what):
+    """A 2-D tensor of bytes as the library reads it: rows a multiple of `unit` bytes apart that may be read to their full width.
+    The tensor itself if it is laid out so, else a copy that is."""
+    import torch
+    if t.dim() != 2 or t.element_size() != 1 or not t.is_cuda:
+        raise SopError(1, f"{what} must be a 2-D CUDA tensor of one byte an element")
+    R, Cc = t.shape
+    ld = t.stride(0) if R > 1 else _up(Cc, unit)
+    if (t.stride(1) == 1 or Cc <= 1) and ld >= Cc and ld % unit == 0 and t.data_ptr() % unit == 0 and \
+            t.untyped_storage().nbytes() - t.storage_offset() >= (R - 1) * ld + _up(Cc, unit):
+        return t, ld
+    ld = _up(Cc, unit)
+    buf = torch.zeros((R, ld), dtype=torch.uint8, device=t.device)
+    buf[:, :Cc] = t.view(torch.uint8) if t.is_contiguous() else t.contiguous().view(torch.uint8)
+    return buf.view(t.dtype)[:, :Cc], ld
+
+
+class Fp8Blocks:
+    """A matrix in 8 bits: codes (torch.float8_e4m3fn or float8_e5m2, [R, C]) and one power-of-two scale (torch.float8_e8m0fnu) for
+    each block of `rows` x 128 (rows = 1: activations and gradients; rows = 128: weights).  codes_t: the same codes as a [C, R]
+    matrix, where the product over the other index is wanted too.  Tensors that are not laid out as the library reads them (rows of
+    codes 16 bytes apart, of scales 4) are copied, once."""
+    __slots__ = ("codes", "scales", "rows", "codes_t", "shape", "_m", "_t")
+
+    def __init__(self, codes, scales, rows: int = 1, codes_t=None):
+        import torch
+        fmt = E4M3 if codes.dtype == torch.float8_e4m3fn else E5M2 if codes.dtype == torch.float8_e5m2 else None
+        if fmt is None:
+            raise SopError(1, "codes must be float8_e4m3fn or float8_e5m2")
+        if scales.dtype not in (torch.float8_e8m0fnu, torch.uint8):
+            raise SopError(1, "scales must be float8_e8m0fnu (or its bytes)")
+        if rows not in (1, 128):
+            raise SopError(1, "blocks have 1 or 128 rows")
+        self.codes, ld = _spaced(codes, 16, "codes")
+        self.scales, lds = _spaced(scales, 4, "scales")
+        R, K = codes.shape
+        if tuple(scales.shape) != (-(-R // rows), -(-K // 128)):
+            raise SopError(2, f"codes of {R} x {K} in blocks of {rows} x 128 have scales of {-(-R // rows)} x {-(-K // 128)}")
+        if scales.device != codes.device:
+            raise SopError(1, "codes and scales must be on one GPU")
+        self.rows, self.shape, self.codes_t, self._t = rows, (R, K), None, None
+        self._m = _F8Matrix(self.codes.data_ptr(), ld, self.scales.data_ptr(), lds, fmt, rows)
+        if codes_t is not None:
+            if rows != 128 or codes_t.dtype != codes.dtype or tuple(codes_t.shape) != (K, R) or codes_t.device != codes.device:
+                raise SopError(2, "codes_t must be the codes of 128 x 128 blocks, transposed")
+            self.codes_t, ldt = _spaced(codes_t, 16, "codes_t")
+            self._t = _F8Matrix(self.codes_t.data_ptr(), ldt, self.scales.data_ptr(), lds, fmt, rows)
+
+    @classmethod
+    def empty(cls, R, K, dtype, device, rows: int = 1, transposed: bool = False):
+        import torch
+        dt = {E4M3: torch.float8_e4m3fn, E5M2: torch.float8_e5m2}.get(dtype, dtype)
+
+        def room(r, c, unit, t):
+            ld = _up(c, unit)
+            return torch.empty((r, ld), dtype=t, device=device) if ld == c else torch.empty((r, ld), dtype=t, device=device)[:, :c]
+
+        return cls(room(R, K, 16, dt), room(-(-R // rows), -(-K // 128), 4, torch.float8_e8m0fnu), rows, room(K, R, 16, dt) if transposed else None)
+
+
+class PackedWeights:
+    """A packed layer [N, K] as it is held for products: what pack_blocks / search_layer(pack=True) wrote (words, payload, n_bits), its
+    codebooks (one table, or two where the words carry a selector) and the scale format and layer shift k of the search."""
+    __slots__ = ("words", "payload", "shape", "tables", "_w")
+
+    def __init__(self, words, payload, N, K, g, n_bits, fmt: ScaleFmt, tables, k: int = 0):
+        import torch
+        if not (words.is_cuda and payload.is_cuda) or words.device != payload.device:
+            raise SopError(1, "words and payload must be CUDA tensors on one GPU (no CPU fallback)")
+        if words.element_size() != 2 or payload.dtype != torch.uint8 or not (words.is_contiguous() and payload.is_contiguous()):
+            raise SopError(1, "words must be contiguous 16-bit integers, payload contiguous uint8")
+        if N < 1 or K < 1 or g < 1 or K % g or words.numel() != N * K // g or payload.numel() != N * K * n_bits // 8:
+            raise SopError(2, "words and payload do not hold N x K weights in blocks of g with n_bits codes")
+        if not 1 <= len(tables) <= 2:
+            raise SopError(3, "one codebook or two")
+        self.words, self.payload, self.shape = words, payload, (N, K)
+        self.tables = [np.ascontiguousarray(t, dtype=np.float32) for t in tables]
+        a, b = self.tables[0], self.tables[1] if len(tables) == 2 else None
+        self._w = _Packed(words.data_ptr(), payload.data_ptr(), N, K, g, n_bits, fmt, k, _fp(a), a.size, None if b is None else _fp(b), 0 if b is None else b.size)
 
 
 class Context:
@@ -645,4 +754,117 @@ class Context:
         _check(lib().sop_pair_search(self._h, C.c_void_p(W.data_ptr()), dt, M, K, W.stride(0), C.c_void_p(c.data_ptr()), g,
                                      fmt, k, metric, None, 0, C.byref(o),
                                      C.c_void_p(st)), self._h)
+        return out
+
+    # ---- products of a linear layer with narrow operands
+
+    def _here(self, *tensors):
+        for t in tensors:
+            if not t.is_cuda or t.device.index != self.device:
+                raise SopError(1, "tensors must be on the context's GPU (no CPU fallback)")
+
+    def _stream(self, stream):
+        import torch
+        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
+
+    def _numbers(self, x, what, dtypes=None):
+        """(sop_dtype, row stride) of a matrix of numbers."""
+        import torch
+        self._here(x)
+        if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+            raise SopError(2, f"{what} must be a 2-D tensor with contiguous rows")
+        if x.dtype not in (dtypes or (torch.float32, torch.bfloat16)):
+            raise SopError(1, f"{what} must be " + ("bfloat16" if dtypes else "float32 or bfloat16"))
+        return (BF16 if x.dtype == torch.bfloat16 else F32), (x.stride(0) if x.shape[0] > 1 else _up(x.shape[1], 8))
+
+    def _result(self, out, M, N, dtype, device):
+        """A matrix to write to: `out` if it fits, else a new one."""
+        import torch
+        if out is None:
+            if dtype not in (torch.float32, torch.bfloat16):
+                raise SopError(1, "results are float32 or bfloat16")
+            return torch.empty((M, N), dtype=dtype, device=device)
+        if tuple(out.shape) != (M, N):
+            raise SopError(2, f"out must be {M} x {N}")
+        return out
+
+    def fp8_quantize(self, x, rows: int = 1, fmt=E4M3, transposed: bool = False, stream=None) -> Fp8Blocks:
+        """sop_fp8_quantize: x [M, K] float32 or bfloat16 into 8 bits (fmt: E4M3 / E5M2, or the torch type) with one power-of-two scale for
+        each block of rows x 128.  transposed (rows = 128 only): the codes as a [K, M] matrix too."""
+        dt, ldx = self._numbers(x, "x")
+        if transposed and rows != 128:
+            raise SopError(1, "a transposed copy is made of 128 x 128 blocks only")
+        M, K = x.shape
+        q = Fp8Blocks.empty(M, K, fmt, x.device, rows, transposed)
+        _check(lib().sop_fp8_quantize(self._h, x.data_ptr(), dt, M, K, ldx, q._m, q._t.codes if transposed else None, q._t.ld_codes if transposed else 0,
+                                      self._stream(stream)), self._h)
+        return q
+
+    def fp8_matmul(self, x: Fp8Blocks, w: Fp8Blocks, transposed: bool = False, dtype=None, out=None, stream=None):
+        """sop_fp8_matmul: y = x w^T of x [M, K] (rows = 1) and w [N, K] (rows = 128); transposed: y = x w of x [M, N] and the same w by its
+        codes_t (the input gradient).  dtype: bfloat16 (default) or float32; or `out`, a matrix of either type to write to."""
+        import torch
+        self._here(x.codes, w.codes)
+        if transposed and w._t is None:
+            raise SopError(1, "the transposed product needs the weight's codes_t (fp8_quantize(..., transposed=True))")
+        (M, K), (N, Kw) = x.shape, (w.shape[::-1] if transposed else w.shape)
+        if K != Kw:
+            raise SopError(2, f"x has rows of {K} elements, the weight wants {Kw}")
+        out = self._result(out, M, N, torch.bfloat16 if dtype is None else dtype, x.codes.device)
+        dt, ldy = self._numbers(out, "out")
+        _check(lib().sop_fp8_matmul(self._h, x._m, w._t if transposed else w._m, int(transposed), M, N, K, out.data_ptr(), dt, ldy, self._stream(stream)), self._h)
+        return out
+
+    def fp8_weight_grad(self, dy, x: Fp8Blocks, dtype=None, out=None, accumulate: bool = False, stream=None):
+        """sop_fp8_weight_grad: dw [N, K] = dy^T x from dy [M, N] bfloat16 and the 8-bit checkpoint x [M, K] (rows = 1); dtype: float32 (default)
+        or bfloat16; accumulate: added to `out`."""
+        import torch
+        self._here(x.codes)
+        _, lddy = self._numbers(dy, "dy", (torch.bfloat16,))
+        (M, N), K = dy.shape, x.shape[1]
+        if x.shape[0] != M:
+            raise SopError(2, f"dy has {M} rows, the checkpoint {x.shape[0]}")
+        if accumulate and out is None:
+            raise SopError(1, "accumulate needs out")
+        out = self._result(out, N, K, torch.float32 if dtype is None else dtype, dy.device)
+        dt, ldw = self._numbers(out, "out")
+        _check(lib().sop_fp8_weight_grad(self._h, dy.data_ptr(), lddy, x._m, M, N, K, out.data_ptr(), dt, ldw, int(accumulate), self._stream(stream)), self._h)
+        return out
+
+    def fp8_gated(self, gate, up, fmt=E4M3, stream=None):
+        """sop_fp8_gated: (h, gate8, up8) of gate, up [M, F]: h = silu(gate) * up in 8 bits, and the 8-bit checkpoints of gate and up."""
+        dt, ldg = self._numbers(gate, "gate")
+        du, ldu = self._numbers(up, "up")
+        if gate.shape != up.shape or dt != du:
+            raise SopError(2, "gate and up must have one shape and type")
+        M, F = gate.shape
+        h, g8, u8 = (Fp8Blocks.empty(M, F, fmt, gate.device) for _ in range(3))
+        _check(lib().sop_fp8_gated(self._h, gate.data_ptr(), ldg, up.data_ptr(), ldu, dt, M, F, h._m, g8._m, u8._m, self._stream(stream)), self._h)
+        return h, g8, u8
+
+    def fp8_gated_grad(self, gate8: Fp8Blocks, up8: Fp8Blocks, dh, fmt=E5M2, stream=None):
+        """sop_fp8_gated_grad: (dgate, dup, dgate8, dup8) from the checkpoints of fp8_gated and dh [M, F]: numbers of dh's type, and 8 bits."""
+        import torch
+        self._here(gate8.codes, up8.codes)
+        dt, ldd = self._numbers(dh, "dh")
+        M, F = dh.shape
+        if gate8.shape != (M, F) or up8.shape != (M, F):
+            raise SopError(2, "the checkpoints and dh must have one shape")
+        dgate, dup = torch.empty((M, F), dtype=dh.dtype, device=dh.device), torch.empty((M, F), dtype=dh.dtype, device=dh.device)
+        g8, u8 = (Fp8Blocks.empty(M, F, fmt, dh.device) for _ in range(2))
+        _check(lib().sop_fp8_gated_grad(self._h, gate8._m, up8._m, dh.data_ptr(), ldd, dt, M, F, dgate.data_ptr(), max(F, 1), dup.data_ptr(), max(F, 1),
+                                        g8._m, u8._m, self._stream(stream)), self._h)
+        return dgate, dup, g8, u8
+
+    def packed_matmul(self, x, w: PackedWeights, out=None, stream=None):
+        """sop_packed_matmul: y [M, N] bfloat16 = x w^T of x [M, K] bfloat16 and a packed layer."""
+        import torch
+        self._here(w.words)
+        _, ldx = self._numbers(x, "x", (torch.bfloat16,))
+        (M, K), N = x.shape, w.shape[0]
+        if K != w.shape[1]:
+            raise SopError(2, f"x has rows of {K} elements, the layer wants {w.shape[1]}")
+        out = self._result(out, M, N, torch.bfloat16, x.device)
+        _, ldy = self._numbers(out, "out", (torch.bfloat16,))
+        _check(lib().sop_packed_matmul(self._h, x.data_ptr(), ldx, w._w, M, out.data_ptr(), ldy, self._stream(stream)), self._h)
         return out

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "sop_kparams.h"
+#include "sop_ctx.h"
 #include "sop_host.h"
 
 using soph::AlphabetPlan;
@@ -169,6 +170,13 @@ struct DeviceGuard {
     ~DeviceGuard() { if (switched) (void)hipSetDevice(prev); }
 };
 }  // namespace
+
+// What the entry points of other translation units see of a context (sop_ctx.h)
+namespace sopc {
+sop_status fail(sop_ctx* c, sop_status s, const char* msg) { return ::fail(c, s, msg); }
+int device(const sop_ctx* c) { return c->device; }
+int compute_units(const sop_ctx* c) { return c->n_cu; }
+}  // namespace sopc
 
 extern "C" const char* sop_last_error(sop_ctx* ctx) { return ctx ? ctx->err.c_str() : soph::host_last_error(); }
 

@@ -1,0 +1,158 @@
+// What the products of a linear layer with narrow operands share between the host side (sop_linear_api.cpp) and the
+// kernels: launch parameters, the rules that choose a variant, and small device helpers.
+#ifndef SOP_LINEAR_H
+#define SOP_LINEAR_H
+#include <stdint.h>
+
+/* Quantiser into 8-bit floats with one power-of-two scale for each block of 128 (rows x 128, rows = 1 or 128) */
+struct F8QuantParams {
+    const void* x; long long ldx;            // elements
+    long long M, K;
+    unsigned char* codes; long long ldc;     // bytes
+    unsigned char* scales; long long lds;    // bytes; [M or ceil(M/128)][ceil(K/128)]
+    unsigned char* codes_t; long long ldct;  // null: not written; [K][M]
+};
+
+/* Gated unit: h = silu(gate) * up, all three into 8 bits */
+struct F8Out { unsigned char* codes; long long ldc; unsigned char* scales; long long lds; };
+struct F8In { const unsigned char* codes; long long ldc; const unsigned char* scales; long long lds; };
+struct F8GatedParams {
+    const void* gate; long long ldg;         // elements
+    const void* up; long long ldu;
+    long long M, F;
+    F8Out h, g8, u8;
+};
+/* ... and its gradient from the 8-bit checkpoints */
+struct F8GatedGradParams {
+    F8In g8, u8;
+    const void* dh; long long lddh;          // elements
+    long long M, F;
+    void* dgate; long long lddg;             // of dh's type
+    void* dup; long long lddu;
+    F8Out dg8, du8;
+};
+
+/* y[m, n] = sum over blocks b of 2^(xs[m, b] + ws[n / 128, b] - 254) sum_{k in b} x[m, k] w[n, k] */
+struct F8MmParams {
+    const unsigned char* x; long long ldx; const unsigned char* xs; long long ldxs;
+    const unsigned char* w; long long ldw; const unsigned char* ws; long long ws_n, ws_k;   // scale of block (n / 128, k / 128) at n * ws_n + k * ws_k
+    int M, N, K;
+    void* y; long long ldy; int out_bf16;
+};
+
+/* dw[n, k] = sum_m dy[m, n] x[m, k] 2^(xs[m, k / 128] - 127) (+ dw) */
+struct WgradParams {
+    const uint16_t* dy; long long lddy;      // bf16
+    const unsigned char* x; long long ldx; const unsigned char* xs; long long ldxs;
+    int M, N, K;
+    void* dw; long long lddw; int out_bf16, accumulate;
+};
+
+/* y[m, n] = sum_k x[m, k] s[n, k / g] L_sel[code[n, k]] */
+#define SOP_K_PACKED_TAB 64
+struct PackedMmParams {
+    const uint16_t* x; long long ldx;        // bf16
+    const uint16_t* words; const unsigned char* payload;
+    int M, N, K, g, n_bits;
+    int mag_shift, mag_mask, man_bits, man_mask, exp_off;   // scale = (mantissa with its leading one) * 2^(max(e, 1) + exp_off)
+    int sign_pos, sel_pos;                   // -1: absent
+    uint16_t* y; long long ldy;              // bf16
+    float tab[2][SOP_K_PACKED_TAB];
+};
+
+#if defined(__HIPCC__)
+namespace sopk {
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+
+// 2^(b - 127); 255 stands for NaN
+__device__ __forceinline__ float e8m0_value(unsigned int b)
+{
+    const unsigned int bits = b == 0 ? 0x00400000u : (b == 255 ? 0x7FC00000u : b << 23);
+    return __uint_as_float(bits);
+}
+// nearest bf16 (ties to even) of a number that is no NaN, or a NaN, in the low 16 bits
+__device__ __forceinline__ unsigned int bf16_bits(float x)
+{
+    return (unsigned int)__builtin_bit_cast(unsigned short, (__bf16)x);
+}
+__device__ __forceinline__ unsigned int bf16_pair(float lo, float hi)
+{
+    v2bf v;
+    v[0] = (__bf16)lo; v[1] = (__bf16)hi;
+    return __builtin_bit_cast(unsigned int, v);
+}
+// eight 8-bit floats times a scale, as bf16: exact
+template <bool E5M2> __device__ __forceinline__ v4i eight_bf16(unsigned int lo, unsigned int hi, float s)
+{
+    v4i r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const unsigned int w = i ? hi : lo;
+        const v2bf a = E5M2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, false) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
+        const v2bf b = E5M2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true);
+        r[2 * i] = __builtin_bit_cast(int, a);
+        r[2 * i + 1] = __builtin_bit_cast(int, b);
+    }
+    return r;
+}
+// The tiles of an operand in LDS: rows of 128 bytes, eight chunks of 16.  Chunk c of row r stands at position c ^ swz(r), so that
+// the 16 rows that one matrix instruction reads at the same c, and rows 2 or 4 apart that a transposing store writes, fall on
+// different banks.
+__device__ __forceinline__ int swz(int r) { return (r ^ (r >> 3)) & 7; }
+
+// One step of 64 elements of a product of bf16 operands whose tiles stand in LDS as above: acc[a][b] holds rows 4q .. 4q + 3 of b's
+// sixteen and column r16 of a's sixteen.
+template <int FA, int FB>
+__device__ __forceinline__ void bf16_step(const unsigned char* ta, const unsigned char* tb, int ra, int rb, int q, v4f (&acc)[FA][FB])
+{
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        v8bf fb[FB];
+#pragma unroll
+        for (int b = 0; b < FB; ++b) { const int r = rb + b * 16; fb[b] = *reinterpret_cast<const v8bf*>(tb + r * 128 + (((4 * s + q) ^ swz(r)) << 4)); }
+#pragma unroll
+        for (int a = 0; a < FA; ++a) {
+            const int r = ra + a * 16;
+            const v8bf fa = *reinterpret_cast<const v8bf*>(ta + r * 128 + (((4 * s + q) ^ swz(r)) << 4));
+#pragma unroll
+            for (int b = 0; b < FB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[b], fa, acc[a][b], 0, 0, 0);
+        }
+    }
+}
+// zeroes the bytes of a 16-byte chunk beyond the first `n`
+__device__ __forceinline__ v4i keep_bytes(v4i v, int n)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = n - 4 * i;
+        v[i] = k >= 4 ? v[i] : k <= 0 ? 0 : (int)((unsigned int)v[i] & ((1u << (8 * k)) - 1u));
+    }
+    return v;
+}
+// What this wavefront's direct loads into LDS still owe has arrived (each wavefront waits for its own before the barrier that
+// lets the others read it).
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned char* to)   // 16 bytes a lane, `to` the wavefront's first
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// Workgroups that follow each other go to the eight XCDs in turn, each with an L2 of its own: XCD i gets the i-th part of the tiles,
+// and walks it in groups of `group` tile rows, so that the tiles in flight on it share their operands' panels.
+__device__ __forceinline__ void tile_of(int id, int n_tiles, int rows, int cols, int group, int& r, int& c)
+{
+    const int per = n_tiles >> 3, rest = n_tiles & 7, xcd = id & 7, k = id >> 3;
+    const int at = xcd * per + (xcd < rest ? xcd : rest) + k;
+    const int in = group * cols, g0 = at / in * group, span = rows - g0 < group ? rows - g0 : group;
+    const int off = at - g0 * cols;
+    r = g0 + off % span;
+    c = off / span;
+}
+}  // namespace sopk
+#endif
+#endif
