@@ -309,20 +309,29 @@ def _up(n, unit):
 
 
 def _spaced(t, unit, what):
-    """A 2-D tensor of bytes as the library reads it: rows a multiple of `unit` bytes apart that may be read to their full width.
-    The tensor itself if it is laid out so, else a copy that is."""
+    """A 2-D tensor of bytes as the library reads it: rows a multiple of `unit` bytes apart that may be read to a multiple of `unit`.
+    The tensor itself if it is laid out so, else a copy that is; and the distance of its rows."""
     import torch
     if t.dim() != 2 or t.element_size() != 1 or not t.is_cuda:
         raise SopError(1, f"{what} must be a 2-D CUDA tensor of one byte an element")
     R, Cc = t.shape
-    ld = t.stride(0) if R > 1 else _up(Cc, unit)
-    if (t.stride(1) == 1 or Cc <= 1) and ld >= Cc and ld % unit == 0 and t.data_ptr() % unit == 0 and \
-            t.untyped_storage().nbytes() - t.storage_offset() >= (R - 1) * ld + _up(Cc, unit):
+    ld, step = t.stride()
+    if R <= 1:
+        ld = _up(Cc, unit)
+    if (step == 1 or Cc <= 1) and ld >= Cc and ld % unit == 0 and t.data_ptr() % unit == 0 and \
+            (Cc % unit == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= (R - 1) * ld + _up(Cc, unit)):
         return t, ld
     ld = _up(Cc, unit)
     buf = torch.zeros((R, ld), dtype=torch.uint8, device=t.device)
-    buf[:, :Cc] = t.view(torch.uint8) if t.is_contiguous() else t.contiguous().view(torch.uint8)
+    buf[:, :Cc] = t.contiguous().view(torch.uint8)
     return buf.view(t.dtype)[:, :Cc], ld
+
+
+def _room(torch, R, Cc, unit, dtype, device):
+    """An uninitialised [R, Cc] of bytes laid out so, and the distance of its rows."""
+    ld = -(-Cc // unit) * unit
+    t = torch.empty((R, ld), dtype=dtype, device=device)
+    return (t if ld == Cc else t[:, :Cc]), ld
 
 
 class Fp8Blocks:
@@ -330,14 +339,14 @@ class Fp8Blocks:
     each block of `rows` x 128 (rows = 1: activations and gradients; rows = 128: weights).  codes_t: the same codes as a [C, R]
     matrix, where the product over the other index is wanted too.  Tensors that are not laid out as the library reads them (rows of
     codes 16 bytes apart, of scales 4) are copied, once."""
-    __slots__ = ("codes", "scales", "rows", "codes_t", "shape", "_m", "_t")
+    __slots__ = ("codes", "scales", "rows", "codes_t", "shape", "device", "_m", "_t")
 
     def __init__(self, codes, scales, rows: int = 1, codes_t=None):
         import torch
-        fmt = E4M3 if codes.dtype == torch.float8_e4m3fn else E5M2 if codes.dtype == torch.float8_e5m2 else None
+        fmt = E4M3 if codes.dtype is torch.float8_e4m3fn else E5M2 if codes.dtype is torch.float8_e5m2 else None
         if fmt is None:
             raise SopError(1, "codes must be float8_e4m3fn or float8_e5m2")
-        if scales.dtype not in (torch.float8_e8m0fnu, torch.uint8):
+        if scales.dtype is not torch.float8_e8m0fnu and scales.dtype is not torch.uint8:
             raise SopError(1, "scales must be float8_e8m0fnu (or its bytes)")
         if rows not in (1, 128):
             raise SopError(1, "blocks have 1 or 128 rows")
@@ -346,32 +355,45 @@ class Fp8Blocks:
         R, K = codes.shape
         if tuple(scales.shape) != (-(-R // rows), -(-K // 128)):
             raise SopError(2, f"codes of {R} x {K} in blocks of {rows} x 128 have scales of {-(-R // rows)} x {-(-K // 128)}")
-        if scales.device != codes.device:
+        self.device = codes.get_device()
+        if scales.get_device() != self.device:
             raise SopError(1, "codes and scales must be on one GPU")
         self.rows, self.shape, self.codes_t, self._t = rows, (R, K), None, None
         self._m = _F8Matrix(self.codes.data_ptr(), ld, self.scales.data_ptr(), lds, fmt, rows)
         if codes_t is not None:
-            if rows != 128 or codes_t.dtype != codes.dtype or tuple(codes_t.shape) != (K, R) or codes_t.device != codes.device:
+            if rows != 128 or codes_t.dtype is not codes.dtype or tuple(codes_t.shape) != (K, R) or codes_t.get_device() != self.device:
                 raise SopError(2, "codes_t must be the codes of 128 x 128 blocks, transposed")
             self.codes_t, ldt = _spaced(codes_t, 16, "codes_t")
             self._t = _F8Matrix(self.codes_t.data_ptr(), ldt, self.scales.data_ptr(), lds, fmt, rows)
 
     @classmethod
-    def empty(cls, R, K, dtype, device, rows: int = 1, transposed: bool = False):
+    def empty(cls, R, K, fmt, device, rows: int = 1, transposed: bool = False):
+        """Uninitialised, to be written by a call of the library.  fmt: E4M3, E5M2 or the torch type."""
         import torch
-        dt = {E4M3: torch.float8_e4m3fn, E5M2: torch.float8_e5m2}.get(dtype, dtype)
-
-        def room(r, c, unit, t):
-            ld = _up(c, unit)
-            return torch.empty((r, ld), dtype=t, device=device) if ld == c else torch.empty((r, ld), dtype=t, device=device)[:, :c]
-
-        return cls(room(R, K, 16, dt), room(-(-R // rows), -(-K // 128), 4, torch.float8_e8m0fnu), rows, room(K, R, 16, dt) if transposed else None)
+        if fmt == E4M3 or fmt is torch.float8_e4m3fn:
+            fmt, dt = E4M3, torch.float8_e4m3fn
+        elif fmt == E5M2 or fmt is torch.float8_e5m2:
+            fmt, dt = E5M2, torch.float8_e5m2
+        else:
+            raise SopError(1, "the format must be E4M3 or E5M2")
+        if rows != 1 and rows != 128:
+            raise SopError(1, "blocks have 1 or 128 rows")
+        q = cls.__new__(cls)
+        q.codes, ld = _room(torch, R, K, 16, dt, device)
+        q.scales, lds = _room(torch, -(-R // rows), -(-K // 128), 4, torch.float8_e8m0fnu, device)
+        q.rows, q.shape, q.device, q.codes_t, q._t = rows, (R, K), q.codes.get_device(), None, None
+        at = q.scales.data_ptr()
+        q._m = _F8Matrix(q.codes.data_ptr(), ld, at, lds, fmt, rows)
+        if transposed:
+            q.codes_t, ldt = _room(torch, K, R, 16, dt, device)
+            q._t = _F8Matrix(q.codes_t.data_ptr(), ldt, at, lds, fmt, rows)
+        return q
 
 
 class PackedWeights:
     """A packed layer [N, K] as it is held for products: what pack_blocks / search_layer(pack=True) wrote (words, payload, n_bits), its
     codebooks (one table, or two where the words carry a selector) and the scale format and layer shift k of the search."""
-    __slots__ = ("words", "payload", "shape", "tables", "_w")
+    __slots__ = ("words", "payload", "shape", "tables", "device", "_w")
 
     def __init__(self, words, payload, N, K, g, n_bits, fmt: ScaleFmt, tables, k: int = 0):
         import torch
@@ -383,7 +405,7 @@ class PackedWeights:
             raise SopError(2, "words and payload do not hold N x K weights in blocks of g with n_bits codes")
         if not 1 <= len(tables) <= 2:
             raise SopError(3, "one codebook or two")
-        self.words, self.payload, self.shape = words, payload, (N, K)
+        self.words, self.payload, self.shape, self.device = words, payload, (N, K), words.get_device()
         self.tables = [np.ascontiguousarray(t, dtype=np.float32) for t in tables]
         a, b = self.tables[0], self.tables[1] if len(tables) == 2 else None
         self._w = _Packed(words.data_ptr(), payload.data_ptr(), N, K, g, n_bits, fmt, k, _fp(a), a.size, None if b is None else _fp(b), 0 if b is None else b.size)
@@ -400,6 +422,11 @@ class Context:
         self.n_entries = []
         self.n_pairs = 0
         self._ws = None
+        import torch
+        self._lib, self._bf16, self._f32 = lib(), torch.bfloat16, torch.float32
+        self._dtypes = {torch.float32: F32, torch.bfloat16: BF16}
+        # the current stream's handle, without an object around it where torch can give it so
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
     def close(self):
         if self._h:
@@ -756,37 +783,38 @@ class Context:
                                      C.c_void_p(st)), self._h)
         return out
 
-    # ---- products of a linear layer with narrow operands
+    # ---- products of a linear layer with narrow operands (calls of a few microseconds: their Python side is kept short)
 
-    def _here(self, *tensors):
-        for t in tensors:
-            if not t.is_cuda or t.device.index != self.device:
-                raise SopError(1, "tensors must be on the context's GPU (no CPU fallback)")
+    def _here(self, *matrices):
+        for q in matrices:
+            if q.device != self.device:
+                raise SopError(1, "operands must be on the context's GPU (no CPU fallback)")
 
-    def _stream(self, stream):
-        import torch
-        return torch.cuda.current_stream(self.device).cuda_stream if stream is None else stream
+    def _numbers(self, x, what, bf16_only=False):
+        """(sop_dtype, row stride) of a matrix of numbers on the context's GPU."""
+        if x.get_device() != self.device:
+            raise SopError(1, f"{what} must be on the context's GPU (no CPU fallback)")
+        dt = self._dtypes.get(x.dtype)
+        if dt is None or (bf16_only and dt != BF16):
+            raise SopError(1, f"{what} must be " + ("bfloat16" if bf16_only else "float32 or bfloat16"))
+        if x.dim() != 2:
+            raise SopError(2, f"{what} must be a 2-D tensor")
+        R, Cc = x.shape
+        ld, step = x.stride()
+        if step != 1 and Cc > 1:
+            raise SopError(2, f"{what} must have contiguous rows")
+        return dt, (ld if R > 1 else -(-Cc // 8) * 8)                # (of one row the stride says nothing)
 
-    def _numbers(self, x, what, dtypes=None):
-        """(sop_dtype, row stride) of a matrix of numbers."""
-        import torch
-        self._here(x)
-        if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
-            raise SopError(2, f"{what} must be a 2-D tensor with contiguous rows")
-        if x.dtype not in (dtypes or (torch.float32, torch.bfloat16)):
-            raise SopError(1, f"{what} must be " + ("bfloat16" if dtypes else "float32 or bfloat16"))
-        return (BF16 if x.dtype == torch.bfloat16 else F32), (x.stride(0) if x.shape[0] > 1 else _up(x.shape[1], 8))
-
-    def _result(self, out, M, N, dtype, device):
-        """A matrix to write to: `out` if it fits, else a new one."""
-        import torch
+    def _result(self, out, M, N, dtype, x):
+        """(matrix to write to, its sop_dtype, row stride): `out` if it fits, else a new one beside x."""
         if out is None:
-            if dtype not in (torch.float32, torch.bfloat16):
+            dt = self._dtypes.get(dtype)
+            if dt is None:
                 raise SopError(1, "results are float32 or bfloat16")
-            return torch.empty((M, N), dtype=dtype, device=device)
+            return x.new_empty((M, N), dtype=dtype), dt, N
         if tuple(out.shape) != (M, N):
             raise SopError(2, f"out must be {M} x {N}")
-        return out
+        return (out, *self._numbers(out, "out"))
 
     def fp8_quantize(self, x, rows: int = 1, fmt=E4M3, transposed: bool = False, stream=None) -> Fp8Blocks:
         """sop_fp8_quantize: x [M, K] float32 or bfloat16 into 8 bits (fmt: E4M3 / E5M2, or the torch type) with one power-of-two scale for
@@ -796,39 +824,44 @@ class Context:
             raise SopError(1, "a transposed copy is made of 128 x 128 blocks only")
         M, K = x.shape
         q = Fp8Blocks.empty(M, K, fmt, x.device, rows, transposed)
-        _check(lib().sop_fp8_quantize(self._h, x.data_ptr(), dt, M, K, ldx, q._m, q._t.codes if transposed else None, q._t.ld_codes if transposed else 0,
-                                      self._stream(stream)), self._h)
+        s = self._lib.sop_fp8_quantize(self._h, x.data_ptr(), dt, M, K, ldx, q._m, q._t.codes if transposed else None, q._t.ld_codes if transposed else 0,
+                                       self._raw_stream(self.device) if stream is None else stream)
+        if s:
+            _check(s, self._h)
         return q
 
     def fp8_matmul(self, x: Fp8Blocks, w: Fp8Blocks, transposed: bool = False, dtype=None, out=None, stream=None):
         """sop_fp8_matmul: y = x w^T of x [M, K] (rows = 1) and w [N, K] (rows = 128); transposed: y = x w of x [M, N] and the same w by its
         codes_t (the input gradient).  dtype: bfloat16 (default) or float32; or `out`, a matrix of either type to write to."""
-        import torch
-        self._here(x.codes, w.codes)
+        self._here(x, w)
         if transposed and w._t is None:
             raise SopError(1, "the transposed product needs the weight's codes_t (fp8_quantize(..., transposed=True))")
-        (M, K), (N, Kw) = x.shape, (w.shape[::-1] if transposed else w.shape)
+        M, K = x.shape
+        Kw, N = w.shape if transposed else w.shape[::-1]
         if K != Kw:
             raise SopError(2, f"x has rows of {K} elements, the weight wants {Kw}")
-        out = self._result(out, M, N, torch.bfloat16 if dtype is None else dtype, x.codes.device)
-        dt, ldy = self._numbers(out, "out")
-        _check(lib().sop_fp8_matmul(self._h, x._m, w._t if transposed else w._m, int(transposed), M, N, K, out.data_ptr(), dt, ldy, self._stream(stream)), self._h)
+        out, dt, ldy = self._result(out, M, N, dtype or self._bf16, x.codes)
+        s = self._lib.sop_fp8_matmul(self._h, x._m, w._t if transposed else w._m, transposed, M, N, K, out.data_ptr(), dt, ldy,
+                                     self._raw_stream(self.device) if stream is None else stream)
+        if s:
+            _check(s, self._h)
         return out
 
     def fp8_weight_grad(self, dy, x: Fp8Blocks, dtype=None, out=None, accumulate: bool = False, stream=None):
         """sop_fp8_weight_grad: dw [N, K] = dy^T x from dy [M, N] bfloat16 and the 8-bit checkpoint x [M, K] (rows = 1); dtype: float32 (default)
         or bfloat16; accumulate: added to `out`."""
-        import torch
-        self._here(x.codes)
-        _, lddy = self._numbers(dy, "dy", (torch.bfloat16,))
+        self._here(x)
+        _, lddy = self._numbers(dy, "dy", True)
         (M, N), K = dy.shape, x.shape[1]
         if x.shape[0] != M:
             raise SopError(2, f"dy has {M} rows, the checkpoint {x.shape[0]}")
         if accumulate and out is None:
             raise SopError(1, "accumulate needs out")
-        out = self._result(out, N, K, torch.float32 if dtype is None else dtype, dy.device)
-        dt, ldw = self._numbers(out, "out")
-        _check(lib().sop_fp8_weight_grad(self._h, dy.data_ptr(), lddy, x._m, M, N, K, out.data_ptr(), dt, ldw, int(accumulate), self._stream(stream)), self._h)
+        out, dt, ldw = self._result(out, N, K, dtype or self._f32, dy)
+        s = self._lib.sop_fp8_weight_grad(self._h, dy.data_ptr(), lddy, x._m, M, N, K, out.data_ptr(), dt, ldw, accumulate,
+                                          self._raw_stream(self.device) if stream is None else stream)
+        if s:
+            _check(s, self._h)
         return out
 
     def fp8_gated(self, gate, up, fmt=E4M3, stream=None):
@@ -838,33 +871,41 @@ class Context:
         if gate.shape != up.shape or dt != du:
             raise SopError(2, "gate and up must have one shape and type")
         M, F = gate.shape
-        h, g8, u8 = (Fp8Blocks.empty(M, F, fmt, gate.device) for _ in range(3))
-        _check(lib().sop_fp8_gated(self._h, gate.data_ptr(), ldg, up.data_ptr(), ldu, dt, M, F, h._m, g8._m, u8._m, self._stream(stream)), self._h)
+        dev = gate.device
+        h, g8, u8 = Fp8Blocks.empty(M, F, fmt, dev), Fp8Blocks.empty(M, F, fmt, dev), Fp8Blocks.empty(M, F, fmt, dev)
+        s = self._lib.sop_fp8_gated(self._h, gate.data_ptr(), ldg, up.data_ptr(), ldu, dt, M, F, h._m, g8._m, u8._m,
+                                    self._raw_stream(self.device) if stream is None else stream)
+        if s:
+            _check(s, self._h)
         return h, g8, u8
 
     def fp8_gated_grad(self, gate8: Fp8Blocks, up8: Fp8Blocks, dh, fmt=E5M2, stream=None):
         """sop_fp8_gated_grad: (dgate, dup, dgate8, dup8) from the checkpoints of fp8_gated and dh [M, F]: numbers of dh's type, and 8 bits."""
-        import torch
-        self._here(gate8.codes, up8.codes)
+        self._here(gate8, up8)
         dt, ldd = self._numbers(dh, "dh")
         M, F = dh.shape
         if gate8.shape != (M, F) or up8.shape != (M, F):
             raise SopError(2, "the checkpoints and dh must have one shape")
-        dgate, dup = torch.empty((M, F), dtype=dh.dtype, device=dh.device), torch.empty((M, F), dtype=dh.dtype, device=dh.device)
-        g8, u8 = (Fp8Blocks.empty(M, F, fmt, dh.device) for _ in range(2))
-        _check(lib().sop_fp8_gated_grad(self._h, gate8._m, up8._m, dh.data_ptr(), ldd, dt, M, F, dgate.data_ptr(), max(F, 1), dup.data_ptr(), max(F, 1),
-                                        g8._m, u8._m, self._stream(stream)), self._h)
+        dev = dh.device
+        dgate, dup = dh.new_empty((M, F)), dh.new_empty((M, F))
+        g8, u8 = Fp8Blocks.empty(M, F, fmt, dev), Fp8Blocks.empty(M, F, fmt, dev)
+        s = self._lib.sop_fp8_gated_grad(self._h, gate8._m, up8._m, dh.data_ptr(), ldd, dt, M, F, dgate.data_ptr(), F, dup.data_ptr(), F, g8._m, u8._m,
+                                         self._raw_stream(self.device) if stream is None else stream)
+        if s:
+            _check(s, self._h)
         return dgate, dup, g8, u8
 
     def packed_matmul(self, x, w: PackedWeights, out=None, stream=None):
         """sop_packed_matmul: y [M, N] bfloat16 = x w^T of x [M, K] bfloat16 and a packed layer."""
-        import torch
-        self._here(w.words)
-        _, ldx = self._numbers(x, "x", (torch.bfloat16,))
-        (M, K), N = x.shape, w.shape[0]
-        if K != w.shape[1]:
-            raise SopError(2, f"x has rows of {K} elements, the layer wants {w.shape[1]}")
-        out = self._result(out, M, N, torch.bfloat16, x.device)
-        _, ldy = self._numbers(out, "out", (torch.bfloat16,))
-        _check(lib().sop_packed_matmul(self._h, x.data_ptr(), ldx, w._w, M, out.data_ptr(), ldy, self._stream(stream)), self._h)
+        self._here(w)
+        _, ldx = self._numbers(x, "x", True)
+        (M, K), (N, Kw) = x.shape, w.shape
+        if K != Kw:
+            raise SopError(2, f"x has rows of {K} elements, the layer wants {Kw}")
+        out, dt, ldy = self._result(out, M, N, self._bf16, x)
+        if dt != BF16:
+            raise SopError(1, "out must be bfloat16")
+        s = self._lib.sop_packed_matmul(self._h, x.data_ptr(), ldx, w._w, M, out.data_ptr(), ldy, self._raw_stream(self.device) if stream is None else stream)
+        if s:
+            _check(s, self._h)
         return out
