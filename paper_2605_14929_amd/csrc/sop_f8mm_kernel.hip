@@ -9,29 +9,17 @@
 //         whose sums are binary32 throughout (1e-7 off), at half the rate.
 #include <hip/hip_runtime.h>
 
-#include <type_traits>
-
 #include "sop_linear.h"
 
 namespace sopk {
 
-__device__ __forceinline__ v4f mfma_f8(v8i w, v8i x, v4f acc, std::integral_constant<int, 0>, int sw, int sx)
+template <int XF> __device__ __forceinline__ v4f mfma_f8(v8i w, v8i x, v4f acc, int sw, int sx)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 0, 0, sw, 0, sx);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, XF, 0, sw, 0, sx);
 }
-__device__ __forceinline__ v4f mfma_f8(v8i w, v8i x, v4f acc, std::integral_constant<int, 1>, int sw, int sx)
+template <int XF> __device__ __forceinline__ v16f mfma_f8(v8i w, v8i x, v16f acc, int sw, int sx)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 1, 0, sw, 0, sx);
-}
-
-template <bool E5M2> __device__ __forceinline__ v4f mfma_exact(v8i w, v8i x, v4f acc, int sw, int sx)
-{
-    const float fw = e8m0_value((unsigned int)sw), fx = e8m0_value((unsigned int)sx);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, eight_bf16<false>(w[2 * i], w[2 * i + 1], fw)),
-                                                      __builtin_bit_cast(v8bf, eight_bf16<E5M2>(x[2 * i], x[2 * i + 1], fx)), acc, 0, 0, 0);
-    return acc;
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, acc, 0, XF, 0, sw, 0, sx);
 }
 
 // four neighbouring columns of a row of y
@@ -58,135 +46,176 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
     }
 }
 
-// ---- tiles: BM x BN of y by WR x WC wavefronts, 128 elements along K a step, two steps in LDS.
-template <int BM, int BN, int WR, int WC, int XF>
+// ---- tiles: BM x BN of y by WR x WC wavefronts, 128 elements along K a step, two steps in LDS.  A wavefront's part is made of 32 x 32
+// squares.  In LDS a row is eight chunks of 16 bytes, chunk c at position c ^ (row & 7): rows eight apart lie alike, so that all
+// squares are read at constant distances, and eight neighbouring rows fall on different banks.
+template <int BM, int BN, int WR, int WC, int XF, bool EXACT>
 __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
-    constexpr int NT = WR * WC * 64, FM = BM / WR / 16, FN = BN / WC / 16, CX = BM * 8 / NT, CW = BN * 8 / NT;
+    constexpr int NT = WR * WC * 64, FM = BM / WR / 32, FN = BN / WC / 32, CX = BM * 8 / NT, CW = BN * 8 / NT;
     constexpr int STAGE = (BM + BN) * 128;
     static_assert(BN / WC <= 128 && 128 % (BN / WC) == 0, "a wavefront's columns share a scale of w");
+    static_assert(NT % 64 == 0 && FM * WR * 32 == BM && FN * WC * 32 == BN, "whole squares");
     extern __shared__ __align__(16) unsigned char lds[];
     int tm, tn;
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
-    const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WC * (BM / WR), wn = wave % WC * (BN / WC);
     const unsigned char* xb = p.x + (long long)m0 * p.ldx;
     const unsigned char* wb = p.w + (long long)n0 * p.ldw;
+    const int KF = p.K >> 7, KB = (p.K + 127) >> 7;                     // whole steps, all steps
     unsigned int ox[CX], ow[CW];                                        // byte offsets of this thread's chunks; rows beyond the matrix read its last
 #pragma unroll
     for (int i = 0; i < CX; ++i) {
         const int c = i * NT + tid, r = c >> 3;
-        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + (((c & 7) ^ swz(r)) << 4);
+        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + (((c ^ r) & 7) << 4);
     }
 #pragma unroll
     for (int i = 0; i < CW; ++i) {
         const int c = i * NT + tid, r = c >> 3;
-        ow[i] = (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw + (((c & 7) ^ swz(r)) << 4);
+        ow[i] = (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw + (((c ^ r) & 7) << 4);
     }
-    const int KB = (p.K + 127) >> 7;
-
+    const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
+    const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
     auto load = [&](int kt) {
-        unsigned char* to = lds + (kt & 1) * STAGE;
-        const unsigned char* xk = xb + (long long)kt * 128;
-        const unsigned char* wk = wb + (long long)kt * 128;
-        if (kt * 128 + 128 <= p.K) {
+        unsigned char* to = lds + (kt & 1) * STAGE + (wave << 10);
 #pragma unroll
-            for (int i = 0; i < CX; ++i)
-                load_to_lds(xk + ox[i], to + (i * NT + (wave << 6)) * 16);
+        for (int i = 0; i < CX; ++i) load_to_lds(xw, ox[i], kt * 128, to + i * NT * 16);
 #pragma unroll
-            for (int i = 0; i < CW; ++i)
-                load_to_lds(wk + ow[i], to + BM * 128 + (i * NT + (wave << 6)) * 16);
-        } else {                                                        // the last step of an odd K: elements beyond it count as zeros
-            const int left = p.K - kt * 128;
-#pragma unroll
-            for (int i = 0; i < CX; ++i) {
-                const int c = i * NT + tid, n = left - (((c & 7) ^ swz(c >> 3)) << 4);
-                v4i v = {0, 0, 0, 0};
-                if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(xk + ox[i]), n);
-                *reinterpret_cast<v4i*>(to + c * 16) = v;
-            }
-#pragma unroll
-            for (int i = 0; i < CW; ++i) {
-                const int c = i * NT + tid, n = left - (((c & 7) ^ swz(c >> 3)) << 4);
-                v4i v = {0, 0, 0, 0};
-                if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(wk + ow[i]), n);
-                *reinterpret_cast<v4i*>(to + BM * 128 + c * 16) = v;
-            }
-        }
+        for (int i = 0; i < CW; ++i) load_to_lds(ww, ow[i], kt * 128, to + BM * 128 + i * NT * 16);
     };
 
-    // scales: four steps of a row of x in a word; the four of w likewise
-    const int r16 = lane & 15, q = lane >> 4;
-    unsigned int sxo[FM];
-#pragma unroll
-    for (int f = 0; f < FM; ++f) sxo[f] = (unsigned int)min(wm + f * 16 + r16, p.M - 1 - m0) * (unsigned int)p.ldxs;
-    const unsigned char* xsb = p.xs + (long long)m0 * p.ldxs;
+    // scales: four steps of a row of x in a word, four of w likewise; the next four are asked for while these are used
+    const int r32 = lane & 31, h = lane >> 5;
+    const Window xsw = window(p.xs + (long long)m0 * p.ldxs, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldxs + (unsigned int)((KB + 3) & ~3));
     const unsigned char* wsb = p.ws + (long long)min((n0 + wn) >> 7, (p.N - 1) >> 7) * p.ws_n;
-    unsigned int sx[FM], sw = 0;
-    auto scales = [&](int kt) {                                         // kt a multiple of four
+    unsigned int sxo[FM], sx[FM], nx[FM], sw, nw[4];                     // (bytes of w stay apart until they are used: to join them is to wait for them)
 #pragma unroll
-        for (int f = 0; f < FM; ++f) sx[f] = *reinterpret_cast<const unsigned int*>(xsb + sxo[f] + kt);
-        sw = 0;
+    for (int f = 0; f < FM; ++f) sxo[f] = (unsigned int)min(wm + f * 32 + r32, p.M - 1 - m0) * (unsigned int)p.ldxs;
+    auto scales = [&](int kt) {                                         // kt a multiple of four, below KB
 #pragma unroll
-        for (int j = 0; j < 4; ++j) if (kt + j < KB) sw |= (unsigned int)wsb[(long long)(kt + j) * p.ws_k] << (8 * j);
+        for (int f = 0; f < FM; ++f) nx[f] = load_word(xsw, sxo[f], kt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) nw[j] = wsb[(long long)min(kt + j, KB - 1) * p.ws_k];
     };
 
-    v4f acc[FM][FN];
+    v16f acc[FM][FN];
 #pragma unroll
     for (int a = 0; a < FM; ++a)
 #pragma unroll
-        for (int b = 0; b < FN; ++b) acc[a][b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b = 0; b < FN; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
 
-    // where this lane's 32 bytes of a row of 16 rows lie: chunks 2q and 2q + 1
-    auto frag = [&](const unsigned char* tile, int row) {
-        const v4i lo = *reinterpret_cast<const v4i*>(tile + row * 128 + (((2 * q) ^ swz(row)) << 4));
-        const v4i hi = *reinterpret_cast<const v4i*>(tile + row * 128 + (((2 * q + 1) ^ swz(row)) << 4));
+    // this lane's 64 bytes of a row: chunks 2h, 2h + 1 (the first 64 elements' share) and 4 + 2h, 5 + 2h
+    const unsigned int sz = (unsigned int)(r32 & 7), row_x = (unsigned int)(wm + r32) * 128, row_w = (unsigned int)(BM + wn + r32) * 128;
+    const unsigned int c0 = ((unsigned int)(2 * h) ^ sz) << 4;
+    auto frag = [&](const unsigned char* half, unsigned int row, int f, int j) {
+        const unsigned int c = c0 ^ (j << 6);
+        const v4i lo = *reinterpret_cast<const v4i*>(half + (row + c) + f * 4096);
+        const v4i hi = *reinterpret_cast<const v4i*>(half + (row + (c ^ 16)) + f * 4096);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-
-    load(0);
-    for (int kt = 0; kt < KB; ++kt) {
-        if ((kt & 3) == 0) scales(kt);
-        wait_loads();
-        __syncthreads();                                                // this step has arrived, and nobody reads the other half any more
-        if (kt + 1 < KB) load(kt + 1);
-        const unsigned char* tx = lds + (kt & 1) * STAGE;
-        const unsigned char* tw = tx + BM * 128;
-        v8i w[FN];
+    auto compute = [&](int kt) {
+        const unsigned char* half = lds + (kt & 1) * STAGE;
 #pragma unroll
-        for (int b = 0; b < FN; ++b) w[b] = frag(tw, wn + b * 16 + r16);
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (EXACT) {
+                v4i w[FN][4];
+                const float fw = e8m0_value(sw & 255u);
 #pragma unroll
-        for (int a = 0; a < FM; ++a) {
-            const v8i x = frag(tx, wm + a * 16 + r16);
+                for (int b = 0; b < FN; ++b) {
+                    const v8i c = frag(half, row_w, b, j);
 #pragma unroll
-            for (int b = 0; b < FN; ++b) acc[a][b] = mfma_f8(w[b], x, acc[a][b], std::integral_constant<int, XF>{}, (int)sw, (int)sx[a]);
+                    for (int i = 0; i < 4; ++i) w[b][i] = eight_bf16<false>(c[2 * i], c[2 * i + 1], fw);
+                }
+#pragma unroll
+                for (int a = 0; a < FM; ++a) {
+                    const v8i c = frag(half, row_x, a, j);
+                    const float fx = e8m0_value(sx[a] & 255u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const v8bf x = __builtin_bit_cast(v8bf, eight_bf16<XF == 1>(c[2 * i], c[2 * i + 1], fx));
+#pragma unroll
+                        for (int b = 0; b < FN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, w[b][i]), x, acc[a][b], 0, 0, 0);
+                    }
+                }
+            } else {
+                v8i w[FN];
+#pragma unroll
+                for (int b = 0; b < FN; ++b) w[b] = frag(half, row_w, b, j);
+#pragma unroll
+                for (int a = 0; a < FM; ++a) {
+                    const v8i x = frag(half, row_x, a, j);
+#pragma unroll
+                    for (int b = 0; b < FN; ++b) acc[a][b] = mfma_f8<XF>(w[b], x, acc[a][b], (int)sw, (int)sx[a]);
+                }
+            }
         }
 #pragma unroll
         for (int f = 0; f < FM; ++f) sx[f] >>= 8;
         sw >>= 8;
+    };
+    auto turn = [&](int kt) {                                           // before step kt: its scales into place, the next ones asked for
+        if ((kt & 3) == 0) {
+#pragma unroll
+            for (int f = 0; f < FM; ++f) sx[f] = nx[f];
+            sw = nw[0] | nw[1] << 8 | nw[2] << 16 | nw[3] << 24;
+            if (kt + 4 < KB) scales(kt + 4);
+        }
+    };
+
+    scales(0);
+    if (KF) load(0);
+    for (int kt = 0; kt < KF; ++kt) {
+        wait_loads();
+        __syncthreads();                                                // this step has arrived, and nobody reads the other half any more
+        if (kt + 1 < KF) load(kt + 1);
+        turn(kt);
+        compute(kt);
+    }
+    if (KF < KB) {                                                      // the last step of an odd K: elements beyond it count as zeros
+        unsigned char* to = lds + (KF & 1) * STAGE;
+        const int left = p.K & 127;
+#pragma unroll 1
+        for (int c = tid; c < (BM + BN) * 8; c += NT) {
+            const bool of_x = c < BM * 8;
+            const int d = of_x ? c : c - BM * 8, r = d >> 3, col = ((d ^ r) & 7) << 4, n = left - col;
+            const unsigned char* row = of_x ? xb + (long long)min(r, p.M - 1 - m0) * p.ldx : wb + (long long)min(r, p.N - 1 - n0) * p.ldw;
+            v4i v = {0, 0, 0, 0};
+            if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + col), n);
+            *reinterpret_cast<v4i*>(to + c * 16) = v;
+        }
+        __syncthreads();
+        turn(KF);
+        compute(KF);
     }
 #pragma unroll
     for (int a = 0; a < FM; ++a)
 #pragma unroll
-        for (int b = 0; b < FN; ++b) store_y(p, m0 + wm + a * 16 + r16, n0 + wn + b * 16 + 4 * q, acc[a][b]);
+        for (int b = 0; b < FN; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * h, v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
 }
 
-// ---- few rows of x: FM x 16 of them by FN x 16 columns a workgroup, K dealt out to its eight wavefronts step by step.  Operands go
-// from memory to registers as the matrix instruction wants them; the wavefronts' sums meet in LDS in a fixed order.
-template <int FM, int FN, int XF, bool EXACT>
-__global__ __launch_bounds__(512) void f8mm_rows_kernel(const F8MmParams p)
+// ---- few tiles: FM x 16 rows of x by FN x 16 columns a workgroup, K dealt out to its W wavefronts, U steps at a time.  Operands go from
+// memory to registers as the matrix instruction wants them; the wavefronts' sums meet in LDS in a fixed order.
+template <int FM, int FN, int U, int W, int XF, bool EXACT>
+__global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
-    constexpr int W = 8;
     __shared__ v4f part[W][FM][FN][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
-    const int n0 = blockIdx.x * (FN * 16), KB = (p.K + 127) >> 7;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
+    int tm, tn;
+    tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
+    const int m0 = tm * (FM * 16), n0 = tn * (FN * 16), KF = p.K >> 7, KB = (p.K + 127) >> 7;
     const unsigned char* xr[FM];
     const unsigned char* xsr[FM];
     const unsigned char* wr[FN];
     const unsigned char* wsr[FN];
 #pragma unroll
     for (int a = 0; a < FM; ++a) {
-        const int m = min(a * 16 + r16, p.M - 1);
+        const int m = min(m0 + a * 16 + r16, p.M - 1);
         xr[a] = p.x + (long long)m * p.ldx + q * 32;
         xsr[a] = p.xs + (long long)m * p.ldxs;
     }
@@ -201,32 +230,61 @@ __global__ __launch_bounds__(512) void f8mm_rows_kernel(const F8MmParams p)
     for (int a = 0; a < FM; ++a)
 #pragma unroll
         for (int b = 0; b < FN; ++b) acc[a][b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    auto get = [&](const unsigned char* row, int kt) {                  // 32 bytes of a row; rows are readable up to a multiple of 16
-        const unsigned char* at = row + (long long)kt * 128;
-        v4i lo, hi;
-        if (kt * 128 + 128 <= p.K) {
-            lo = *reinterpret_cast<const v4i*>(at);
-            hi = *reinterpret_cast<const v4i*>(at + 16);
-        } else {
-            const int left = p.K - kt * 128 - q * 32;
-            lo = v4i{0, 0, 0, 0}; hi = lo;
-            if (left > 0) lo = keep_bytes(*reinterpret_cast<const v4i*>(at), left);
-            if (left > 16) hi = keep_bytes(*reinterpret_cast<const v4i*>(at + 16), left - 16);
-        }
+    auto whole = [&](const unsigned char* row, int kt) {                // 32 bytes of a row
+        const v4i lo = *reinterpret_cast<const v4i*>(row + (long long)kt * 128), hi = *reinterpret_cast<const v4i*>(row + (long long)kt * 128 + 16);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    for (int kt = wave; kt < KB; kt += W) {
+    auto rest = [&](const unsigned char* row) {                         // ... of the last step of an odd K (rows are readable up to a multiple of 16)
+        const int left = (p.K & 127) - q * 32;
+        v4i lo = {0, 0, 0, 0}, hi = lo;
+        if (left > 0) lo = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128), left);
+        if (left > 16) hi = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + 16), left - 16);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto add = [&](const v8i (&x)[FM], const v8i (&w)[FN], const int (&sx)[FM], const int (&sw)[FN]) {
+        if constexpr (EXACT) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v8bf fx[FM], fw[FN];
+#pragma unroll
+                for (int a = 0; a < FM; ++a) fx[a] = __builtin_bit_cast(v8bf, eight_bf16<XF == 1>(x[a][2 * i], x[a][2 * i + 1], e8m0_value((unsigned int)sx[a])));
+#pragma unroll
+                for (int b = 0; b < FN; ++b) fw[b] = __builtin_bit_cast(v8bf, eight_bf16<false>(w[b][2 * i], w[b][2 * i + 1], e8m0_value((unsigned int)sw[b])));
+#pragma unroll
+                for (int a = 0; a < FM; ++a)
+#pragma unroll
+                    for (int b = 0; b < FN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[b], fx[a], acc[a][b], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int a = 0; a < FM; ++a)
+#pragma unroll
+                for (int b = 0; b < FN; ++b) acc[a][b] = mfma_f8<XF>(w[b], x[a], acc[a][b], sw[b], sx[a]);
+        }
+    };
+    int kt = wave;
+    for (; kt + (U - 1) * W < KF; kt += U * W) {                        // U steps in flight
+        v8i x[U][FM], w[U][FN];
+        int sx[U][FM], sw[U][FN];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int b = 0; b < FN; ++b) { w[u][b] = whole(wr[b], kt + u * W); sw[u][b] = wsr[b][(long long)(kt + u * W) * p.ws_k]; }
+#pragma unroll
+            for (int a = 0; a < FM; ++a) { x[u][a] = whole(xr[a], kt + u * W); sx[u][a] = xsr[a][kt + u * W]; }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(x[u], w[u], sx[u], sw[u]);
+    }
+#pragma unroll 1
+    for (; kt < KB; kt += W) {
         v8i x[FM], w[FN];
         int sx[FM], sw[FN];
 #pragma unroll
-        for (int b = 0; b < FN; ++b) { w[b] = get(wr[b], kt); sw[b] = wsr[b][(long long)kt * p.ws_k]; }
+        for (int b = 0; b < FN; ++b) { w[b] = kt < KF ? whole(wr[b], kt) : rest(wr[b]); sw[b] = wsr[b][(long long)kt * p.ws_k]; }
 #pragma unroll
-        for (int a = 0; a < FM; ++a) { x[a] = get(xr[a], kt); sx[a] = xsr[a][kt]; }
-#pragma unroll
-        for (int a = 0; a < FM; ++a)
-#pragma unroll
-            for (int b = 0; b < FN; ++b)
-                acc[a][b] = EXACT ? mfma_exact<XF == 1>(w[b], x[a], acc[a][b], sw[b], sx[a]) : mfma_f8(w[b], x[a], acc[a][b], std::integral_constant<int, XF>{}, sw[b], sx[a]);
+        for (int a = 0; a < FM; ++a) { x[a] = kt < KF ? whole(xr[a], kt) : rest(xr[a]); sx[a] = xsr[a][kt]; }
+        add(x, w, sx, sw);
     }
 #pragma unroll
     for (int a = 0; a < FM; ++a)
@@ -238,85 +296,14 @@ __global__ __launch_bounds__(512) void f8mm_rows_kernel(const F8MmParams p)
         v4f s = part[0][a][b][lane];
 #pragma unroll
         for (int i = 1; i < W; ++i) s += part[i][a][b][lane];
-        store_y(p, a * 16 + r16, n0 + b * 16 + 4 * q, s);
+        store_y(p, m0 + a * 16 + r16, n0 + b * 16 + 4 * q, s);
     }
-}
-
-// ---- tiles whose operands become bf16 on their way into LDS: 64 elements along K a step
-template <int BM, int BN, int WR, int WC, int XF>
-__global__ __launch_bounds__(WR * WC * 64) void f8mm_exact_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
-{
-    constexpr int NT = WR * WC * 64, FM = BM / WR / 16, FN = BN / WC / 16, IX = BM * 4 / NT, IW = BN * 4 / NT, STAGE = (BM + BN) * 128;
-    static_assert(IX * NT == BM * 4 && IW * NT == BN * 4, "whole items");
-    extern __shared__ __align__(16) unsigned char lds[];
-    int tm, tn;
-    tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
-    const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, q = lane >> 4;
-    const int wm = wave / WC * (BM / WR), wn = wave % WC * (BN / WC);
-    // an item: sixteen codes of a row, four items a row and step
-    v4i cx[IX], cw[IW];
-    unsigned int sx[IX], sw[IW];
-    auto load = [&](int t) {
-        const int k = t * 64 + (tid & 3) * 16, left = p.K - k;          // (NT is a multiple of four: all items of a thread lie in the same columns)
-#pragma unroll
-        for (int i = 0; i < IX; ++i) {
-            const long long m = min(m0 + ((i * NT + tid) >> 2), p.M - 1);
-            cx[i] = v4i{0, 0, 0, 0};
-            if (left > 0) cx[i] = *reinterpret_cast<const v4i*>(p.x + m * p.ldx + k);
-            if (left < 16) cx[i] = keep_bytes(cx[i], left);
-            sx[i] = p.xs[m * p.ldxs + (t >> 1)];
-        }
-#pragma unroll
-        for (int i = 0; i < IW; ++i) {
-            const long long n = min(n0 + ((i * NT + tid) >> 2), p.N - 1);
-            cw[i] = v4i{0, 0, 0, 0};
-            if (left > 0) cw[i] = *reinterpret_cast<const v4i*>(p.w + n * p.ldw + k);
-            if (left < 16) cw[i] = keep_bytes(cw[i], left);
-            sw[i] = p.ws[(n >> 7) * p.ws_n + (t >> 1) * p.ws_k];
-        }
-    };
-    auto store = [&](unsigned char* to) {
-        const int c = (tid & 3) * 2;
-#pragma unroll
-        for (int i = 0; i < IX; ++i) {
-            const int r = (i * NT + tid) >> 2;
-            const float s = e8m0_value(sx[i]);
-            *reinterpret_cast<v4i*>(to + r * 128 + ((c ^ swz(r)) << 4)) = eight_bf16<XF == 1>(cx[i][0], cx[i][1], s);
-            *reinterpret_cast<v4i*>(to + r * 128 + (((c + 1) ^ swz(r)) << 4)) = eight_bf16<XF == 1>(cx[i][2], cx[i][3], s);
-        }
-        to += BM * 128;
-#pragma unroll
-        for (int i = 0; i < IW; ++i) {
-            const int r = (i * NT + tid) >> 2;
-            const float s = e8m0_value(sw[i]);
-            *reinterpret_cast<v4i*>(to + r * 128 + ((c ^ swz(r)) << 4)) = eight_bf16<false>(cw[i][0], cw[i][1], s);
-            *reinterpret_cast<v4i*>(to + r * 128 + (((c + 1) ^ swz(r)) << 4)) = eight_bf16<false>(cw[i][2], cw[i][3], s);
-        }
-    };
-    v4f acc[FM][FN];
-#pragma unroll
-    for (int a = 0; a < FM; ++a)
-#pragma unroll
-        for (int b = 0; b < FN; ++b) acc[a][b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const int steps = (p.K + 63) >> 6;
-    load(0);
-    for (int t = 0; t < steps; ++t) {
-        unsigned char* half = lds + (t & 1) * STAGE;
-        store(half);                                                    // (last read two steps ago, before the barrier of the step between)
-        __syncthreads();
-        if (t + 1 < steps) load(t + 1);
-        bf16_step<FM, FN>(half, half + BM * 128, wm + r16, wn + r16, q, acc);
-    }
-#pragma unroll
-    for (int a = 0; a < FM; ++a)
-#pragma unroll
-        for (int b = 0; b < FN; ++b) store_y(p, m0 + wm + a * 16 + r16, n0 + wn + b * 16 + 4 * q, acc[a][b]);
 }
 
 template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t tile_go(const F8MmParams& p, hipStream_t st)
 {
     const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128;
-    auto fn = EXACT ? &f8mm_exact_kernel<BM, BN, WR, WC, XF> : &f8mm_tile_kernel<BM, BN, WR, WC, XF>;
+    auto fn = &f8mm_tile_kernel<BM, BN, WR, WC, XF, EXACT>;
     if (bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
@@ -324,20 +311,20 @@ template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t 
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(WR * WC * 64), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int FM, int FN, int XF, bool EXACT> static hipError_t rows_go(const F8MmParams& p, hipStream_t st)
+template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t rows_go(const F8MmParams& p, hipStream_t st)
 {
-    hipLaunchKernelGGL((f8mm_rows_kernel<FM, FN, XF, EXACT>), dim3((unsigned)((p.N + FN * 16 - 1) / (FN * 16))), dim3(512), 0, st, p);
+    const int tm = (p.M + FM * 16 - 1) / (FM * 16), tn = (p.N + FN * 16 - 1) / (FN * 16);
+    hipLaunchKernelGGL((f8mm_rows_kernel<FM, FN, U, W, XF, EXACT>), dim3((unsigned)(tm * tn)), dim3(W * 64), 0, st, p, tm, tn, 8);
     return hipGetLastError();
 }
 template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int n_cu, hipStream_t st)
 {
     auto tiles = [&](int bm, int bn) { return (long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn); };
-    if (p.M <= 16) return rows_go<1, 1, XF, EXACT>(p, st);
-    if (p.M <= 32) return rows_go<2, 2, XF, EXACT>(p, st);
-    if (p.M <= 64) return rows_go<4, 2, XF, EXACT>(p, st);
-    if (tiles(256, 256) >= n_cu) return tile_go<256, 256, 2, 4, XF, EXACT>(p, st);
-    if (tiles(128, 128) >= n_cu) return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
-    return tile_go<64, 64, 2, 2, XF, EXACT>(p, st);
+    if (p.M <= 16) return rows_go<1, 1, 4, 16, XF, EXACT>(p, st);
+    if (p.M <= 32) return rows_go<2, 2, 2, 8, XF, EXACT>(p, st);
+    if (p.M <= 64 || tiles(64, 64) <= n_cu) return rows_go<4, 4, 1, 8, XF, EXACT>(p, st);
+    if (!EXACT && tiles(256, 256) >= n_cu) return tile_go<256, 256, 2, 4, XF, EXACT>(p, st);
+    return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
 }
 
 }  // namespace sopk

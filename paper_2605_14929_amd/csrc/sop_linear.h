@@ -65,6 +65,7 @@ namespace sopk {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
@@ -137,9 +138,20 @@ __device__ __forceinline__ v4i keep_bytes(v4i v, int n)
 // What this wavefront's direct loads into LDS still owe has arrived (each wavefront waits for its own before the barrier that
 // lets the others read it).
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ void load_to_lds(const unsigned char* from, unsigned char* to)   // 16 bytes a lane, `to` the wavefront's first
+// 16 bytes a lane from `bytes` bytes at p + at + uni (uni the same for all lanes) straight into LDS, lane by lane from `to` on (the same for
+// all lanes); what lies beyond the bytes arrives as zeros.
+struct Window { __amdgpu_buffer_rsrc_t r; };
+__device__ __forceinline__ Window window(const void* p, unsigned int bytes)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    return Window{__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000)};
+}
+__device__ __forceinline__ unsigned int load_word(const Window& w, unsigned int at, unsigned int uni)
+{
+    return (unsigned int)__builtin_amdgcn_raw_buffer_load_b32(w.r, (int)at, (int)uni, 0);
+}
+__device__ __forceinline__ void load_to_lds(const Window& w, unsigned int at, unsigned int uni, unsigned char* to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(w.r, (__attribute__((address_space(3))) void*)to, 16, (int)at, (int)uni, 0, 0);
 }
 
 // Workgroups that follow each other go to the eight XCDs in turn, each with an L2 of its own: XCD i gets the i-th part of the tiles,

@@ -221,10 +221,11 @@ extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, 
     if (M == 0) return SOP_OK;
     if (const char* why = plain_fault(x, w->K, ldx, 2)) return bad(c, call, SOP_EINVAL, why);
     if (!rows16(x, ldx, 2)) return bad(c, call, SOP_EINVAL, "x is on 16 bytes, its row stride a multiple of 8 elements");
+    if (w->K > kMaxStride / 2 || (ldx > kMaxStride / 2 && M > 1)) return bad(c, call, SOP_ESHAPE, "rows of x are at most 2^22 elements apart");
     if (const char* why = plain_fault(y, w->N, ldy, 2)) return bad(c, call, SOP_EINVAL, why);
     PackedMmParams p;
     std::memset(&p, 0, sizeof(p));
-    p.x = static_cast<const uint16_t*>(x); p.ldx = ldx; p.words = w->words_dev; p.payload = w->payload_dev;
+    p.x = static_cast<const uint16_t*>(x); p.ldx = M > 1 ? ldx : w->K; p.words = w->words_dev; p.payload = w->payload_dev;
     p.M = (int)M; p.N = (int)w->N; p.K = (int)w->K; p.g = g; p.n_bits = w->n_bits;
     p.mag_shift = sb ? m : (m > 0 ? m - 1 : 0);
     p.mag_mask = (1 << (xb + yb)) - 1; p.man_bits = yb; p.man_mask = (1 << yb) - 1;

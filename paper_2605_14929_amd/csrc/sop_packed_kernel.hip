@@ -135,18 +135,19 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
     const int wm = wave / WC * (BM / WR), wn = wave % WC * (BN / WC), lg = 31 - __builtin_clz(p.g);
     if (tid < 2 * SOP_K_PACKED_TAB) tab[tid] = p.tab[tid / SOP_K_PACKED_TAB][tid % SOP_K_PACKED_TAB];
     const unsigned char* xb = reinterpret_cast<const unsigned char*>(p.x + (long long)m0 * p.ldx);
-    long long ox[CX];
+    unsigned int ox[CX];                                                // (a row of x has at most 2^22 elements: the entry point's check)
 #pragma unroll
     for (int i = 0; i < CX; ++i) {
         const int c = i * NT + tid, r = c >> 3;
-        ox[i] = (long long)min(r, p.M - 1 - m0) * p.ldx * 2 + (((c & 7) ^ swz(r)) << 4);
+        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + (((c & 7) ^ swz(r)) << 4);
     }
+    const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)(p.ldx * 2) + (unsigned int)p.K * 2);
     auto load_x = [&](int t) {
         unsigned char* to = lds + (t & 1) * STAGE;
         const unsigned char* xk = xb + (long long)t * 128;
         if (t * 64 + 64 <= p.K) {
 #pragma unroll
-            for (int i = 0; i < CX; ++i) load_to_lds(xk + ox[i], to + (i * NT + (wave << 6)) * 16);
+            for (int i = 0; i < CX; ++i) load_to_lds(xw, ox[i], t * 128, to + (i * NT + (wave << 6)) * 16);
         } else {
             const int left = (p.K - t * 64) * 2;
 #pragma unroll
