@@ -62,7 +62,9 @@ struct PackedMmParams {
 
 #if defined(__HIPCC__)
 namespace sopk {
+typedef int v2i __attribute__((ext_vector_type(2)));
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -135,24 +137,35 @@ __device__ __forceinline__ v4i keep_bytes(v4i v, int n)
     }
     return v;
 }
-// What this wavefront's direct loads into LDS still owe has arrived (each wavefront waits for its own before the barrier that
-// lets the others read it).
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-// 16 bytes a lane from `bytes` bytes at p + at + uni (uni the same for all lanes) straight into LDS, lane by lane from `to` on (the same for
-// all lanes); what lies beyond the bytes arrives as zeros.
-struct Window { __amdgpu_buffer_rsrc_t r; };
+// `bytes` bytes from p on, for loads at byte offsets at + uni (uni the same for all lanes); what lies beyond arrives as zeros.
+struct Window { v4i r; };
 __device__ __forceinline__ Window window(const void* p, unsigned int bytes)
 {
-    return Window{__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000)};
+    const unsigned long long a = reinterpret_cast<unsigned long long>(p);
+    return Window{v4i{__builtin_amdgcn_readfirstlane((int)a), __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xFFFF), __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000}};
 }
 __device__ __forceinline__ unsigned int load_word(const Window& w, unsigned int at, unsigned int uni)
 {
-    return (unsigned int)__builtin_amdgcn_raw_buffer_load_b32(w.r, (int)at, (int)uni, 0);
+    const auto r = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)(unsigned int)w.r[0] | (unsigned long long)(unsigned int)w.r[1] << 32), 0, w.r[2], 0x00027000);
+    return (unsigned int)__builtin_amdgcn_raw_buffer_load_b32(r, (int)at, (int)uni, 0);
+}
+// ... 16 (or 4) bytes a lane straight into LDS, lane by lane from `to` on (the same for all lanes).  Written out so that the compiler does not
+// wait for them by itself before other reads of LDS: whoever reads what they bring waits for its own wavefront's loads (wait_loads),
+// then meets the others at a barrier.  (m0, which holds the place in LDS, is written right before each use by whoever uses it.)
+__device__ __forceinline__ unsigned int lds_address(const unsigned char* p)
+{
+    return (unsigned int)__builtin_amdgcn_readfirstlane((int)(unsigned int)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) unsigned char*)p));
 }
 __device__ __forceinline__ void load_to_lds(const Window& w, unsigned int at, unsigned int uni, unsigned char* to)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(w.r, (__attribute__((address_space(3))) void*)to, 16, (int)at, (int)uni, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds_address(to)), "v"(at), "s"(w.r), "s"(uni) : "memory");
 }
+__device__ __forceinline__ void load_word_to_lds(const Window& w, unsigned int at, unsigned int uni, unsigned char* to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds_address(to)), "v"(at), "s"(w.r), "s"(uni) : "memory");
+}
+// all but the N loads asked for last have arrived (N = 0: all)
+template <int N = 0> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // Workgroups that follow each other go to the eight XCDs in turn, each with an L2 of its own: XCD i gets the i-th part of the tiles,
 // and walks it in groups of `group` tile rows, so that the tiles in flight on it share their operands' panels.

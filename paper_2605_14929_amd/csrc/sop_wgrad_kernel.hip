@@ -5,8 +5,10 @@
 // operand and 32 elements of the sum) cannot take it.  An 8-bit number times a power of two is a bf16 number, though: the
 // checkpoint becomes bf16 exactly on its way into LDS, and the bf16 matrix instruction adds nothing but binary32 sums.
 //
-// Both operands arrive with the summed index outermost, the matrix instruction wants it innermost: a thread loads eight rows of two
-// (dy) or four (x) columns, turns them in registers by byte permutations, and writes eight sums' worth of a column as one chunk.
+// Both operands arrive with the summed index outermost, the matrix instruction wants it innermost.  Where dy's rows lie on 16 bytes,
+// both go to LDS as they are, straight from memory, and are turned by LDS's transposing reads (a sixteen-lane group reads four rows of
+// sixteen 16-bit, or eight rows of sixteen 8-bit elements and receives the columns); the checkpoint stays in 8 bits until then.
+// Otherwise a thread loads eight rows of two (dy) or four (x) columns, turns them in registers, and writes columns.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -17,6 +19,35 @@ namespace sopk {
 
 // two neighbouring bf16 of a row, aligned or not
 struct __attribute__((packed)) Pair { unsigned int v; };
+
+// four neighbouring columns of a row of dw
+__device__ __forceinline__ void store_dw(const WgradParams& p, int n, int k, v4f v)
+{
+    if (n >= p.N || k >= p.K) return;
+    const long long at = (long long)n * p.lddw + k;
+    const bool four = k + 3 < p.K;
+    if (p.out_bf16) {
+        uint16_t* w = reinterpret_cast<uint16_t*>(p.dw) + at;
+        if (p.accumulate) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (k + i < p.K) v[i] += __uint_as_float((unsigned int)w[i] << 16);
+        }
+        if (four && (reinterpret_cast<uintptr_t>(w) & 7) == 0) *reinterpret_cast<uint2*>(w) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (k + i < p.K) w[i] = (uint16_t)bf16_bits(v[i]);
+        }
+    } else {
+        float* w = reinterpret_cast<float*>(p.dw) + at;
+        if (four && (reinterpret_cast<uintptr_t>(w) & 15) == 0) {
+            if (p.accumulate) v += *reinterpret_cast<const v4f*>(w);
+            *reinterpret_cast<v4f*>(w) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (k + i < p.K) w[i] = p.accumulate ? v[i] + w[i] : v[i];
+        }
+    }
+}
 
 template <int BN, int BK, int WR, int WC, bool X5>
 __global__ __launch_bounds__(WR * WC * 64) void wgrad_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
@@ -130,42 +161,163 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_kernel(const WgradParams p
         bf16_step<FA, FB>(half, half + BN * 128, wn + r16, wk + r16, q, acc);
     }
 #pragma unroll
-    for (int a = 0; a < FA; ++a) {
-        const int n = n0 + wn + a * 16 + r16;
-        if (n >= p.N) continue;
+    for (int a = 0; a < FA; ++a)
 #pragma unroll
-        for (int b = 0; b < FB; ++b) {
-            const int k = k0 + wk + b * 16 + 4 * q;
-            if (k >= p.K) continue;
-            const long long at = (long long)n * p.lddw + k;
-            const bool four = k + 3 < p.K;
-            if (p.out_bf16) {
-                uint16_t* w = reinterpret_cast<uint16_t*>(p.dw) + at;
-                v4f v = acc[a][b];
-                if (p.accumulate) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) if (k + i < p.K) v[i] += __uint_as_float((unsigned int)w[i] << 16);
-                }
-                if (four && (reinterpret_cast<uintptr_t>(w) & 7) == 0) *reinterpret_cast<uint2*>(w) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-                else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) if (k + i < p.K) w[i] = (uint16_t)bf16_bits(v[i]);
-                }
-            } else {
-                float* w = reinterpret_cast<float*>(p.dw) + at;
-                v4f v = acc[a][b];
-                if (four && (reinterpret_cast<uintptr_t>(w) & 15) == 0) {
-                    if (p.accumulate) v += *reinterpret_cast<const v4f*>(w);
-                    *reinterpret_cast<v4f*>(w) = v;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) if (k + i < p.K) w[i] = p.accumulate ? v[i] + w[i] : v[i];
-                }
-            }
-        }
-    }
+        for (int b = 0; b < FB; ++b) store_dw(p, n0 + wn + a * 16 + r16, k0 + wk + b * 16 + 4 * q, acc[a][b]);
 }
 
+// two codes of a column (the low or the high half of a word) under the scales of their rows, as bf16
+template <bool E5M2, bool HIGH> __device__ __forceinline__ int two_rows(int c, float s0, float s1)
+{
+    const v2bf a = E5M2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, s0, HIGH) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s0, HIGH);
+    const v2bf b = E5M2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(c, s1, HIGH) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s1, HIGH);
+    return (int)__builtin_amdgcn_perm(__builtin_bit_cast(unsigned int, b), __builtin_bit_cast(unsigned int, a), 0x07060100u);
+}
+
+// ---- rows of dy on 16 bytes.  64 rows a step, three steps in LDS: one being multiplied, one on its way or there, one being asked for.
+// In LDS a row is chunks of 16 bytes; chunk c of row m stands at position c ^ 2 (m & 3) (dy) or c ^ (m & 7) (x), so that the rows a
+// sixteen-lane group reads together fall on different banks.
+template <int BN, int BK, int WR, int WC, bool X5>
+__global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
+{
+    constexpr int NT = WR * WC * 64, FA = BN / WR / 32, FB = BK / WC / 32, NKB = BK / 128;
+    constexpr int CD = BN / 8, CX = BK / 16, LD = 64 * CD / NT, LX = 64 * CX / NT, XAT = 64 * BN * 2, SAT = XAT + 64 * BK, STAGE = SAT + NKB * 256;
+    static_assert(LD * NT == 64 * CD && LX * NT == 64 * CX && LD == 4 && LX == 2 && NT / CD % 4 == 0 && NT / CX % 8 == 0 && BK / WC <= 128, "shares of a step");
+    extern __shared__ __align__(16) unsigned char lds[];
+    int tn, tk;
+    tile_of(blockIdx.x, tiles_n * tiles_k, tiles_n, tiles_k, group, tn, tk);
+    const int n0 = tn * BN, k0 = tk * BK, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wn = wave / WC * (BN / WR), wk = wave % WC * (BK / WC), i16 = lane & 15, g16 = lane >> 4 & 1, h = lane >> 5;
+    const int steps = (p.M + 63) >> 6;
+
+    // where this thread's chunks come from, within 64 rows; chunks beyond the last column read the last one, and their sums go nowhere.
+    // (An aligned chunk with one element inside the matrix lies on its page.)
+    unsigned int od[LD], ox[LX];
+    {
+        const int m = tid / CD, n = min(n0 + ((tid % CD) ^ ((m & 3) << 1)) * 8, (p.N - 1) & ~7);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) od[i] = ((unsigned int)(m + i * (NT / CD)) * (unsigned int)p.lddy + (unsigned int)n) * 2u;
+    }
+    {
+        const int m = tid / CX, k = min(k0 + ((tid % CX) ^ (m & 7)) * 16, (p.K - 1) & ~15);
+#pragma unroll
+        for (int i = 0; i < LX; ++i) ox[i] = (unsigned int)(m + i * (NT / CX)) * (unsigned int)p.ldx + (unsigned int)k;
+    }
+    const unsigned int wide_n = (unsigned int)((p.N + 7) & ~7) * 2u, wide_k = (unsigned int)((p.K + 15) & ~15);
+    auto load = [&](int t, unsigned char* to) {                         // rows beyond the last arrive as zeros
+        const long long m0 = (long long)t * 64;
+        const unsigned int last = (unsigned int)min(64, p.M - (int)m0) - 1;
+        const Window d = window(p.dy + m0 * p.lddy, last * (unsigned int)p.lddy * 2u + wide_n);
+        const Window x = window(p.x + m0 * p.ldx, last * (unsigned int)p.ldx + wide_k);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) load_to_lds(d, od[i], 0, to + (i * NT + wave * 64) * 16);
+#pragma unroll
+        for (int i = 0; i < LX; ++i) load_to_lds(x, ox[i], 0, to + XAT + (i * NT + wave * 64) * 16);
+    };
+    // Scales: the words that hold this tile's bytes come into LDS a step ahead of the step's operands (the first wavefront asks for
+    // them), and become numbers there while the step before is multiplied.
+    unsigned char* const words = lds + 3 * STAGE;
+    auto load_scales = [&](int t) {
+        const long long m0 = (long long)t * 64;
+        const unsigned int last = (unsigned int)min(64, p.M - (int)m0) - 1;
+        load_word_to_lds(window(p.xs + m0 * p.ldxs, last * (unsigned int)p.ldxs + (unsigned int)p.ldxs), min((unsigned int)lane, last) * (unsigned int)p.ldxs + (unsigned int)(k0 >> 7 & ~3), 0,
+                         words + t % 3 * 256);
+    };
+    auto put_scales = [&](int t, unsigned char* to) {
+        if (tid < 64 * NKB) {
+            const unsigned int w = *reinterpret_cast<const unsigned int*>(words + t % 3 * 256 + (tid & 63) * 4);
+            *reinterpret_cast<float*>(to + SAT + tid * 4) = e8m0_value(w >> (8 * (((k0 >> 7) + (tid >> 6)) & 3)) & 255u);
+        }
+    };
+
+    // what this lane reads, relative to a step's place: squares of 32 columns, every second one of dy and x at its own place
+    unsigned int ad[2], ax[2];
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+        const int c = (wn >> 3) + 4 * o + 2 * g16 + (i16 >> 1 & 1), m = 8 * h + (i16 >> 2);
+        ad[o] = (unsigned int)(m * (BN * 2) + ((c ^ ((m & 3) << 1)) << 4) + (i16 & 1) * 8);
+        const int cx = (wk >> 4) + 2 * o + g16, mx = 8 * h + (i16 >> 1);
+        ax[o] = (unsigned int)(XAT + mx * BK + ((cx ^ (mx & 7)) << 4) + (i16 & 1) * 8);
+    }
+    const unsigned int as = (unsigned int)(SAT + (wk >> 7) * 256 + h * 32);
+
+    v16f acc[FA][FB];
+#pragma unroll
+    for (int a = 0; a < FA; ++a)
+#pragma unroll
+        for (int b = 0; b < FB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+    typedef __attribute__((address_space(3))) v4s* lds16;
+    typedef __attribute__((address_space(3))) v2i* lds8;
+
+    auto compute = [&](const unsigned char* at) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {                                   // sixteen rows
+            const v4f s0 = *reinterpret_cast<const v4f*>(at + as + s * 64), s1 = *reinterpret_cast<const v4f*>(at + as + s * 64 + 16);
+            const float sc[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+            v8bf x[FB];
+#pragma unroll
+            for (int b = 0; b < FB; ++b) {
+                const v2i c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8)(at + ax[b & 1] + s * (16 * BK) + (b >> 1) * 64));
+                v4i r;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {                           // rows 4i .. 4i + 3
+                    r[2 * i] = two_rows<X5, false>(c[i], sc[4 * i], sc[4 * i + 1]);
+                    r[2 * i + 1] = two_rows<X5, true>(c[i], sc[4 * i + 2], sc[4 * i + 3]);
+                }
+                x[b] = __builtin_bit_cast(v8bf, r);
+            }
+#pragma unroll
+            for (int a = 0; a < FA; ++a) {
+                const v4s d0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(at + ad[a & 1] + s * (32 * BN) + (a >> 1) * 128));
+                const v4s d1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(at + ad[a & 1] + s * (32 * BN) + 8 * BN + (a >> 1) * 128));
+                const v8bf d = __builtin_bit_cast(v8bf, __builtin_shufflevector(d0, d1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int b = 0; b < FB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[b], d, acc[a][b], 0, 0, 0);
+            }
+        }
+    };
+
+    unsigned char *now = lds, *next = lds + STAGE, *after = lds + 2 * STAGE;
+    load(0, now);
+    if (wave == 0) { load_scales(0); if (steps > 1) load_scales(1); }
+    wait_loads();
+    if (steps > 1) load(1, next);
+    if (wave == 0 && steps > 2) load_scales(2);
+    __syncthreads();
+    put_scales(0, now);
+    for (int t = 0; t < steps; ++t) {
+        // what was asked for a step ago, and nothing older, may still be on its way: LD + LX loads, the first wavefront's scales
+        if (t + 2 < steps && wave == 0) wait_loads<LD + LX + 1>(); else if (t + 1 < steps) wait_loads<LD + LX>(); else wait_loads();
+        __syncthreads();
+        if (t + 1 < steps) put_scales(t + 1, next);
+        if (t + 2 < steps) load(t + 2, after);
+        if (t + 3 < steps && wave == 0) load_scales(t + 3);
+        compute(now);
+        unsigned char* u = now;
+        now = next; next = after; after = u;
+    }
+#pragma unroll
+    for (int a = 0; a < FA; ++a)
+#pragma unroll
+        for (int b = 0; b < FB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_dw(p, n0 + wn + a * 32 + (lane & 31), k0 + wk + b * 32 + 8 * i + 4 * h,
+                         v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+}
+
+template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_turn_go(const WgradParams& p, hipStream_t st)
+{
+    const int tn = (p.N + BN - 1) / BN, tk = (p.K + BK - 1) / BK, bytes = 3 * (64 * BN * 2 + 64 * BK + BK / 128 * 256) + 3 * 256;
+    if (bytes > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&wgrad_turn_kernel<BN, BK, WR, WC, X5>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((wgrad_turn_kernel<BN, BK, WR, WC, X5>), dim3((unsigned)(tn * tk)), dim3(WR * WC * 64), bytes, st, p, tn, tk, 8);
+    return hipGetLastError();
+}
 template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_go(const WgradParams& p, hipStream_t st)
 {
     const int tn = (p.N + BN - 1) / BN, tk = (p.K + BK - 1) / BK, bytes = 2 * (BN + BK) * 128;
@@ -179,6 +331,8 @@ template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_go(co
 template <bool X5> static hipError_t wgrad_pick(const WgradParams& p, int n_cu, hipStream_t st)
 {
     auto tiles = [&](int a, int b) { return (long long)((p.N + a - 1) / a) * ((p.K + b - 1) / b); };
+    const bool on16 = (reinterpret_cast<uintptr_t>(p.dy) & 15) == 0 && (p.lddy & 7) == 0 && p.lddy <= 1 << 22;
+    if (p.M > 0 && on16) return tiles(256, 256) >= n_cu ? wgrad_turn_go<256, 256, 2, 4, X5>(p, st) : wgrad_turn_go<128, 128, 2, 2, X5>(p, st);
     if (tiles(256, 256) >= n_cu) return wgrad_go<256, 256, 2, 4, X5>(p, st);
     if (tiles(128, 128) >= n_cu) return wgrad_go<128, 128, 2, 2, X5>(p, st);
     return wgrad_go<64, 128, 2, 2, X5>(p, st);
