@@ -55,7 +55,7 @@ struct PackedMmParams {
     const uint16_t* words; const unsigned char* payload;
     int M, N, K, g, n_bits;
     int mag_shift, mag_mask, man_bits, man_mask, exp_off;   // scale = (mantissa with its leading one) * 2^(max(e, 1) + exp_off)
-    int sign_pos, sel_pos;                   // -1: absent
+    int sign_up, sel_pos, sel_mask;          // word << sign_up has the sign in bit 31 (0: none); selector = word >> sel_pos & sel_mask
     uint16_t* y; long long ldy;              // bf16
     float tab[2][SOP_K_PACKED_TAB];
 };
@@ -125,6 +125,26 @@ __device__ __forceinline__ void bf16_step(const unsigned char* ta, const unsigne
 #pragma unroll
             for (int b = 0; b < FB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[b], fa, acc[a][b], 0, 0, 0);
         }
+    }
+}
+// The same by 32 x 32 squares, tiles whose chunk c of row r stands at position c ^ (r & 7): `row` = byte offset of this lane's row (lane & 31) of
+// the wavefront's first square, h = lane >> 5.  acc[a][b][i] holds row 8 (i / 4) + 4 h + i % 4 of b's square, column lane & 31 of a's.
+__device__ __forceinline__ v8bf square_frag(const unsigned char* tile, unsigned int row, unsigned int z, int f, int s)
+{
+    return *reinterpret_cast<const v8bf*>(tile + (row + (((unsigned int)(2 * s) << 4) ^ z)) + f * 4096);
+}
+template <int FA, int FB>
+__device__ __forceinline__ void bf16_squares(const unsigned char* ta, const unsigned char* tb, unsigned int ra, unsigned int rb, int lane, int s, v16f (&acc)[FA][FB])
+{
+    const unsigned int z = (unsigned int)((lane >> 5) ^ (lane & 7)) << 4;   // chunk 2 s + h of a row that is lane & 7 modulo 8
+    v8bf fb[FB];
+#pragma unroll
+    for (int b = 0; b < FB; ++b) fb[b] = square_frag(tb, rb, z, b, s);
+#pragma unroll
+    for (int a = 0; a < FA; ++a) {
+        const v8bf fa = square_frag(ta, ra, z, a, s);
+#pragma unroll
+        for (int b = 0; b < FB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[b], fa, acc[a][b], 0, 0, 0);
     }
 }
 // zeroes the bytes of a 16-byte chunk beyond the first `n`

@@ -230,8 +230,9 @@ extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, 
     p.mag_shift = sb ? m : (m > 0 ? m - 1 : 0);
     p.mag_mask = (1 << (xb + yb)) - 1; p.man_bits = yb; p.man_mask = (1 << yb) - 1;
     p.exp_off = -bias - yb - w->layer_shift_k;
-    p.sign_pos = sb ? b - 1 : -1;
-    p.sel_pos = !w->table_b ? -1 : (sb ? m - 1 : b - 1);
+    p.sign_up = sb ? 32 - b : 0;                                        // (16-bit words: bit 31 stays empty where there is no sign)
+    p.sel_mask = w->table_b ? 1 : 0;
+    p.sel_pos = !w->table_b ? 0 : (sb ? m - 1 : b - 1);
     p.y = static_cast<uint16_t*>(y); p.ldy = ldy;
     for (int i = 0; i < SOP_K_PACKED_TAB; ++i) {
         p.tab[0][i] = w->table_a[i < w->entries_a ? i : w->entries_a - 1];
