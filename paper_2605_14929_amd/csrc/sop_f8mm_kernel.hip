@@ -47,8 +47,8 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
 }
 
 // ---- tiles: BM x BN of y by WR x WC wavefronts, 128 elements along K a step, two steps in LDS.  A wavefront's part is made of 32 x 32
-// squares.  In LDS a row is eight chunks of 16 bytes, chunk c at position c ^ (row & 7): rows eight apart lie alike, so that all
-// squares are read at constant distances, and eight neighbouring rows fall on different banks.
+// squares.  In LDS a row is eight chunks of 16 bytes, chunk c at position c ^ (row / 2 & 7): LDS serves a 16-byte read sixteen lanes at
+// a time (0-3, 12-15, 20-23 and 24-27, then the others of the first 32, ...), whose rows so fall on different banks.
 template <int BM, int BN, int WR, int WC, int XF, bool EXACT>
 __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
@@ -68,12 +68,12 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
 #pragma unroll
     for (int i = 0; i < CX; ++i) {
         const int c = i * NT + tid, r = c >> 3;
-        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + (((c ^ r) & 7) << 4);
+        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + (((c ^ r >> 1) & 7) << 4);
     }
 #pragma unroll
     for (int i = 0; i < CW; ++i) {
         const int c = i * NT + tid, r = c >> 3;
-        ow[i] = (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw + (((c ^ r) & 7) << 4);
+        ow[i] = (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw + (((c ^ r >> 1) & 7) << 4);
     }
     const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
     const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
 
     // this lane's 64 bytes of a row: chunks 2h, 2h + 1 (the first 64 elements' share) and 4 + 2h, 5 + 2h
-    const unsigned int sz = (unsigned int)(r32 & 7), row_x = (unsigned int)(wm + r32) * 128, row_w = (unsigned int)(BM + wn + r32) * 128;
+    const unsigned int sz = (unsigned int)(r32 >> 1 & 7), row_x = (unsigned int)(wm + r32) * 128, row_w = (unsigned int)(BM + wn + r32) * 128;
     const unsigned int c0 = ((unsigned int)(2 * h) ^ sz) << 4;
     auto frag = [&](const unsigned char* half, unsigned int row, int f, int j) {
         const unsigned int c = c0 ^ (j << 6);
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
 #pragma unroll 1
         for (int c = tid; c < (BM + BN) * 8; c += NT) {
             const bool of_x = c < BM * 8;
-            const int d = of_x ? c : c - BM * 8, r = d >> 3, col = ((d ^ r) & 7) << 4, n = left - col;
+            const int d = of_x ? c : c - BM * 8, r = d >> 3, col = ((d ^ r >> 1) & 7) << 4, n = left - col;
             const unsigned char* row = of_x ? xb + (long long)min(r, p.M - 1 - m0) * p.ldx : wb + (long long)min(r, p.N - 1 - n0) * p.ldw;
             v4i v = {0, 0, 0, 0};
             if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + col), n);
@@ -194,6 +194,161 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
     for (int a = 0; a < FM; ++a)
 #pragma unroll
         for (int b = 0; b < FN; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * h, v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+}
+
+// ---- large products: 256 x 256 of y by four wavefronts, one on a SIMD, each 128 x 128 of it; 128 elements along K a step, two steps in LDS.
+// What an instruction takes from LDS is what bounds such a tile: eight wavefronts of 128 x 64 read 192 KB a step, these read 128 KB.
+// A wavefront alone on its SIMD overlaps its own work: while a half step (64 elements) is multiplied, the operands of the next half
+// step are read into a second set of registers, one read behind every matrix instruction.  Halfway through a step comes its barrier:
+// the next step has arrived, this one's place in LDS is free for the step after the next.  In LDS a row is eight chunks of 16 bytes,
+// chunk c at position c ^ (row / 2 & 7), as above.
+template <int XF>
+__global__ __launch_bounds__(256) void f8mm_large_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
+{
+    constexpr int BM = 256, BN = 256, F = 4, STAGE = (BM + BN) * 128;
+    extern __shared__ __align__(16) unsigned char lds[];
+    int tm, tn;
+    tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
+    const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1 << 7, wn = (wave & 1) << 7, r32 = lane & 31, h = lane >> 5;
+    const unsigned char* xb = p.x + (long long)m0 * p.ldx;
+    const unsigned char* wb = p.w + (long long)n0 * p.ldw;
+    const int KF = p.K >> 7, KB = (p.K + 127) >> 7;                     // whole steps, all steps
+    unsigned int ox[8], ow[8];                                          // byte offsets of this thread's chunks; rows beyond the matrix read its last
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int c = i * 256 + tid, r = c >> 3, col = ((c ^ r >> 1) & 7) << 4;
+        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + col;
+        ow[i] = (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw + col;
+    }
+    const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
+    const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
+    auto load = [&](const Window& x, const Window& w, int kt, int i) {  // the i-th of eight parts
+        unsigned char* to = lds + (kt & 1) * STAGE + (wave << 10) + i * 4096;
+        load_to_lds(x, ox[i], kt * 128, to);
+        load_to_lds(w, ow[i], kt * 128, to + BM * 128);
+    };
+
+    // scales: four steps of a row of x in a word, four of w likewise; the next four are asked for while these are used
+    const Window xsw = window(p.xs + (long long)m0 * p.ldxs, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldxs + (unsigned int)((KB + 3) & ~3));
+    const unsigned char* wsb = p.ws + (long long)min((n0 + wn) >> 7, (p.N - 1) >> 7) * p.ws_n;
+    unsigned int sxo[F], sx[F], nx[F], sw = 0, nw[4];
+#pragma unroll
+    for (int f = 0; f < F; ++f) sxo[f] = (unsigned int)min(wm + f * 32 + r32, p.M - 1 - m0) * (unsigned int)p.ldxs;
+    auto scales = [&](int kt) {
+#pragma unroll
+        for (int f = 0; f < F; ++f) nx[f] = load_word(xsw, sxo[f], kt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) nw[j] = wsb[(long long)min(kt + j, KB - 1) * p.ws_k];
+    };
+    auto turn = [&](int kt) {                                           // before step kt: its scales into place
+        if ((kt & 3) == 0) {
+#pragma unroll
+            for (int f = 0; f < F; ++f) sx[f] = nx[f];
+            sw = nw[0] | nw[1] << 8 | nw[2] << 16 | nw[3] << 24;
+            if (kt + 4 < KB) scales(kt + 4);
+        } else {
+#pragma unroll
+            for (int f = 0; f < F; ++f) sx[f] >>= 8;
+            sw >>= 8;
+        }
+    };
+
+    v16f acc[F][F];
+#pragma unroll
+    for (int a = 0; a < F; ++a)
+#pragma unroll
+        for (int b = 0; b < F; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+
+    const unsigned int z = (unsigned int)((2 * h) ^ (r32 >> 1 & 7)) << 4;   // chunks 2h and 2h + 1 of the first half step, 4 + 2h and 5 + 2h of the second
+    const unsigned int lx = (unsigned int)(wm + r32) * 128, lw = (unsigned int)(BM + wn + r32) * 128;
+    struct Operands { v4i x[F][2], w[F][2]; };
+    auto read = [&](Operands& o, int kt, int j, int i) {                // the i-th of sixteen reads of half step j
+        const unsigned char* at = lds + (kt & 1) * STAGE + (i & 7) / 2 * 4096;
+        const unsigned int c = z ^ (unsigned int)(j << 6) ^ (unsigned int)((i & 1) << 4);
+        (i < 8 ? o.w : o.x)[(i & 7) / 2][i & 1] = *reinterpret_cast<const v4i*>(at + ((i < 8 ? lw : lx) + c));
+    };
+    auto multiply = [&](const Operands& o, int i) {                     // the i-th of sixteen squares
+        const int a = i >> 2, b = i & 3;
+        acc[a][b] = mfma_f8<XF>(__builtin_shufflevector(o.w[b][0], o.w[b][1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(o.x[a][0], o.x[a][1], 0, 1, 2, 3, 4, 5, 6, 7), acc[a][b], (int)sw, (int)sx[a]);
+    };
+    auto meet = [&]() {                                                 // this wavefront's reads of LDS have ended, what it asked for has arrived
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    Operands first, second;
+    scales(0);
+    if (KF) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) load(xw, ww, 0, i);
+        meet();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) read(first, 0, 0, i);
+        if (KF > 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load(xw, ww, 1, i);
+    }
+    // (One stretch of code for all steps: where there is no further step, empty windows are read, which bring zeros to a place that
+    // nobody reads any more, and operands that nobody uses.)  The
+    // loads of a step are spread over a whole step, one pair behind every fourth or second instruction: a wavefront that issues them
+    // faster than they are taken holds up its own matrix instructions.
+    for (int kt = 0; kt < KF; ++kt) {
+        turn(kt);
+        Window x1 = xw, w1 = ww;
+        x1.r[2] = kt + 1 < KF ? xw.r[2] : 0;
+        w1.r[2] = kt + 1 < KF ? ww.r[2] : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            read(second, kt, 1, i);
+            if (i < 8 && (i & 1)) load(x1, w1, kt + 1, 4 + (i >> 1));
+            multiply(first, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        meet();
+        x1.r[2] = kt + 2 < KF ? xw.r[2] : 0;
+        w1.r[2] = kt + 2 < KF ? ww.r[2] : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if ((i & 3) == 3) load(x1, w1, kt + 2, i >> 2);
+            read(first, kt + 1, 0, i);
+            multiply(second, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    meet();
+    if (KF < KB) {                                                      // the last step of an odd K: elements beyond it count as zeros
+        unsigned char* to = lds + (KF & 1) * STAGE;
+        const int left = p.K & 127;
+#pragma unroll 1
+        for (int c = tid; c < (BM + BN) * 8; c += 256) {
+            const bool of_x = c < BM * 8;
+            const int d = of_x ? c : c - BM * 8, r = d >> 3, col = ((d ^ r >> 1) & 7) << 4, n = left - col;
+            const unsigned char* row = of_x ? xb + (long long)min(r, p.M - 1 - m0) * p.ldx : wb + (long long)min(r, p.N - 1 - n0) * p.ldw;
+            v4i v = {0, 0, 0, 0};
+            if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + col), n);
+            *reinterpret_cast<v4i*>(to + c * 16) = v;
+        }
+        __syncthreads();
+        turn(KF);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) read(first, KF, j, i);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) multiply(first, i);
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < F; ++a)
+#pragma unroll
+        for (int b = 0; b < F; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * h, v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
@@ -311,6 +466,14 @@ template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t 
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(WR * WC * 64), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
+template <int XF> static hipError_t large_go(const F8MmParams& p, hipStream_t st)
+{
+    const int tm = (p.M + 255) / 256, tn = (p.N + 255) / 256, bytes = 2 * 512 * 128;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&f8mm_large_kernel<XF>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(f8mm_large_kernel<XF>, dim3((unsigned)(tm * tn)), dim3(256), bytes, st, p, tm, tn, 8);
+    return hipGetLastError();
+}
 template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t rows_go(const F8MmParams& p, hipStream_t st)
 {
     const int tm = (p.M + FM * 16 - 1) / (FM * 16), tn = (p.N + FN * 16 - 1) / (FN * 16);
@@ -323,7 +486,7 @@ template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int n_cu
     if (p.M <= 16) return rows_go<1, 1, 4, 16, XF, EXACT>(p, st);
     if (p.M <= 32) return rows_go<2, 2, 2, 8, XF, EXACT>(p, st);
     if (p.M <= 64 || tiles(64, 64) <= n_cu) return rows_go<4, 4, 1, 8, XF, EXACT>(p, st);
-    if (!EXACT && tiles(256, 256) >= n_cu) return tile_go<256, 256, 2, 4, XF, EXACT>(p, st);
+    if (!EXACT && tiles(256, 256) >= n_cu) return large_go<XF>(p, st);
     return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
 }
 

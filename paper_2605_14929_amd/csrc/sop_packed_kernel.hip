@@ -200,7 +200,7 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
 #pragma unroll
     for (int i = 0; i < CX; ++i) {
         const int c = i * NT + tid, r = c >> 3;
-        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + (((c ^ r) & 7) << 4);
+        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + (((c ^ r >> 1) & 7) << 4);
     }
     const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)(p.ldx * 2) + (unsigned int)p.K * 2);
     auto load_x = [&](int t) {
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
             const int left = (p.K - t * 64) * 2;
 #pragma unroll 1
             for (int c = tid; c < BM * 8; c += NT) {
-                const int r = c >> 3, col = ((c ^ r) & 7) << 4;
+                const int r = c >> 3, col = ((c ^ r >> 1) & 7) << 4;
                 v4i v = {0, 0, 0, 0};
                 if (col < left) v = *reinterpret_cast<const v4i*>(xb + (long long)min(r, p.M - 1 - m0) * p.ldx + t * 64 + (col >> 1));
                 *reinterpret_cast<v4i*>(to + c * 16) = v;
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
     auto store_w = [&](int t, const Share& z, int i, int h) {           // eight weights: item i, half h
         const int r = (i * NT + tid) >> 2;
         const v4i u = eight_weights<NB>(z.c[i][h], tab, word_table<NB>(p, z.w[i][h]), word_scale(p, z.w[i][h]));
-        *reinterpret_cast<v4i*>(lds + (t & 1) * STAGE + BM * 128 + r * 128 + ((((tid & 3) * 2 + h) ^ (r & 7)) << 4)) = only_if(t * 64 + k16 + 8 * h < p.K, u);
+        *reinterpret_cast<v4i*>(lds + (t & 1) * STAGE + BM * 128 + r * 128 + ((((tid & 3) * 2 + h) ^ (r >> 1 & 7)) << 4)) = only_if(t * 64 + k16 + 8 * h < p.K, u);
     };
     v16f acc[FM][FN];
 #pragma unroll

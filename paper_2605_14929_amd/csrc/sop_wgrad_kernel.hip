@@ -175,8 +175,8 @@ template <bool E5M2, bool HIGH> __device__ __forceinline__ int two_rows(int c, f
 }
 
 // ---- rows of dy on 16 bytes.  64 rows a step, three steps in LDS: one being multiplied, one on its way or there, one being asked for.
-// In LDS a row is chunks of 16 bytes; chunk c of row m stands at position c ^ 2 (m & 3) (dy) or c ^ (m & 7) (x), so that the rows a
-// sixteen-lane group reads together fall on different banks.
+// In LDS a row is chunks of 16 bytes; chunk c of row m stands at position c ^ 4 (m & 3) (dy), c ^ 2 (m & 7) (x, rows of 256 bytes) or
+// c ^ 2 (m / 2 & 3) (x, rows of 128), so that the rows that 32 lanes read together fall on different banks.
 template <int BN, int BK, int WR, int WC, bool X5>
 __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
 {
@@ -190,16 +190,17 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
     const int wn = wave / WC * (BN / WR), wk = wave % WC * (BK / WC), i16 = lane & 15, g16 = lane >> 4 & 1, h = lane >> 5;
     const int steps = (p.M + 63) >> 6;
 
+    auto turn_x = [](int m) { return BK == 256 ? (m & 7) << 1 : (m >> 1 & 3) << 1; };
     // where this thread's chunks come from, within 64 rows; chunks beyond the last column read the last one, and their sums go nowhere.
     // (An aligned chunk with one element inside the matrix lies on its page.)
     unsigned int od[LD], ox[LX];
     {
-        const int m = tid / CD, n = min(n0 + ((tid % CD) ^ ((m & 3) << 1)) * 8, (p.N - 1) & ~7);
+        const int m = tid / CD, n = min(n0 + ((tid % CD) ^ ((m & 3) << 2)) * 8, (p.N - 1) & ~7);
 #pragma unroll
         for (int i = 0; i < LD; ++i) od[i] = ((unsigned int)(m + i * (NT / CD)) * (unsigned int)p.lddy + (unsigned int)n) * 2u;
     }
     {
-        const int m = tid / CX, k = min(k0 + ((tid % CX) ^ (m & 7)) * 16, (p.K - 1) & ~15);
+        const int m = tid / CX, k = min(k0 + ((tid % CX) ^ turn_x(m)) * 16, (p.K - 1) & ~15);
 #pragma unroll
         for (int i = 0; i < LX; ++i) ox[i] = (unsigned int)(m + i * (NT / CX)) * (unsigned int)p.ldx + (unsigned int)k;
     }
@@ -230,14 +231,17 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
         }
     };
 
-    // what this lane reads, relative to a step's place: squares of 32 columns, every second one of dy and x at its own place
-    unsigned int ad[2], ax[2];
+    // what this lane reads of each square of 32 columns, relative to a step's place
+    unsigned int ad[FA], ax[FB];
 #pragma unroll
-    for (int o = 0; o < 2; ++o) {
-        const int c = (wn >> 3) + 4 * o + 2 * g16 + (i16 >> 1 & 1), m = 8 * h + (i16 >> 2);
-        ad[o] = (unsigned int)(m * (BN * 2) + ((c ^ ((m & 3) << 1)) << 4) + (i16 & 1) * 8);
-        const int cx = (wk >> 4) + 2 * o + g16, mx = 8 * h + (i16 >> 1);
-        ax[o] = (unsigned int)(XAT + mx * BK + ((cx ^ (mx & 7)) << 4) + (i16 & 1) * 8);
+    for (int a = 0; a < FA; ++a) {
+        const int c = (wn >> 3) + 4 * a + 2 * g16 + (i16 >> 1 & 1), m = 8 * h + (i16 >> 2);
+        ad[a] = (unsigned int)(m * (BN * 2) + ((c ^ ((m & 3) << 2)) << 4) + (i16 & 1) * 8);
+    }
+#pragma unroll
+    for (int b = 0; b < FB; ++b) {
+        const int c = (wk >> 4) + 2 * b + g16, m = 8 * h + (i16 >> 1);
+        ax[b] = (unsigned int)(XAT + m * BK + ((c ^ turn_x(m)) << 4) + (i16 & 1) * 8);
     }
     const unsigned int as = (unsigned int)(SAT + (wk >> 7) * 256 + h * 32);
 
@@ -259,7 +263,7 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
             v8bf x[FB];
 #pragma unroll
             for (int b = 0; b < FB; ++b) {
-                const v2i c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8)(at + ax[b & 1] + s * (16 * BK) + (b >> 1) * 64));
+                const v2i c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8)(at + ax[b] + s * (16 * BK)));
                 v4i r;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {                           // rows 4i .. 4i + 3
@@ -270,8 +274,8 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
             }
 #pragma unroll
             for (int a = 0; a < FA; ++a) {
-                const v4s d0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(at + ad[a & 1] + s * (32 * BN) + (a >> 1) * 128));
-                const v4s d1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(at + ad[a & 1] + s * (32 * BN) + 8 * BN + (a >> 1) * 128));
+                const v4s d0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(at + ad[a] + s * (32 * BN)));
+                const v4s d1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(at + ad[a] + s * (32 * BN) + 8 * BN));
                 const v8bf d = __builtin_bit_cast(v8bf, __builtin_shufflevector(d0, d1, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                 for (int b = 0; b < FB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[b], d, acc[a][b], 0, 0, 0);
