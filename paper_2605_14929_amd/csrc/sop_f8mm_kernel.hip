@@ -78,7 +78,7 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
     const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
     const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
     auto load = [&](int kt) {
-        unsigned char* to = lds + (kt & 1) * STAGE + (wave << 10);
+        const unsigned int to = lds_address(lds) + (kt & 1) * STAGE + (wave << 10);
 #pragma unroll
         for (int i = 0; i < CX; ++i) load_to_lds(xw, ox[i], kt * 128, to + i * NT * 16);
 #pragma unroll
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(256) void f8mm_large_kernel(const F8MmParams p, int
     const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
     const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
     auto load = [&](const Window& x, const Window& w, int kt, int i) {  // the i-th of eight parts
-        unsigned char* to = lds + (kt & 1) * STAGE + (wave << 10) + i * 4096;
+        const unsigned int to = lds_address(lds) + (kt & 1) * STAGE + (wave << 10) + i * 4096;
         load_to_lds(x, ox[i], kt * 128, to);
         load_to_lds(w, ow[i], kt * 128, to + BM * 128);
     };

@@ -177,13 +177,13 @@ __device__ __forceinline__ unsigned int lds_address(const unsigned char* p)
 {
     return (unsigned int)__builtin_amdgcn_readfirstlane((int)(unsigned int)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) unsigned char*)p));
 }
-__device__ __forceinline__ void load_to_lds(const Window& w, unsigned int at, unsigned int uni, unsigned char* to)
+__device__ __forceinline__ void load_to_lds(const Window& w, unsigned int at, unsigned int uni, unsigned int to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds_address(to)), "v"(at), "s"(w.r), "s"(uni) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(at), "s"(w.r), "s"(uni) : "memory");
 }
-__device__ __forceinline__ void load_word_to_lds(const Window& w, unsigned int at, unsigned int uni, unsigned char* to)
+__device__ __forceinline__ void load_word_to_lds(const Window& w, unsigned int at, unsigned int uni, unsigned int to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds_address(to)), "v"(at), "s"(w.r), "s"(uni) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(at), "s"(w.r), "s"(uni) : "memory");
 }
 // all but the N loads asked for last have arrived (N = 0: all)
 template <int N = 0> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }

@@ -206,8 +206,9 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
     auto load_x = [&](int t) {
         unsigned char* to = lds + (t & 1) * STAGE;
         if (t * 64 + 64 <= p.K) {
+            const unsigned int at = lds_address(to) + (wave << 10);
 #pragma unroll
-            for (int i = 0; i < CX; ++i) load_to_lds(xw, ox[i], t * 128, to + (i * NT + (wave << 6)) * 16);
+            for (int i = 0; i < CX; ++i) load_to_lds(xw, ox[i], t * 128, at + i * NT * 16);
         } else {                                                        // (K is a multiple of eight: whole chunks)
             const int left = (p.K - t * 64) * 2;
 #pragma unroll 1

@@ -211,9 +211,9 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
         const Window d = window(p.dy + m0 * p.lddy, last * (unsigned int)p.lddy * 2u + wide_n);
         const Window x = window(p.x + m0 * p.ldx, last * (unsigned int)p.ldx + wide_k);
 #pragma unroll
-        for (int i = 0; i < LD; ++i) load_to_lds(d, od[i], 0, to + (i * NT + wave * 64) * 16);
+        for (int i = 0; i < LD; ++i) load_to_lds(d, od[i], 0, lds_address(to) + (i * NT + wave * 64) * 16);
 #pragma unroll
-        for (int i = 0; i < LX; ++i) load_to_lds(x, ox[i], 0, to + XAT + (i * NT + wave * 64) * 16);
+        for (int i = 0; i < LX; ++i) load_to_lds(x, ox[i], 0, lds_address(to) + XAT + (i * NT + wave * 64) * 16);
     };
     // Scales: the words that hold this tile's bytes come into LDS a step ahead of the step's operands (the first wavefront asks for
     // them), and become numbers there while the step before is multiplied.
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
         const long long m0 = (long long)t * 64;
         const unsigned int last = (unsigned int)min(64, p.M - (int)m0) - 1;
         load_word_to_lds(window(p.xs + m0 * p.ldxs, last * (unsigned int)p.ldxs + (unsigned int)p.ldxs), min((unsigned int)lane, last) * (unsigned int)p.ldxs + (unsigned int)(k0 >> 7 & ~3), 0,
-                         words + t % 3 * 256);
+                         lds_address(words) + t % 3 * 256);
     };
     auto put_scales = [&](int t, unsigned char* to) {
         if (tid < 64 * NKB) {
@@ -312,6 +312,171 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
                          v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
 }
 
+// ---- large gradients: 256 x 256 of dw by four wavefronts, one on a SIMD, each 128 x 128 of it.  As above, but a wavefront overlaps its own
+// work.  While sixteen rows are multiplied (sixteen matrix instructions), behind each of them stands a sixteenth of: the reads of the next
+// sixteen rows of dy, the reads of the codes after the next, the conversion of the next codes, the loads of the step after the next.  A
+// wavefront issues an instruction in four cycles, so a matrix instruction (32 cycles) hides seven others: they are dealt out evenly.
+// Halfway through a step comes its barrier: the next step has arrived, the place of the step before is free.
+template <bool X5>
+__global__ __launch_bounds__(256) void wgrad_large_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
+{
+    constexpr int BN = 256, BK = 256, XAT = 64 * BN * 2, SAT = XAT + 64 * BK, STAGE = SAT + 512, LD = 8, LX = 4;
+    extern __shared__ __align__(16) unsigned char lds[];
+    int tn, tk;
+    tile_of(blockIdx.x, tiles_n * tiles_k, tiles_n, tiles_k, group, tn, tk);
+    const int n0 = tn * BN, k0 = tk * BK, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wn = wave >> 1 << 7, wk = (wave & 1) << 7, i16 = lane & 15, g16 = lane >> 4 & 1, h = lane >> 5;
+    const int steps = (p.M + 63) >> 6;
+    const unsigned int lds0 = lds_address(lds);
+    unsigned int od[LD], ox[LX];
+    {
+        const int m = tid >> 5, n = min(n0 + ((tid & 31) ^ ((m & 3) << 2)) * 8, (p.N - 1) & ~7);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) od[i] = ((unsigned int)(m + i * 8) * (unsigned int)p.lddy + (unsigned int)n) * 2u;
+    }
+    {
+        const int m = tid >> 4, k = min(k0 + ((tid & 15) ^ ((m & 7) << 1)) * 16, (p.K - 1) & ~15);
+#pragma unroll
+        for (int i = 0; i < LX; ++i) ox[i] = (unsigned int)(m + i * 16) * (unsigned int)p.ldx + (unsigned int)k;
+    }
+    const unsigned int wide_n = (unsigned int)((p.N + 7) & ~7) * 2u, wide_k = (unsigned int)((p.K + 15) & ~15);
+    // the rows of step t; behind the last step nothing (zeros arrive, in a place that nobody reads)
+    auto rows_of = [&](const void* base, long long ld, unsigned int wide, int t) {
+        const int left = p.M - t * 64;
+        return window(reinterpret_cast<const unsigned char*>(base) + (long long)min(t, steps - 1) * 64 * ld, left > 0 ? (unsigned int)(min(64, left) - 1) * (unsigned int)ld + wide : 0u);
+    };
+    auto load_d = [&](const Window& w, int i, unsigned int to) { load_to_lds(w, od[i], 0, to + i * 4096 + (wave << 10)); };
+    auto load_x = [&](const Window& w, int i, unsigned int to) { load_to_lds(w, ox[i], 0, to + XAT + i * 4096 + (wave << 10)); };
+    // the words that hold this tile's scale bytes: a place for every wavefront and three steps
+    const unsigned int so = (unsigned int)lane * (unsigned int)p.ldxs + (unsigned int)(k0 >> 7 & ~3);
+    auto load_scales = [&](int t, int place) { load_word_to_lds(rows_of(p.xs, p.ldxs, (unsigned int)p.ldxs, t), so, 0, lds0 + 3 * STAGE + (place * 4 + wave) * 256); };
+    auto put_scales = [&](int place, unsigned char* to) {               // (rows beyond the last: byte 0, a finite scale of codes that are 0)
+        if (tid < 128) {
+            const unsigned int w = *reinterpret_cast<const unsigned int*>(lds + 3 * STAGE + (place * 4 + wave) * 256 + (tid & 63) * 4);
+            *reinterpret_cast<float*>(to + SAT + tid * 4) = e8m0_value(w >> (8 * (((k0 >> 7) + (tid >> 6)) & 3)) & 255u);
+        }
+    };
+
+    // where this lane reads: dy's squares, the codes' squares, the scales
+    unsigned int ad[4], ax[4], as = lds0 + (unsigned int)(SAT + (wk >> 7) * 256 + h * 32);
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        const int c = (wn >> 3) + 4 * a + 2 * g16 + (i16 >> 1 & 1), m = 8 * h + (i16 >> 2);
+        ad[a] = lds0 + (unsigned int)(m * (BN * 2) + ((c ^ ((m & 3) << 2)) << 4) + (i16 & 1) * 8);
+        const int cx = (wk >> 4) + 2 * a + g16, mx = 8 * h + (i16 >> 1);
+        ax[a] = lds0 + (unsigned int)(XAT + mx * BK + ((cx ^ ((mx & 7) << 1)) << 4) + (i16 & 1) * 8);
+    }
+    typedef __attribute__((address_space(3))) v4s* lds16;
+    typedef __attribute__((address_space(3))) v2i* lds8;
+    typedef __attribute__((address_space(3))) v4f* ldsf;
+
+    v16f acc[4][4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+    v4s d[2][4][2];
+    v2i c[2][4];
+    v4f sc[2][2];
+    v4i x[2][4];
+    auto read_d = [&](int s, int i) { d[s & 1][i >> 1][i & 1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(uintptr_t)(ad[i >> 1] + s * (32 * BN) + (i & 1) * (8 * BN))); };
+    auto read_c = [&](int s, int i) {
+        if (i < 2) sc[s & 1][i] = *(ldsf)(uintptr_t)(as + s * 64 + i * 16);
+        else c[s & 1][i - 2] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8)(uintptr_t)(ax[i - 2] + s * (16 * BK)));
+    };
+    auto convert = [&](int s, int i) {                                  // a word: two of a column's eight codes
+        const int b = i >> 2, k = i & 3;
+        const v4f f = sc[s & 1][k >> 1];
+        const int w = k & 1 ? two_rows<X5, true>(c[s & 1][b][k >> 1], f[2], f[3]) : two_rows<X5, false>(c[s & 1][b][k >> 1], f[0], f[1]);
+        x[s & 1][b][k] = w;
+        asm volatile("" : "+v"(x[s & 1][b][k]));                        // (here, and not where it is used)
+    };
+    auto multiply = [&](int s, int i) {
+        const int a = i >> 2, b = i & 3;
+        const v8bf y = __builtin_bit_cast(v8bf, __builtin_shufflevector(d[s & 1][a][0], d[s & 1][a][1], 0, 1, 2, 3, 4, 5, 6, 7));
+        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, x[s & 1][b]), y, acc[a][b], 0, 0, 0);
+    };
+
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {                                       // two steps' operands, three steps' scale words
+        const Window wd = rows_of(p.dy, p.lddy * 2, wide_n, t), wx = rows_of(p.x, p.ldx, wide_k, t);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) load_d(wd, i, lds0 + t * STAGE);
+#pragma unroll
+        for (int i = 0; i < LX; ++i) load_x(wx, i, lds0 + t * STAGE);
+        load_scales(t, t);
+    }
+    load_scales(2, 2);
+    wait_loads();
+    __syncthreads();
+    put_scales(0, lds);
+    put_scales(1, lds + STAGE);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) read_d(0, i);
+#pragma unroll
+    for (int i = 0; i < 6; ++i) { read_c(0, i); read_c(1, i); }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) convert(0, i);
+    int r = 0;                                                          // t modulo 3: the place of step t
+    for (int t = 0; t < steps; ++t) {
+        const int r1 = r == 2 ? 0 : r + 1, r2 = r1 == 2 ? 0 : r1 + 1;   // ... of step t + 1, of step t + 2
+        const unsigned int hop = (unsigned int)(r1 - r) * STAGE;
+        auto part = [&](auto S) {                                       // sixteen rows
+            constexpr int s = decltype(S)::value;
+            if (s == 2) {                                               // from here on codes and scales are the next step's, a sixteen later dy
+#pragma unroll
+                for (int a = 0; a < 4; ++a) ax[a] += hop;
+                as += hop;
+            }
+            if (s == 3) {
+#pragma unroll
+                for (int a = 0; a < 4; ++a) ad[a] += hop;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                multiply(s, i);
+                if (i & 1) read_d((s + 1) & 3, i >> 1);
+                else if (i < 12) read_c((s + 2) & 3, i >> 1);
+                convert(s + 1, i);
+                if (s == 2 && (i & 1) == 0) load_d(rows_of(p.dy, p.lddy * 2, wide_n, t + 2), i >> 1, lds0 + r2 * STAGE);
+                if (s == 3 && i < 8 && (i & 1) == 0) load_x(rows_of(p.x, p.ldx, wide_k, t + 2), i >> 1, lds0 + r2 * STAGE);
+                if (s == 3 && i == 8) load_scales(t + 3, r);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        part(std::integral_constant<int, 0>{});
+        part(std::integral_constant<int, 1>{});
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        put_scales(r2, lds + r2 * STAGE);
+        part(std::integral_constant<int, 2>{});
+        part(std::integral_constant<int, 3>{});
+        r = r1;
+    }
+    wait_loads();
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_dw(p, n0 + wn + a * 32 + (lane & 31), k0 + wk + b * 32 + 8 * i + 4 * h,
+                         v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+}
+
+template <bool X5> static hipError_t wgrad_large_go(const WgradParams& p, hipStream_t st)
+{
+    const int tn = (p.N + 255) / 256, tk = (p.K + 255) / 256, bytes = 3 * (64 * 512 + 64 * 256 + 512) + 3 * 4 * 256;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&wgrad_large_kernel<X5>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(wgrad_large_kernel<X5>, dim3((unsigned)(tn * tk)), dim3(256), bytes, st, p, tn, tk, 8);
+    return hipGetLastError();
+}
+
 template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_turn_go(const WgradParams& p, hipStream_t st)
 {
     const int tn = (p.N + BN - 1) / BN, tk = (p.K + BK - 1) / BK, bytes = 3 * (64 * BN * 2 + 64 * BK + BK / 128 * 256) + 3 * 256;
@@ -336,7 +501,7 @@ template <bool X5> static hipError_t wgrad_pick(const WgradParams& p, int n_cu, 
 {
     auto tiles = [&](int a, int b) { return (long long)((p.N + a - 1) / a) * ((p.K + b - 1) / b); };
     const bool on16 = (reinterpret_cast<uintptr_t>(p.dy) & 15) == 0 && (p.lddy & 7) == 0 && p.lddy <= 1 << 22;
-    if (p.M > 0 && on16) return tiles(256, 256) >= n_cu ? wgrad_turn_go<256, 256, 2, 4, X5>(p, st) : wgrad_turn_go<128, 128, 2, 2, X5>(p, st);
+    if (p.M > 0 && on16) return tiles(256, 256) >= n_cu ? wgrad_large_go<X5>(p, st) : wgrad_turn_go<128, 128, 2, 2, X5>(p, st);
     if (tiles(256, 256) >= n_cu) return wgrad_go<256, 256, 2, 4, X5>(p, st);
     if (tiles(128, 128) >= n_cu) return wgrad_go<128, 128, 2, 2, X5>(p, st);
     return wgrad_go<64, 128, 2, 2, X5>(p, st);
