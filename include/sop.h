@@ -576,7 +576,7 @@ sop_status sop_fp8_gated_grad(sop_ctx* ctx, const sop_f8_matrix* gate8, const so
  * is then not looked at).  A code beyond its codebook's entries stands for the last one. */
 typedef struct {
     const uint16_t* words_dev;    /* N * K / g                                  */
-    const uint8_t*  payload_dev;  /* N * K * n_bits / 8 bytes                   */
+    const uint8_t*  payload_dev;  /* N * K * n_bits / 8 bytes, 8-byte aligned   */
     int64_t N, K;
     int g, n_bits;                /* g 8, 16, 32 or 64; n_bits 1..6             */
     sop_scale_fmt fmt;

@@ -66,6 +66,7 @@ typedef int v2i __attribute__((ext_vector_type(2)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v8s __attribute__((ext_vector_type(8)));
@@ -165,10 +166,13 @@ __device__ __forceinline__ Window window(const void* p, unsigned int bytes)
     const unsigned long long a = reinterpret_cast<unsigned long long>(p);
     return Window{v4i{__builtin_amdgcn_readfirstlane((int)a), __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xFFFF), __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000}};
 }
+__device__ __forceinline__ auto resource(const Window& w)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)(unsigned int)w.r[0] | (unsigned long long)(unsigned int)w.r[1] << 32), 0, w.r[2], 0x00027000);
+}
 __device__ __forceinline__ unsigned int load_word(const Window& w, unsigned int at, unsigned int uni)
 {
-    const auto r = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((unsigned long long)(unsigned int)w.r[0] | (unsigned long long)(unsigned int)w.r[1] << 32), 0, w.r[2], 0x00027000);
-    return (unsigned int)__builtin_amdgcn_raw_buffer_load_b32(r, (int)at, (int)uni, 0);
+    return (unsigned int)__builtin_amdgcn_raw_buffer_load_b32(resource(w), (int)at, (int)uni, 0);
 }
 // ... 16 (or 4) bytes a lane straight into LDS, lane by lane from `to` on (the same for all lanes).  Written out so that the compiler does not
 // wait for them by itself before other reads of LDS: whoever reads what they bring waits for its own wavefront's loads (wait_loads),

@@ -209,7 +209,7 @@ extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, 
     const int g = w->g;
     if ((g != 8 && g != 16 && g != 32 && g != 64) || w->K % g) return bad(c, call, SOP_ESHAPE, "g is 8, 16, 32 or 64 and divides K");
     if (w->n_bits < 1 || w->n_bits > 6) return bad(c, call, SOP_EINVAL, "codes have 1 to 6 bits");
-    if (!w->words_dev || !w->payload_dev || off(w->words_dev, 2)) return bad(c, call, SOP_EINVAL, "words and payload must not be NULL, words on 2 bytes");
+    if (!w->words_dev || !w->payload_dev || off(w->words_dev, 2) || off(w->payload_dev, 8)) return bad(c, call, SOP_EINVAL, "words and payload must not be NULL, words on 2 bytes, payload on 8");
     if (!w->table_a || w->entries_a < 1 || w->entries_a > SOP_MAX_ENTRIES) return bad(c, call, SOP_EATOM, "the first codebook has 1 to 64 entries");
     if ((w->table_b != nullptr) != (w->entries_b > 0) || w->entries_b < 0 || w->entries_b > SOP_MAX_ENTRIES) return bad(c, call, SOP_EATOM, "the second codebook has 1 to 64 entries, or is NULL with 0");
     const int sb = w->fmt.sign_bits, xb = w->fmt.exp_bits, yb = w->fmt.man_bits, b = w->fmt.container_bits, m = b - sb - xb - yb;

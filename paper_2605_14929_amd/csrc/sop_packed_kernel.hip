@@ -290,6 +290,210 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
                         v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
 }
 
+// ---- large products of 4-bit codes: 256 x 256 of y by four wavefronts, one on a SIMD, each 128 x 128 of it; 64 elements along K a step,
+// two steps in LDS.  While sixteen elements are multiplied (sixteen matrix instructions), the next sixteen's operands are read, and between
+// two barriers (64 matrix instructions) every thread forms 64 weights of the step after the next, eight by eight: behind each matrix
+// instruction stand a part of the look-ups and of the scale word of an eight, and a part of the products of the eight before.  A matrix
+// instruction (32 cycles) hides seven others of its wavefront, so what a weight costs in instructions is what counts: two codes (a byte of
+// the payload) are looked up at once, in a table of the 256 pairs of either codebook.  Halfway through a step comes its barrier: the
+// next step is there, this one's place is free.
+template <bool G8>
+__global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
+{
+    constexpr int BM = 256, BN = 256, STAGE = (BM + BN) * 128, TAB = 4096, WORDS = G8 ? 2 : 1;
+    constexpr unsigned int NOWHERE = 0xE0000000u;                       // an offset beyond every window
+    extern __shared__ __align__(4096) unsigned char lds[];
+    int tm, tn;
+    tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
+    const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1 << 7, wn = (wave & 1) << 7, lg = 31 - __builtin_clz(p.g), steps = (p.K + 63) >> 6;
+    const unsigned int tab0 = lds_address(lds), lds0 = tab0 + TAB;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) *reinterpret_cast<float2*>(lds + b * 2048 + tid * 8) = make_float2(p.tab[b][tid & 15], p.tab[b][tid >> 4]);
+
+    // x: chunks of 16 bytes straight into LDS
+    const unsigned int xcol = (unsigned int)((tid ^ tid >> 4) & 7) << 4;   // (rows 32 apart lie alike)
+    unsigned int ox[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ox[i] = (unsigned int)min(i * 32 + (tid >> 3), p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + xcol;
+    const Window xw = window(p.x + (long long)m0 * p.ldx, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)(p.ldx * 2) + (unsigned int)p.K * 2);
+    auto load_x = [&](int t, int i) { load_to_lds(xw, ox[i], t * 128, lds0 + (t & 1) * STAGE + (wave << 10) + i * 4096); };
+    // w: an item is sixteen codes of a row, four items a row and step, four of a thread
+    const int rows = min(BN, p.N - n0), k16 = (tid & 3) * 16;
+    const unsigned int prow = (unsigned int)(p.K >> 1), wrow = (unsigned int)(p.K >> lg) * 2u;
+    const Window pw = window(p.payload + (long long)n0 * prow, (unsigned int)rows * prow), ww = window(p.words + (long long)n0 * (p.K >> lg), (unsigned int)rows * wrow);
+    unsigned int op[4], ow[4][WORDS];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned int r = (unsigned int)min(i * 64 + (tid >> 2), rows - 1);
+        op[i] = r * prow + (unsigned int)(k16 >> 1);
+#pragma unroll
+        for (int h = 0; h < WORDS; ++h) ow[i][h] = r * wrow + (unsigned int)((k16 >> lg) + h) * 2u;
+    }
+    // Elements of the last step beyond K: x is asked for nowhere, and zeros arrive; so are the scale words, whose scale is 0.
+    const bool odd = (p.K & 63) != 0;
+    auto end_x = [&](int t) {
+        if (odd && t == steps - 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ox[i] = t * 128 + (int)xcol < p.K * 2 ? ox[i] : NOWHERE;
+        }
+    };
+    auto end_w = [&](int t) {
+        if (odd && t == steps - 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < WORDS; ++h) ow[i][h] = t * 64 + k16 + 8 * h < p.K ? ow[i][h] : NOWHERE;
+        }
+    };
+    struct Item { unsigned int c[2], w[WORDS]; };
+    auto load_w = [&](Item& z, int t, int i) {
+        const auto c = __builtin_amdgcn_raw_buffer_load_b64(resource(pw), (int)op[i], t * 32, 0);
+        z.c[0] = c[0]; z.c[1] = c[1];
+#pragma unroll
+        for (int h = 0; h < WORDS; ++h) z.w[h] = __builtin_amdgcn_raw_buffer_load_b16(resource(ww), (int)ow[i][h], t * (128 >> lg), 0);
+    };
+
+    v16f acc[4][4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+
+    typedef __attribute__((address_space(3))) v4i* ldsi;
+    typedef __attribute__((address_space(3))) v2f* ldsp;
+    unsigned int put[2], putting[2] = {0, 0};                           // where this thread's weights go (rows 64 apart lie alike)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) put[h] = lds0 + BM * 128 + (unsigned int)(tid >> 2) * 128 + (unsigned int)((((tid & 3) * 2 + h) ^ (tid >> 3 & 7)) << 4);
+    v2f v[2][4];
+    float scale[2];
+    unsigned int book = 0, mag = 0, ex = 0, frac = 0;
+    // eight weights (half h of item z; o = 0 or 1 in turn): the e-th of eight parts of the look-ups and the scale
+    auto look_up = [&](const Item& z, int h, int o, int e) {
+        const unsigned int w = z.w[h & (WORDS - 1)];
+        if (e == 0) book = tab0 | (w >> p.sel_pos & (unsigned int)p.sel_mask) << 11;
+        if (!(e & 1)) {
+            const unsigned int m = e == 0 ? z.c[h] << 3 : z.c[h] >> (4 * e - 3);
+            v[o][e >> 1] = *(ldsp)(uintptr_t)((m & 0x7F8u) | book);
+        }
+        if (e == 1) { mag = (w >> p.mag_shift) & (unsigned int)p.mag_mask; ex = mag >> p.man_bits; }
+        if (e == 3) { frac = (mag & (unsigned int)p.man_mask) | min(ex, 1u) << p.man_bits; ex = max(ex, 1u); }
+        if (e == 5) { scale[o] = __builtin_amdgcn_ldexpf((float)frac, (int)ex + p.exp_off); }
+        if (e == 7) scale[o] = __uint_as_float(__float_as_uint(scale[o]) | (w << p.sign_up & 0x80000000u));
+    };
+    v4i u;
+    // ... of their products, rounded and stored as item i
+    auto form = [&](int i, int h, int o, int e) {
+        if (e == 0) asm volatile("" : "+v"(v[o][0]), "+v"(v[o][1]), "+v"(v[o][2]), "+v"(v[o][3]));   // (one wait for all four)
+        if (!(e & 1)) return;
+        u[e >> 1] = (int)bf16_pair(scale[o] * v[o][e >> 1][0], scale[o] * v[o][e >> 1][1]);
+        asm volatile("" : "+v"(u[e >> 1]));
+        if (e == 7) *(ldsi)(uintptr_t)(putting[h] + i * 8192) = u;
+    };
+
+    const int r32 = lane & 31;
+    unsigned int at[4];                                                 // the s-th sixteen elements of this lane's row, without the row
+#pragma unroll
+    for (int s = 0; s < 4; ++s) at[s] = lds0 + (unsigned int)r32 * 128 + ((unsigned int)(((lane >> 5) ^ (r32 >> 1 & 7)) << 4) ^ (unsigned int)(s << 5));
+    v4i fx[2][4], fw[2][4];
+    unsigned int rx = 0, rw = 0;
+    auto from = [&](unsigned int stage, int s) { rx = at[s] + (stage + wm * 128); rw = at[s] + (stage + (BM + wn) * 128); };
+    auto read = [&](int s, int i) {                                     // the i-th of eight reads
+        if (i < 4) fw[s & 1][i] = *(ldsi)(uintptr_t)(rw + i * 4096);
+        else fx[s & 1][i - 4] = *(ldsi)(uintptr_t)(rx + (i - 4) * 4096);
+    };
+    auto multiply = [&](int s, int i) {
+        const int a = i >> 2, b = i & 3;
+        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, fw[s & 1][b]), __builtin_bit_cast(v8bf, fx[s & 1][a]), acc[a][b], 0, 0, 0);
+    };
+
+    Item now[4], next[4];
+    auto settle = [&](Item (&z)[4]) {                                   // what has arrived is used as such (and not waited for again behind later loads)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            asm volatile("" : "+v"(z[i].c[0]), "+v"(z[i].c[1]), "+v"(z[i].w[0]));
+            if (G8) asm volatile("" : "+v"(z[i].w[WORDS - 1]));
+        }
+    };
+    __syncthreads();                                                    // the codebooks are there
+    // the first step whole; of the second, x and a quarter of the weights
+    for (int t = 0; t < 2; ++t) {
+        end_x(t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) load_x(t, i);
+    }
+    end_w(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_w(next[i], 0, i);
+    end_w(1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_w(now[i], 1, i);
+    putting[0] = put[0]; putting[1] = put[1];
+#pragma unroll
+    for (int g = 0; g < 10; ++g) {
+        if (g == 8) { putting[0] += STAGE; putting[1] += STAGE; }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) look_up(g < 8 ? next[g >> 1] : now[0], g & 1, 0, e);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) form(g >> 1 & 3, g & 1, 0, e);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) look_up(now[1], 0, 0, e);
+    wait_loads();
+    __syncthreads();
+    settle(now);
+    from(0, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) read(0, i);
+    for (int t = 0; t < steps; ++t) {
+        const unsigned int here = (t & 1) * STAGE, there = STAGE - here;
+        // sixteen elements of K, and a quarter of the work between two barriers: behind a step's last sixteen elements the first quarter of the
+        // step after the next, behind the next step's first three times sixteen the others
+        auto part = [&](auto S) {
+            constexpr int s = decltype(S)::value, Q = (s + 1) & 3;
+            from(s == 3 ? there : here, (s + 1) & 3);
+            if (s == 0) end_w(t + 2);
+            if (s == 3) {
+                end_x(t + 2);
+                putting[0] = put[0] + here; putting[1] = put[1] + here;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                multiply(s, i);
+                if ((i & 1) == 0) read((s + 1) & 3, i >> 1);
+                const int g = Q * 2 + (i >> 3), e = i & 7;              // the eight whose products are formed; the one after it is looked up
+                form(g >> 1, g & 1, g & 1, e);
+                if (s == 2 && i == 8) { wait_loads(); settle(next); }
+                if (g < 7) look_up(now[(g + 1) >> 1], (g + 1) & 1, (g + 1) & 1, e);
+                else look_up(next[0], 0, 0, e);
+                if (s == 3 && (i & 1)) load_x(t + 2, i >> 1);
+                if (Q >= 1 && Q < 3 && (i & 7) == 3) load_w(next[(Q - 1) * 2 + (i >> 3)], t + 2, (Q - 1) * 2 + (i >> 3));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        part(std::integral_constant<int, 0>{});
+        part(std::integral_constant<int, 1>{});
+        part(std::integral_constant<int, 2>{});
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // (the loads were waited for eight instructions ago)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) now[i] = next[i];
+        part(std::integral_constant<int, 3>{});
+    }
+    wait_loads();
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * (lane >> 5),
+                        v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+}
+
 template <int NB, int FM, int U, int W> static hipError_t rows_go(const PackedMmParams& p, hipStream_t st)
 {
     auto fn = p.g == 8 ? &packed_rows_kernel<NB, FM, U, W, 4> : p.g == 16 ? &packed_rows_kernel<NB, FM, U, W, 2> : &packed_rows_kernel<NB, FM, U, W, 1>;
@@ -306,12 +510,24 @@ template <int NB, int BM, int BN, int WR, int WC> static hipError_t tile_go(cons
     hipLaunchKernelGGL((packed_tile_kernel<NB, BM, BN, WR, WC>), dim3((unsigned)(tm * tn)), dim3(WR * WC * 64), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
+static hipError_t large_go(const PackedMmParams& p, hipStream_t st)
+{
+    const int tm = (p.M + 255) / 256, tn = (p.N + 255) / 256, bytes = 4096 + 2 * 512 * 128;
+    auto fn = p.g == 8 ? &packed_large_kernel<true> : &packed_large_kernel<false>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(256), bytes, st, p, tm, tn, 8);
+    return hipGetLastError();
+}
 template <int NB> static hipError_t packed_pick(const PackedMmParams& p, int n_cu, hipStream_t st)
 {
     auto tiles = [&](int bm, int bn) { return (long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn); };
     if (p.M <= 16) return rows_go<NB, 1, 3, 16>(p, st);
     if (p.M <= 32) return rows_go<NB, 2, 2, 8>(p, st);
-    if (tiles(256, 256) >= n_cu) return tile_go<NB, 256, 256, 2, 4>(p, st);
+    if (tiles(256, 256) >= n_cu) {
+        if constexpr (NB == 4) return large_go(p, st);
+        else return tile_go<NB, 256, 256, 2, 4>(p, st);
+    }
     if (tiles(128, 128) >= n_cu) return tile_go<NB, 128, 128, 2, 2>(p, st);
     return tile_go<NB, 64, 64, 2, 2>(p, st);
 }
