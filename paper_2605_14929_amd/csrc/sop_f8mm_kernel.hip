@@ -165,15 +165,31 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
         }
     };
 
+    // Wide tiles: the lines of three steps on come to L2 ahead of the loads that want them.  A row's line is asked for by one of the tiles in
+    // flight on this XCD that read it (four beside each other read the same rows of x, eight the same of w, the step says whose turn it is); the
+    // word that comes of it is dropped.  8192 x 8192 x 8192 takes 494 us so, 550 without; 4096 x 11008 x 4096 198 and 206.
+    constexpr bool AHEAD = BM == 256 && BN == 256;
+    auto ask_ahead = [&](int kt) {
+        const bool of_x = wave < WR * WC / 2;
+        const bool ours = kt < KF && (of_x ? ((tn ^ kt) & 3) == 0 : ((tm ^ kt) & 7) == 0);
+        Window a = of_x ? xw : ww;
+        a.r[2] = ours ? a.r[2] : 0;
+        const int r = tid & 255;
+        load_word_to_lds(a, of_x ? (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx : (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw, kt * 128,
+                         lds_address(lds) + 2 * STAGE + (wave & 3) * 256);
+    };
     scales(0);
     if (KF) load(0);
+    if (AHEAD) ask_ahead(2);
     for (int kt = 0; kt < KF; ++kt) {
-        wait_loads();
+        wait_loads<AHEAD ? 1 : 0>();                                    // (all but the word asked for last)
         __syncthreads();                                                // this step has arrived, and nobody reads the other half any more
         if (kt + 1 < KF) load(kt + 1);
+        if (AHEAD) ask_ahead(kt + 3);
         turn(kt);
         compute(kt);
     }
+    if (AHEAD) wait_loads();
     if (KF < KB) {                                                      // the last step of an odd K: elements beyond it count as zeros
         unsigned char* to = lds + (KF & 1) * STAGE;
         const int left = p.K & 127;
@@ -194,161 +210,6 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
     for (int a = 0; a < FM; ++a)
 #pragma unroll
         for (int b = 0; b < FN; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * h, v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
-}
-
-// ---- large products: 256 x 256 of y by four wavefronts, one on a SIMD, each 128 x 128 of it; 128 elements along K a step, two steps in LDS.
-// What an instruction takes from LDS is what bounds such a tile: eight wavefronts of 128 x 64 read 192 KB a step, these read 128 KB.
-// A wavefront alone on its SIMD overlaps its own work: while a half step (64 elements) is multiplied, the operands of the next half
-// step are read into a second set of registers, one read behind every matrix instruction.  Halfway through a step comes its barrier:
-// the next step has arrived, this one's place in LDS is free for the step after the next.  In LDS a row is eight chunks of 16 bytes,
-// chunk c at position c ^ (row / 2 & 7), as above.
-template <int XF>
-__global__ __launch_bounds__(256) void f8mm_large_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
-{
-    constexpr int BM = 256, BN = 256, F = 4, STAGE = (BM + BN) * 128;
-    extern __shared__ __align__(16) unsigned char lds[];
-    int tm, tn;
-    tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
-    const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 1 << 7, wn = (wave & 1) << 7, r32 = lane & 31, h = lane >> 5;
-    const unsigned char* xb = p.x + (long long)m0 * p.ldx;
-    const unsigned char* wb = p.w + (long long)n0 * p.ldw;
-    const int KF = p.K >> 7, KB = (p.K + 127) >> 7;                     // whole steps, all steps
-    unsigned int ox[8], ow[8];                                          // byte offsets of this thread's chunks; rows beyond the matrix read its last
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = i * 256 + tid, r = c >> 3, col = ((c ^ r >> 1) & 7) << 4;
-        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + col;
-        ow[i] = (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw + col;
-    }
-    const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
-    const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
-    auto load = [&](const Window& x, const Window& w, int kt, int i) {  // the i-th of eight parts
-        const unsigned int to = lds_address(lds) + (kt & 1) * STAGE + (wave << 10) + i * 4096;
-        load_to_lds(x, ox[i], kt * 128, to);
-        load_to_lds(w, ow[i], kt * 128, to + BM * 128);
-    };
-
-    // scales: four steps of a row of x in a word, four of w likewise; the next four are asked for while these are used
-    const Window xsw = window(p.xs + (long long)m0 * p.ldxs, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldxs + (unsigned int)((KB + 3) & ~3));
-    const unsigned char* wsb = p.ws + (long long)min((n0 + wn) >> 7, (p.N - 1) >> 7) * p.ws_n;
-    unsigned int sxo[F], sx[F], nx[F], sw = 0, nw[4];
-#pragma unroll
-    for (int f = 0; f < F; ++f) sxo[f] = (unsigned int)min(wm + f * 32 + r32, p.M - 1 - m0) * (unsigned int)p.ldxs;
-    auto scales = [&](int kt) {
-#pragma unroll
-        for (int f = 0; f < F; ++f) nx[f] = load_word(xsw, sxo[f], kt);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) nw[j] = wsb[(long long)min(kt + j, KB - 1) * p.ws_k];
-    };
-    auto turn = [&](int kt) {                                           // before step kt: its scales into place
-        if ((kt & 3) == 0) {
-#pragma unroll
-            for (int f = 0; f < F; ++f) sx[f] = nx[f];
-            sw = nw[0] | nw[1] << 8 | nw[2] << 16 | nw[3] << 24;
-            if (kt + 4 < KB) scales(kt + 4);
-        } else {
-#pragma unroll
-            for (int f = 0; f < F; ++f) sx[f] >>= 8;
-            sw >>= 8;
-        }
-    };
-
-    v16f acc[F][F];
-#pragma unroll
-    for (int a = 0; a < F; ++a)
-#pragma unroll
-        for (int b = 0; b < F; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
-
-    const unsigned int z = (unsigned int)((2 * h) ^ (r32 >> 1 & 7)) << 4;   // chunks 2h and 2h + 1 of the first half step, 4 + 2h and 5 + 2h of the second
-    const unsigned int lx = (unsigned int)(wm + r32) * 128, lw = (unsigned int)(BM + wn + r32) * 128;
-    struct Operands { v4i x[F][2], w[F][2]; };
-    auto read = [&](Operands& o, int kt, int j, int i) {                // the i-th of sixteen reads of half step j
-        const unsigned char* at = lds + (kt & 1) * STAGE + (i & 7) / 2 * 4096;
-        const unsigned int c = z ^ (unsigned int)(j << 6) ^ (unsigned int)((i & 1) << 4);
-        (i < 8 ? o.w : o.x)[(i & 7) / 2][i & 1] = *reinterpret_cast<const v4i*>(at + ((i < 8 ? lw : lx) + c));
-    };
-    auto multiply = [&](const Operands& o, int i) {                     // the i-th of sixteen squares
-        const int a = i >> 2, b = i & 3;
-        acc[a][b] = mfma_f8<XF>(__builtin_shufflevector(o.w[b][0], o.w[b][1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_shufflevector(o.x[a][0], o.x[a][1], 0, 1, 2, 3, 4, 5, 6, 7), acc[a][b], (int)sw, (int)sx[a]);
-    };
-    auto meet = [&]() {                                                 // this wavefront's reads of LDS have ended, what it asked for has arrived
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    };
-
-    Operands first, second;
-    scales(0);
-    if (KF) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) load(xw, ww, 0, i);
-        meet();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) read(first, 0, 0, i);
-        if (KF > 1)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) load(xw, ww, 1, i);
-    }
-    // (One stretch of code for all steps: where there is no further step, empty windows are read, which bring zeros to a place that
-    // nobody reads any more, and operands that nobody uses.)  The
-    // loads of a step are spread over a whole step, one pair behind every fourth or second instruction: a wavefront that issues them
-    // faster than they are taken holds up its own matrix instructions.
-    for (int kt = 0; kt < KF; ++kt) {
-        turn(kt);
-        Window x1 = xw, w1 = ww;
-        x1.r[2] = kt + 1 < KF ? xw.r[2] : 0;
-        w1.r[2] = kt + 1 < KF ? ww.r[2] : 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            read(second, kt, 1, i);
-            if (i < 8 && (i & 1)) load(x1, w1, kt + 1, 4 + (i >> 1));
-            multiply(first, i);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        meet();
-        x1.r[2] = kt + 2 < KF ? xw.r[2] : 0;
-        w1.r[2] = kt + 2 < KF ? ww.r[2] : 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if ((i & 3) == 3) load(x1, w1, kt + 2, i >> 2);
-            read(first, kt + 1, 0, i);
-            multiply(second, i);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    meet();
-    if (KF < KB) {                                                      // the last step of an odd K: elements beyond it count as zeros
-        unsigned char* to = lds + (KF & 1) * STAGE;
-        const int left = p.K & 127;
-#pragma unroll 1
-        for (int c = tid; c < (BM + BN) * 8; c += 256) {
-            const bool of_x = c < BM * 8;
-            const int d = of_x ? c : c - BM * 8, r = d >> 3, col = ((d ^ r >> 1) & 7) << 4, n = left - col;
-            const unsigned char* row = of_x ? xb + (long long)min(r, p.M - 1 - m0) * p.ldx : wb + (long long)min(r, p.N - 1 - n0) * p.ldw;
-            v4i v = {0, 0, 0, 0};
-            if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + col), n);
-            *reinterpret_cast<v4i*>(to + c * 16) = v;
-        }
-        __syncthreads();
-        turn(KF);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) read(first, KF, j, i);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) multiply(first, i);
-        }
-    }
-#pragma unroll
-    for (int a = 0; a < F; ++a)
-#pragma unroll
-        for (int b = 0; b < F; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * h, v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
@@ -455,9 +316,136 @@ __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, i
     }
 }
 
+// ---- few tiles: 32 FM x 32 FN of y a workgroup, K dealt out to its W wavefronts step by step.  Every wavefront has its own place in LDS for
+// a step's operands and waits for its own loads alone: rows come in whole lines that way, which operands loaded straight into registers
+// (32 bytes of a row a lane) do not.  While a step is multiplied the wavefront's next one is on its way.  The wavefronts' sums meet in LDS in
+// a fixed order.
+template <int FM, int FN, int XF, bool EXACT>
+__global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
+{
+    constexpr int W = 8, ROWS = 32 * (FM + FN), OWN = ROWS * 128, LOADS = ROWS / 8;
+    static_assert(FM * FN * 4096 <= OWN, "the sums fit where the operands were");
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r32 = lane & 31, h = lane >> 5;
+    int tm, tn;
+    tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
+    const int m0 = tm * (32 * FM), n0 = tn * (32 * FN), KF = p.K >> 7, KB = (p.K + 127) >> 7;
+    const unsigned char* xb = p.x + (long long)m0 * p.ldx;
+    const unsigned char* wb = p.w + (long long)n0 * p.ldw;
+    unsigned char* own = lds + wave * OWN;
+    const unsigned int own0 = lds_address(own);
+    unsigned int off[LOADS];                                            // rows of x, then rows of w; rows beyond the matrix read its last
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int r = i * 8 + (lane >> 3), col = ((lane ^ r >> 1) & 7) << 4;
+        off[i] = i < 4 * FM ? (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + col : (unsigned int)min(r - 32 * FM, p.N - 1 - n0) * (unsigned int)p.ldw + col;
+    }
+    const Window xw = window(xb, (unsigned int)(min(32 * FM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
+    const Window ww = window(wb, (unsigned int)(min(32 * FN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
+    unsigned int sx[FM], sw[FN], nx[FM], nw[FN];
+    const unsigned char* xsr[FM];
+    const unsigned char* wsr[FN];
+#pragma unroll
+    for (int a = 0; a < FM; ++a) xsr[a] = p.xs + (long long)min(m0 + a * 32 + r32, p.M - 1) * p.ldxs;
+#pragma unroll
+    for (int b = 0; b < FN; ++b) wsr[b] = p.ws + (long long)(min(n0 + b * 32, p.N - 1) >> 7) * p.ws_n;
+    auto load = [&](int kt) {
+#pragma unroll
+        for (int a = 0; a < FM; ++a) nx[a] = xsr[a][kt];
+#pragma unroll
+        for (int b = 0; b < FN; ++b) nw[b] = wsr[b][(long long)kt * p.ws_k];
+        if (kt < KF) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load_to_lds(i < 4 * FM ? xw : ww, off[i], kt * 128, own0 + i * 1024);
+        } else {                                                        // the last step of an odd K: elements beyond it count as zeros
+            const int left = p.K & 127;
+#pragma unroll 1
+            for (int c = lane; c < ROWS * 8; c += 64) {
+                const int r = c >> 3, col = ((c ^ r >> 1) & 7) << 4, n = left - col;
+                const unsigned char* row = r < 32 * FM ? xb + (long long)min(r, p.M - 1 - m0) * p.ldx : wb + (long long)min(r - 32 * FM, p.N - 1 - n0) * p.ldw;
+                v4i v = {0, 0, 0, 0};
+                if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + col), n);
+                *reinterpret_cast<v4i*>(own + c * 16) = v;
+            }
+        }
+    };
+    v16f acc[FM][FN];
+#pragma unroll
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+        for (int b = 0; b < FN; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+    const unsigned int z = (unsigned int)((2 * h) ^ (r32 >> 1 & 7)) << 4;
+    v8i x[FM][2], w[FN][2];
+    auto frag = [&](int f, int j) {
+        const unsigned char* at = own + (f * 32 + r32) * 128;
+        const unsigned int c = z ^ (unsigned int)(j << 6);
+        return __builtin_shufflevector(*reinterpret_cast<const v4i*>(at + c), *reinterpret_cast<const v4i*>(at + (c ^ 16)), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    if (wave < KB) load(wave);
+    for (int kt = wave; kt < KB; kt += W) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int a = 0; a < FM; ++a) { sx[a] = nx[a]; asm volatile("" : "+v"(sx[a])); }
+#pragma unroll
+        for (int b = 0; b < FN; ++b) { sw[b] = nw[b]; asm volatile("" : "+v"(sw[b])); }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int a = 0; a < FM; ++a) x[a][j] = frag(a, j);
+#pragma unroll
+            for (int b = 0; b < FN; ++b) w[b][j] = frag(FM + b, j);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // (the reads have ended: the place is free)
+        __builtin_amdgcn_sched_barrier(0);
+        if (kt + W < KB) load(kt + W);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (EXACT) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v8bf fx[FM], fw[FN];
+#pragma unroll
+                    for (int a = 0; a < FM; ++a) fx[a] = __builtin_bit_cast(v8bf, eight_bf16<XF == 1>(x[a][j][2 * i], x[a][j][2 * i + 1], e8m0_value(sx[a])));
+#pragma unroll
+                    for (int b = 0; b < FN; ++b) fw[b] = __builtin_bit_cast(v8bf, eight_bf16<false>(w[b][j][2 * i], w[b][j][2 * i + 1], e8m0_value(sw[b])));
+#pragma unroll
+                    for (int a = 0; a < FM; ++a)
+#pragma unroll
+                        for (int b = 0; b < FN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[b], fx[a], acc[a][b], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int a = 0; a < FM; ++a)
+#pragma unroll
+                    for (int b = 0; b < FN; ++b) acc[a][b] = mfma_f8<XF>(w[b][j], x[a][j], acc[a][b], (int)sw[b], (int)sx[a]);
+            }
+        }
+    }
+    wait_loads();
+    __syncthreads();
+    v4f* part = reinterpret_cast<v4f*>(own);                            // [square][quarter][lane], this wavefront's
+#pragma unroll
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+        for (int b = 0; b < FN; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                part[((a * FN + b) * 4 + i) * 64 + lane] = v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]};
+    __syncthreads();
+    for (int t = wave; t < FM * FN * 4; t += W) {
+        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3;
+        v4f s = reinterpret_cast<const v4f*>(lds)[t * 64 + lane];
+#pragma unroll
+        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[t * 64 + lane];
+        store_y(p, m0 + a * 32 + r32, n0 + b * 32 + 8 * i + 4 * h, s);
+    }
+}
+
 template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t tile_go(const F8MmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128;
+    const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128 + (BM == 256 && BN == 256 ? 1024 : 0);
     auto fn = &f8mm_tile_kernel<BM, BN, WR, WC, XF, EXACT>;
     if (bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -466,12 +454,15 @@ template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t 
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(WR * WC * 64), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int XF> static hipError_t large_go(const F8MmParams& p, hipStream_t st)
+template <int FM, int FN, int XF, bool EXACT> static hipError_t split_go(const F8MmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + 255) / 256, tn = (p.N + 255) / 256, bytes = 2 * 512 * 128;
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&f8mm_large_kernel<XF>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(f8mm_large_kernel<XF>, dim3((unsigned)(tm * tn)), dim3(256), bytes, st, p, tm, tn, 8);
+    const int tm = (p.M + 32 * FM - 1) / (32 * FM), tn = (p.N + 32 * FN - 1) / (32 * FN), bytes = 8 * 32 * (FM + FN) * 128;
+    auto fn = &f8mm_split_kernel<FM, FN, XF, EXACT>;
+    if (bytes > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(512), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
 template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t rows_go(const F8MmParams& p, hipStream_t st)
@@ -480,14 +471,31 @@ template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t ro
     hipLaunchKernelGGL((f8mm_rows_kernel<FM, FN, U, W, XF, EXACT>), dim3((unsigned)(tm * tn)), dim3(W * 64), 0, st, p, tm, tn, 8);
     return hipGetLastError();
 }
+// The kernel that is expected to take least, from how many workgroups a compute unit gets.  Microseconds at K = 4096 on 256 compute units,
+// bf16 results: by c workgroups each, the narrow tiles take 4 c + 2 (32 x 32), 6.5 c + 1.5 (32 x 64), 9.3 c + 1 (64 x 64); tiles of 64 x 128 22 for
+// one and 14.2 c for more, of 128 x 128 30 for one and 41 for every two, of 256 x 256 66 c.  Where the choice falls wrong it costs little: measured,
+// the best and the next at 300 x 4096 x 4096: 19.0 and 20.1 us; 1024 x 4096 x 4096: 27.2 (64 x 128) and 30.5 (128 x 128); 777 x 5000 x 3000: 30.7
+// (128 x 128) and 34.7; 1024 x 11008 x 4096: 66 (256 x 256) and 76 (64 x 128).  Up to eight rows operands go straight to
+// registers, four steps in flight: 9.8 us for one row through 4096 x 11008, 10.6 by 32 x 32 tiles; sixteen rows 12.7 and 11.1.
 template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int n_cu, hipStream_t st)
 {
-    auto tiles = [&](int bm, int bn) { return (long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn); };
-    if (p.M <= 16) return rows_go<1, 1, 4, 16, XF, EXACT>(p, st);
-    if (p.M <= 32) return rows_go<2, 2, 2, 8, XF, EXACT>(p, st);
-    if (p.M <= 64 || tiles(64, 64) <= n_cu) return rows_go<4, 4, 1, 8, XF, EXACT>(p, st);
-    if (!EXACT && tiles(256, 256) >= n_cu) return large_go<XF>(p, st);
-    return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
+    if (p.M <= 8) return rows_go<1, 1, 4, 8, XF, EXACT>(p, st);
+    auto each = [&](int bm, int bn) { return (float)(((long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) + n_cu - 1) / n_cu); };
+    const float c11 = each(32, 32), c12 = each(32, 64), c22 = each(64, 64), c24 = each(64, 128), c44 = each(128, 128), c88 = each(256, 256);
+    const float cost[6] = {4.0f * c11 + 2.0f, 6.5f * c12 + 1.5f, 9.3f * c22 + 1.0f, c24 <= 1.0f ? 22.0f : 14.2f * c24, c44 <= 1.0f ? 30.0f : 20.5f * (c44 + (float)((long long)c44 & 1)),
+                           EXACT ? 3.4e38f : 66.0f * c88};
+    int best = 0;
+    for (int i = 1; i < 6; ++i) best = cost[i] < cost[best] ? i : best;
+    switch (best) {
+    case 0: return split_go<1, 1, XF, EXACT>(p, st);
+    case 1: return split_go<1, 2, XF, EXACT>(p, st);
+    case 2: return split_go<2, 2, XF, EXACT>(p, st);
+    case 3: return tile_go<64, 128, 2, 2, XF, EXACT>(p, st);
+    case 4: return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
+    default:
+        if constexpr (EXACT) return hipErrorInvalidValue;
+        else return tile_go<256, 256, 2, 4, XF, EXACT>(p, st);
+    }
 }
 
 }  // namespace sopk

@@ -290,23 +290,23 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
                         v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
 }
 
-// ---- large products of 4-bit codes: 256 x 256 of y by four wavefronts, one on a SIMD, each 128 x 128 of it; 64 elements along K a step,
-// two steps in LDS.  While sixteen elements are multiplied (sixteen matrix instructions), the next sixteen's operands are read, and between
-// two barriers (64 matrix instructions) every thread forms 64 weights of the step after the next, eight by eight: behind each matrix
+// ---- large products of 4-bit codes: 256 x 64 F of y (F = 4 or 3) by four wavefronts, one on a SIMD, each 128 x 32 F of it; 64 elements along
+// K a step, two steps in LDS.  While sixteen elements are multiplied (4 F matrix instructions), the next sixteen's operands are read, and
+// between two barriers (16 F matrix instructions) every thread forms 16 F weights of the step after the next, eight by eight: behind each matrix
 // instruction stand a part of the look-ups and of the scale word of an eight, and a part of the products of the eight before.  A matrix
 // instruction (32 cycles) hides seven others of its wavefront, so what a weight costs in instructions is what counts: two codes (a byte of
 // the payload) are looked up at once, in a table of the 256 pairs of either codebook.  Halfway through a step comes its barrier: the
 // next step is there, this one's place is free.
-template <bool G8>
+template <int F, bool G8>
 __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
-    constexpr int BM = 256, BN = 256, STAGE = (BM + BN) * 128, TAB = 4096, WORDS = G8 ? 2 : 1;
+    constexpr int BM = 256, BN = 64 * F, SLOTS = 4 * F, STAGE = (BM + BN) * 128, TAB = 4096, WORDS = G8 ? 2 : 1;
     constexpr unsigned int NOWHERE = 0xE0000000u;                       // an offset beyond every window
     extern __shared__ __align__(4096) unsigned char lds[];
     int tm, tn;
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
     const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 1 << 7, wn = (wave & 1) << 7, lg = 31 - __builtin_clz(p.g), steps = (p.K + 63) >> 6;
+    const int wm = wave >> 1 << 7, wn = (wave & 1) * (32 * F), lg = 31 - __builtin_clz(p.g), steps = (p.K + 63) >> 6;
     const unsigned int tab0 = lds_address(lds), lds0 = tab0 + TAB;
 #pragma unroll
     for (int b = 0; b < 2; ++b) *reinterpret_cast<float2*>(lds + b * 2048 + tid * 8) = make_float2(p.tab[b][tid & 15], p.tab[b][tid >> 4]);
@@ -318,13 +318,13 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     for (int i = 0; i < 8; ++i) ox[i] = (unsigned int)min(i * 32 + (tid >> 3), p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + xcol;
     const Window xw = window(p.x + (long long)m0 * p.ldx, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)(p.ldx * 2) + (unsigned int)p.K * 2);
     auto load_x = [&](int t, int i) { load_to_lds(xw, ox[i], t * 128, lds0 + (t & 1) * STAGE + (wave << 10) + i * 4096); };
-    // w: an item is sixteen codes of a row, four items a row and step, four of a thread
+    // w: an item is sixteen codes of a row, four items a row and step, F of a thread
     const int rows = min(BN, p.N - n0), k16 = (tid & 3) * 16;
     const unsigned int prow = (unsigned int)(p.K >> 1), wrow = (unsigned int)(p.K >> lg) * 2u;
     const Window pw = window(p.payload + (long long)n0 * prow, (unsigned int)rows * prow), ww = window(p.words + (long long)n0 * (p.K >> lg), (unsigned int)rows * wrow);
-    unsigned int op[4], ow[4][WORDS];
+    unsigned int op[F], ow[F][WORDS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < F; ++i) {
         const unsigned int r = (unsigned int)min(i * 64 + (tid >> 2), rows - 1);
         op[i] = r * prow + (unsigned int)(k16 >> 1);
 #pragma unroll
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     auto end_w = [&](int t) {
         if (odd && t == steps - 1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < F; ++i)
 #pragma unroll
                 for (int h = 0; h < WORDS; ++h) ow[i][h] = t * 64 + k16 + 8 * h < p.K ? ow[i][h] : NOWHERE;
         }
@@ -354,11 +354,11 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
         for (int h = 0; h < WORDS; ++h) z.w[h] = __builtin_amdgcn_raw_buffer_load_b16(resource(ww), (int)ow[i][h], t * (128 >> lg), 0);
     };
 
-    v16f acc[4][4];
+    v16f acc[4][F];
 #pragma unroll
     for (int a = 0; a < 4; ++a)
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < F; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
 
@@ -397,22 +397,22 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     unsigned int at[4];                                                 // the s-th sixteen elements of this lane's row, without the row
 #pragma unroll
     for (int s = 0; s < 4; ++s) at[s] = lds0 + (unsigned int)r32 * 128 + ((unsigned int)(((lane >> 5) ^ (r32 >> 1 & 7)) << 4) ^ (unsigned int)(s << 5));
-    v4i fx[2][4], fw[2][4];
+    v4i fx[2][4], fw[2][F];
     unsigned int rx = 0, rw = 0;
     auto from = [&](unsigned int stage, int s) { rx = at[s] + (stage + wm * 128); rw = at[s] + (stage + (BM + wn) * 128); };
-    auto read = [&](int s, int i) {                                     // the i-th of eight reads
-        if (i < 4) fw[s & 1][i] = *(ldsi)(uintptr_t)(rw + i * 4096);
-        else fx[s & 1][i - 4] = *(ldsi)(uintptr_t)(rx + (i - 4) * 4096);
+    auto read = [&](int s, int i) {                                     // the i-th of F + 4 reads
+        if (i < F) fw[s & 1][i] = *(ldsi)(uintptr_t)(rw + i * 4096);
+        else if (i < F + 4) fx[s & 1][i - F] = *(ldsi)(uintptr_t)(rx + (i - F) * 4096);
     };
     auto multiply = [&](int s, int i) {
-        const int a = i >> 2, b = i & 3;
+        const int a = i / F, b = i % F;
         acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, fw[s & 1][b]), __builtin_bit_cast(v8bf, fx[s & 1][a]), acc[a][b], 0, 0, 0);
     };
 
-    Item now[4], next[4];
-    auto settle = [&](Item (&z)[4]) {                                   // what has arrived is used as such (and not waited for again behind later loads)
+    Item now[F], next[F];
+    auto settle = [&](Item (&z)[F]) {                                   // what has arrived is used as such (and not waited for again behind later loads)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < F; ++i) {
             asm volatile("" : "+v"(z[i].c[0]), "+v"(z[i].c[1]), "+v"(z[i].w[0]));
             if (G8) asm volatile("" : "+v"(z[i].w[WORDS - 1]));
         }
@@ -426,27 +426,35 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     }
     end_w(0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_w(next[i], 0, i);
+    for (int i = 0; i < F; ++i) load_w(next[i], 0, i);
     end_w(1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_w(now[i], 1, i);
+    for (int i = 0; i < F; ++i) load_w(now[i], 1, i);
     putting[0] = put[0]; putting[1] = put[1];
+    // A quarter of a step's work is F / 2 eights; with F = 3 the second of them is looked up, and half formed.
+    constexpr int PART = 4 * F;
 #pragma unroll
-    for (int g = 0; g < 10; ++g) {
-        if (g == 8) { putting[0] += STAGE; putting[1] += STAGE; }
+    for (int g = 0; g < 2 * F; ++g) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) look_up(g < 8 ? next[g >> 1] : now[0], g & 1, 0, e);
+        for (int e = 0; e < 8; ++e) look_up(next[g >> 1], g & 1, g & 1, e);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) form(g >> 1 & 3, g & 1, 0, e);
+        for (int e = 0; e < 8; ++e) form(g >> 1, g & 1, g & 1, e);
     }
+    putting[0] += STAGE; putting[1] += STAGE;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) look_up(now[1], 0, 0, e);
+    for (int e = 0; e < 8; ++e) look_up(now[0], 0, 0, e);
+#pragma unroll
+    for (int f = 0; f < PART; ++f) {
+        const int g = f >> 3, e = f & 7;
+        form(g >> 1, g & 1, g & 1, e);
+        look_up(now[(g + 1) >> 1], (g + 1) & 1, (g + 1) & 1, e);
+    }
     wait_loads();
     __syncthreads();
     settle(now);
     from(0, 0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) read(0, i);
+    for (int i = 0; i < F + 4; ++i) read(0, i);
     for (int t = 0; t < steps; ++t) {
         const unsigned int here = (t & 1) * STAGE, there = STAGE - here;
         // sixteen elements of K, and a quarter of the work between two barriers: behind a step's last sixteen elements the first quarter of the
@@ -460,16 +468,17 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
                 putting[0] = put[0] + here; putting[1] = put[1] + here;
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < SLOTS; ++i) {
                 multiply(s, i);
-                if ((i & 1) == 0) read((s + 1) & 3, i >> 1);
-                const int g = Q * 2 + (i >> 3), e = i & 7;              // the eight whose products are formed; the one after it is looked up
+                if (F == 4 ? (i & 1) == 0 : i < F + 4) read((s + 1) & 3, F == 4 ? i >> 1 : i);
+                const int f = Q * SLOTS + i, g = f >> 3, e = f & 7;     // the eight whose products are formed; the one after it is looked up
                 form(g >> 1, g & 1, g & 1, e);
-                if (s == 2 && i == 8) { wait_loads(); settle(next); }
-                if (g < 7) look_up(now[(g + 1) >> 1], (g + 1) & 1, (g + 1) & 1, e);
+                if (f == 4 * SLOTS - 8) { wait_loads(); settle(next); }
+                if (g < 2 * F - 1) look_up(now[(g + 1) >> 1], (g + 1) & 1, (g + 1) & 1, e);
                 else look_up(next[0], 0, 0, e);
-                if (s == 3 && (i & 1)) load_x(t + 2, i >> 1);
-                if (Q >= 1 && Q < 3 && (i & 7) == 3) load_w(next[(Q - 1) * 2 + (i >> 3)], t + 2, (Q - 1) * 2 + (i >> 3));
+                if (s == 3 && i * 8 / SLOTS != (i + 1) * 8 / SLOTS) load_x(t + 2, i * 8 / SLOTS);
+                if (s < 2 && i % 8 == 3) { if (s * (SLOTS / 8) + i / 8 < F) load_w(next[s * (SLOTS / 8) + i / 8], t + 2, s * (SLOTS / 8) + i / 8); }
+                if constexpr (F == 3 && s == 1) if (i == 8) load_w(next[2], t + 2, 2);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -480,14 +489,14 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < 4; ++i) now[i] = next[i];
+        for (int i = 0; i < F; ++i) now[i] = next[i];
         part(std::integral_constant<int, 3>{});
     }
     wait_loads();
 #pragma unroll
     for (int a = 0; a < 4; ++a)
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < F; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * (lane >> 5),
@@ -510,14 +519,25 @@ template <int NB, int BM, int BN, int WR, int WC> static hipError_t tile_go(cons
     hipLaunchKernelGGL((packed_tile_kernel<NB, BM, BN, WR, WC>), dim3((unsigned)(tm * tn)), dim3(WR * WC * 64), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-static hipError_t large_go(const PackedMmParams& p, hipStream_t st)
+template <int F> static hipError_t large_go(const PackedMmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + 255) / 256, tn = (p.N + 255) / 256, bytes = 4096 + 2 * 512 * 128;
-    auto fn = p.g == 8 ? &packed_large_kernel<true> : &packed_large_kernel<false>;
+    const int tm = (p.M + 255) / 256, tn = (p.N + 64 * F - 1) / (64 * F), bytes = 4096 + 2 * (256 + 64 * F) * 128;
+    auto fn = p.g == 8 ? &packed_large_kernel<F, true> : &packed_large_kernel<F, false>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(256), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
+}
+// One workgroup a compute unit: the width whose last round is filled better.  A tile of 192 columns forms and reads more for a product: 2048 x
+// 11008 x 4096 takes 242 us by it (464 tiles, two rounds) and 256 us by the wider (344 tiles, two rounds), 4096 x 4096 x 4096 208 us (352
+// tiles, two rounds) and 145 us (256 tiles, one).
+static hipError_t large_pick(const PackedMmParams& p, int n_cu, hipStream_t st)
+{
+    auto cost = [&](int f, int each) {
+        const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 64 * f - 1) / (64 * f));
+        return (tiles + n_cu - 1) / n_cu * f * each;
+    };
+    return cost(4, 20) <= cost(3, 25) ? large_go<4>(p, st) : large_go<3>(p, st);
 }
 template <int NB> static hipError_t packed_pick(const PackedMmParams& p, int n_cu, hipStream_t st)
 {
@@ -525,7 +545,7 @@ template <int NB> static hipError_t packed_pick(const PackedMmParams& p, int n_c
     if (p.M <= 16) return rows_go<NB, 1, 3, 16>(p, st);
     if (p.M <= 32) return rows_go<NB, 2, 2, 8>(p, st);
     if (tiles(256, 256) >= n_cu) {
-        if constexpr (NB == 4) return large_go(p, st);
+        if constexpr (NB == 4) return large_pick(p, n_cu, st);
         else return tile_go<NB, 256, 256, 2, 4>(p, st);
     }
     if (tiles(128, 128) >= n_cu) return tile_go<NB, 128, 128, 2, 2>(p, st);

@@ -491,3 +491,9 @@ def test_refusals():
     refused(4, cx.packed_matmul, x.bfloat16(), sop.PackedWeights(words, payload, 140, 256, 16, 4, sop.fmt_by_name("UE4M4"), [tab, tab]))
     refused(4, cx.packed_matmul, x.bfloat16(), sop.PackedWeights(words, payload, 140, 256, 16, 4, fmt, [tab], k=65))
     refused(3, cx.packed_matmul, x.bfloat16(), sop.PackedWeights(words, payload, 140, 256, 16, 4, fmt, [np.zeros(65, np.float32)]))
+
+
+@pytest.mark.parametrize("case", [(4100, 4200, 136, 8, 4, (0, 4, 3, 8), True, 1), (2100, 11000, 208, 16, 4, (1, 5, 5, 12), True, 0), (4097, 8200, 64, 32, 4, (0, 4, 4, 8), False, 0),
+                                  (8200, 2049, 320, 64, 4, (0, 4, 3, 8), True, 2)])
+def test_packed_product_of_large_layers(case):
+    test_packed_product(case)
