@@ -128,27 +128,8 @@ __device__ __forceinline__ void bf16_step(const unsigned char* ta, const unsigne
         }
     }
 }
-// The same by 32 x 32 squares, tiles whose chunk c of row r stands at position c ^ (r >> 1 & 7): LDS serves a 16-byte read sixteen lanes
-// at a time (0-3, 12-15, 20-23 and 24-27, then the others of the first 32, ...), whose rows so fall on different banks.  ra, rb: byte
-// offset of this lane's row (lane & 31) of the wavefront's first square, h = lane >> 5.  acc[a][b][i] holds row 8 (i / 4) + 4 h + i % 4 of b's square, column lane & 31 of a's.
-__device__ __forceinline__ v8bf square_frag(const unsigned char* tile, unsigned int row, unsigned int z, int f, int s)
-{
-    return *reinterpret_cast<const v8bf*>(tile + (row + (((unsigned int)(2 * s) << 4) ^ z)) + f * 4096);
-}
-template <int FA, int FB>
-__device__ __forceinline__ void bf16_squares(const unsigned char* ta, const unsigned char* tb, unsigned int ra, unsigned int rb, int lane, int s, v16f (&acc)[FA][FB])
-{
-    const unsigned int z = (unsigned int)((lane >> 5) ^ (lane >> 1 & 7)) << 4;   // chunk 2 s + h
-    v8bf fb[FB];
-#pragma unroll
-    for (int b = 0; b < FB; ++b) fb[b] = square_frag(tb, rb, z, b, s);
-#pragma unroll
-    for (int a = 0; a < FA; ++a) {
-        const v8bf fa = square_frag(ta, ra, z, a, s);
-#pragma unroll
-        for (int b = 0; b < FB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[b], fa, acc[a][b], 0, 0, 0);
-    }
-}
+// Operands read 16 bytes a lane for 32 x 32 squares: chunk c of a 128-byte row r stands at position c ^ (r >> 1 & 7).  LDS serves such a read
+// sixteen lanes at a time (0-3, 12-15, 20-23 and 24-27, then the others of the first 32, ...), whose rows so fall on different banks.
 // zeroes the bytes of a 16-byte chunk beyond the first `n`
 __device__ __forceinline__ v4i keep_bytes(v4i v, int n)
 {

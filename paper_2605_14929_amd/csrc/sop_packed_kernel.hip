@@ -182,70 +182,56 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
     }
 }
 
-// ---- tiles: BM x BN of y, 64 elements along K a step, two steps in LDS.  The weights are formed once a tile, on their way into LDS.
-template <int NB, int BM, int BN, int WR, int WC>
-__global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
+// ---- narrow tiles, K dealt out: 32 FM x 32 FN of y a workgroup, its eight wavefronts taking steps of 64 S elements in turn.  A wavefront has its
+// step of x in a place of its own in LDS (no barrier before the sums are joined), and forms the weights in the registers that the matrix
+// instructions read: a lane takes 32 neighbouring codes of its row, eight for each of four instructions, and the same elements of x.  The next
+// step is asked for when this one's operands have been read.
+template <int NB, int FM, int FN, int S, int WPL>
+__global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
-    constexpr int NT = WR * WC * 64, FM = BM / WR / 32, FN = BN / WC / 32, CX = BM * 8 / NT, IW = BN * 4 / NT, STAGE = (BM + BN) * 128;
-    static_assert(IW * NT == BN * 4 && CX * NT == BM * 8 && FM * WR * 32 == BM && FN * WC * 32 == BN, "whole items and squares");
+    constexpr int W = 8, OWN = (S > FN ? S : FN) * FM * 4096;
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ float tab[2 << NB];
+    __shared__ __align__(16) float tab[2 << NB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, h = lane >> 5, lg = 31 - __builtin_clz(p.g);
     int tm, tn;
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
-    const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / WC * (BM / WR), wn = wave % WC * (BN / WC), lg = 31 - __builtin_clz(p.g);
-    put_codebooks<NB>(p, tab, tid);
-    const uint16_t* xb = p.x + (long long)m0 * p.ldx;
-    unsigned int ox[CX];                                                // (a row of x has at most 2^22 elements: the entry point's check)
+    const int m0 = tm * (32 * FM), n0 = tn * (32 * FN), whole = p.K / (64 * S);
+    unsigned char* own = lds + wave * OWN;
+    const unsigned int own0 = lds_address(own);
+    const Window xw = window(p.x + (long long)m0 * p.ldx, ((unsigned int)(min(32 * FM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)p.K) * 2);
+    unsigned int off[4 * FM];                                           // rows beyond the matrix read its last
 #pragma unroll
-    for (int i = 0; i < CX; ++i) {
-        const int c = i * NT + tid, r = c >> 3;
-        ox[i] = (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + (((c ^ r >> 1) & 7) << 4);
+    for (int i = 0; i < 4 * FM; ++i) off[i] = (unsigned int)min(i * 8 + (lane >> 3), p.M - 1 - m0) * (unsigned int)p.ldx * 2 + (((lane ^ (i * 8 + (lane >> 3)) >> 1) & 7) << 4);
+    const unsigned char* pay[FN];
+    const uint16_t* words[FN];
+#pragma unroll
+    for (int b = 0; b < FN; ++b) {
+        const long long n = min(n0 + b * 32 + r32, p.N - 1);
+        pay[b] = p.payload + n * (p.K / 8) * NB;
+        words[b] = p.words + n * (p.K >> lg);
     }
-    const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)(p.ldx * 2) + (unsigned int)p.K * 2);
-    auto load_x = [&](int t) {
-        unsigned char* to = lds + (t & 1) * STAGE;
-        if (t * 64 + 64 <= p.K) {
-            const unsigned int at = lds_address(to) + (wave << 10);
+    struct Part { unsigned int c[NB], w[WPL == 4 ? 2 : 1]; };
+    Part z[S][FN];
+    auto load = [&](int t) {
 #pragma unroll
-            for (int i = 0; i < CX; ++i) load_to_lds(xw, ox[i], t * 128, at + i * NT * 16);
-        } else {                                                        // (K is a multiple of eight: whole chunks)
-            const int left = (p.K - t * 64) * 2;
-#pragma unroll 1
-            for (int c = tid; c < BM * 8; c += NT) {
-                const int r = c >> 3, col = ((c ^ r >> 1) & 7) << 4;
-                v4i v = {0, 0, 0, 0};
-                if (col < left) v = *reinterpret_cast<const v4i*>(xb + (long long)min(r, p.M - 1 - m0) * p.ldx + t * 64 + (col >> 1));
-                *reinterpret_cast<v4i*>(to + c * 16) = v;
+        for (int s = 0; s < S; ++s) {
+            const int k = (t * S + s) * 64 + h * 32;
+#pragma unroll
+            for (int b = 0; b < FN; ++b) {
+                const Words<NB> c = *reinterpret_cast<const Words<NB>*>(pay[b] + (k >> 3) * NB);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) z[s][b].c[i] = c.v[i];
+                const uint16_t* w = words[b] + (k >> lg);
+                if (WPL == 1) z[s][b].w[0] = w[0];
+                else {
+                    const Words<WPL == 4 ? 2 : 1> v = *reinterpret_cast<const Words<WPL == 4 ? 2 : 1>*>(w);
+#pragma unroll
+                    for (int i = 0; i < (WPL == 4 ? 2 : 1); ++i) z[s][b].w[i] = v.v[i];
+                }
             }
+#pragma unroll
+            for (int i = 0; i < 4 * FM; ++i) load_to_lds(xw, off[i], (t * S + s) * 128, own0 + (s * 4 * FM + i) * 1024);
         }
-    };
-    // an item: sixteen codes of a row, four items a row and step
-    const unsigned char* pay[IW];
-    const uint16_t* words[IW];
-    const int k16 = (tid & 3) * 16;
-#pragma unroll
-    for (int i = 0; i < IW; ++i) {
-        const long long n = min(n0 + ((i * NT + tid) >> 2), p.N - 1);
-        pay[i] = p.payload + n * (p.K >> 3) * NB;
-        words[i] = p.words + n * (p.K >> lg);
-    }
-    struct Share { Codes c[IW][2]; unsigned int w[IW][2]; };            // what a thread forms weights of, a step
-    auto load_w = [&](int t, Share& z) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k = min(t * 64 + k16 + 8 * h, p.K - 8);
-#pragma unroll
-            for (int i = 0; i < IW; ++i) {
-                z.c[i][h] = eight_codes<NB>(pay[i] + (k >> 3) * NB);
-                z.w[i][h] = words[i][k >> lg];
-            }
-        }
-    };
-    auto store_w = [&](int t, const Share& z, int i, int h) {           // eight weights: item i, half h
-        const int r = (i * NT + tid) >> 2;
-        const v4i u = eight_weights<NB>(z.c[i][h], tab, word_table<NB>(p, z.w[i][h]), word_scale(p, z.w[i][h]));
-        *reinterpret_cast<v4i*>(lds + (t & 1) * STAGE + BM * 128 + r * 128 + ((((tid & 3) * 2 + h) ^ (r >> 1 & 7)) << 4)) = only_if(t * 64 + k16 + 8 * h < p.K, u);
     };
     v16f acc[FM][FN];
 #pragma unroll
@@ -254,88 +240,142 @@ __global__ __launch_bounds__(WR * WC * 64) void packed_tile_kernel(const PackedM
         for (int b = 0; b < FN; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
-    const int steps = (p.K + 63) >> 6;
-    const unsigned int row_x = (unsigned int)(wm + (lane & 31)) * 128, row_w = (unsigned int)(wn + (lane & 31)) * 128;
-    Share now, next;
-    load_w(0, now);
-    load_w(1, next);
-    load_x(0);
-    __syncthreads();                                                    // the codebooks are there
+    put_codebooks<NB>(p, tab, tid);
+    __syncthreads();
+    if (wave < whole) load(wave);
+    for (int t = wave; t < whole; t += W) {
+        Part c[S][FN];
+        v4i x[S][FM][4];
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < 2 * IW; ++i) store_w(0, now, i >> 1, i & 1);
-    for (int t = 0; t < steps; ++t) {
-        wait_loads();
-        __syncthreads();
-        const bool more = t + 1 < steps;
-        now = next;
-        if (more) { load_w(t + 2, next); load_x(t + 1); }               // (codes are asked for two steps ahead, so that they are there when their turn comes)
-        const unsigned char* half = lds + (t & 1) * STAGE;
-        // sixteen elements of K are multiplied, then a part of the next step's weights is formed: of the two wavefronts on a SIMD one forms
-        // weights while the other one's matrix instructions run
+        for (int s = 0; s < S; ++s) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            bf16_squares<FM, FN>(half, half + BM * 128, row_x, row_w, lane, s, acc);
-            if (more)
+            for (int b = 0; b < FN; ++b) {
+                c[s][b] = z[s][b];
 #pragma unroll
-                for (int i = s * IW / 2; i < (s + 1) * IW / 2; ++i) store_w(t + 1, now, i >> 1, i & 1);
+                for (int i = 0; i < NB; ++i) asm volatile("" : "+v"(c[s][b].c[i]));
+#pragma unroll
+                for (int i = 0; i < (WPL == 4 ? 2 : 1); ++i) asm volatile("" : "+v"(c[s][b].w[i]));
+            }
+#pragma unroll
+            for (int a = 0; a < FM; ++a)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[s][a][j] = *reinterpret_cast<const v4i*>(own + ((s * FM + a) * 32 + r32) * 128 + (((4 * h + j) ^ (r32 >> 1 & 7)) << 4));
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // (the reads have ended: the place is free)
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + W < whole) load(t + W);
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int b = 0; b < FN; ++b) {
+                float sc[WPL];
+                unsigned int book[WPL];
+#pragma unroll
+                for (int i = 0; i < WPL; ++i) {
+                    const unsigned int w = c[s][b].w[i >> 1] >> (16 * (i & 1)) & 0xFFFFu;
+                    sc[i] = word_scale(p, w);
+                    book[i] = word_table<NB>(p, w);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const v4i u = eight_weights<NB>(eight_of<NB>(c[s][b].c, j), tab, book[j * WPL / 4], sc[j * WPL / 4]);
+#pragma unroll
+                    for (int a = 0; a < FM; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, u), __builtin_bit_cast(v8bf, x[s][a][j]), acc[a][b], 0, 0, 0);
+                }
+            }
+    }
+#pragma unroll 1
+    for (int k0 = whole * 64 * S + wave * 16; k0 < p.K; k0 += W * 16) {  // what is left of K, sixteen elements a wavefront
+        const int k = k0 + 8 * h;
+        const bool in = k < p.K;
+        const int ks = in ? k : p.K - 8;
+        v4i u[FN];
+#pragma unroll
+        for (int b = 0; b < FN; ++b) {
+            const unsigned int w = words[b][ks >> lg];
+            u[b] = only_if(in, eight_weights<NB>(eight_codes<NB>(pay[b] + (ks >> 3) * NB), tab, word_table<NB>(p, w), word_scale(p, w)));
+        }
+#pragma unroll
+        for (int a = 0; a < FM; ++a) {
+            const v4i v = only_if(in, *reinterpret_cast<const v4i*>(p.x + (long long)min(m0 + a * 32 + r32, p.M - 1) * p.ldx + ks));
+#pragma unroll
+            for (int b = 0; b < FN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, u[b]), __builtin_bit_cast(v8bf, v), acc[a][b], 0, 0, 0);
         }
     }
+    wait_loads();
+    __syncthreads();
+    v4f* part = reinterpret_cast<v4f*>(own);                            // [square][quarter][lane], this wavefront's
 #pragma unroll
     for (int a = 0; a < FM; ++a)
 #pragma unroll
         for (int b = 0; b < FN; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                store_y(p, m0 + wm + a * 32 + (lane & 31), n0 + wn + b * 32 + 8 * i + 4 * (lane >> 5),
-                        v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+                part[((a * FN + b) * 4 + i) * 64 + lane] = v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]};
+    __syncthreads();
+    for (int t = wave; t < FM * FN * 4; t += W) {
+        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3;
+        v4f s = reinterpret_cast<const v4f*>(lds)[t * 64 + lane];
+#pragma unroll
+        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[t * 64 + lane];
+        store_y(p, m0 + a * 32 + r32, n0 + b * 32 + 8 * i + 4 * h, s);
+    }
 }
 
-// ---- large products of 4-bit codes: 256 x 64 F of y (F = 4 or 3) by four wavefronts, one on a SIMD, each 128 x 32 F of it; 64 elements along
-// K a step, two steps in LDS.  While sixteen elements are multiplied (4 F matrix instructions), the next sixteen's operands are read, and
-// between two barriers (16 F matrix instructions) every thread forms 16 F weights of the step after the next, eight by eight: behind each matrix
+// ---- wide tiles: 64 E x 64 F of y (4 x 4, 4 x 3, 2 x 2) by four wavefronts, each 32 E x 32 F of it; 64 elements along K a step,
+// two steps in LDS.  While sixteen elements are multiplied (E F matrix instructions), the next sixteen's operands are read, and between
+// two barriers (4 E F matrix instructions) every thread forms 16 F weights of the step after the next, eight by eight: behind each matrix
 // instruction stand a part of the look-ups and of the scale word of an eight, and a part of the products of the eight before.  A matrix
-// instruction (32 cycles) hides seven others of its wavefront, so what a weight costs in instructions is what counts: two codes (a byte of
-// the payload) are looked up at once, in a table of the 256 pairs of either codebook.  Halfway through a step comes its barrier: the
+// instruction (32 cycles) hides seven others of its wavefront, so what a weight costs in instructions is what counts: two codes
+// are looked up at once, in a table of the 4^NB pairs of either codebook.  Before its last sixteen elements through a step comes its barrier: the
 // next step is there, this one's place is free.
-template <int F, bool G8>
-__global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
+template <int NB, int E, int F, bool G8>
+__global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
-    constexpr int BM = 256, BN = 64 * F, SLOTS = 4 * F, STAGE = (BM + BN) * 128, TAB = 4096, WORDS = G8 ? 2 : 1;
+    constexpr int BM = 64 * E, BN = 64 * F, SLOTS = E * F, EACH = 4 / E, XL = 2 * E, STAGE = (BM + BN) * 128, BOOK = 8 << 2 * NB, TAB = 2 * BOOK, CW = (NB + 1) / 2, WORDS = G8 ? 2 : 1;
     constexpr unsigned int NOWHERE = 0xE0000000u;                       // an offset beyond every window
-    extern __shared__ __align__(4096) unsigned char lds[];
+    extern __shared__ __align__(TAB) unsigned char lds[];
     int tm, tn;
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
     const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 1 << 7, wn = (wave & 1) * (32 * F), lg = 31 - __builtin_clz(p.g), steps = (p.K + 63) >> 6;
+    const int wm = (wave >> 1) * (32 * E), wn = (wave & 1) * (32 * F), lg = 31 - __builtin_clz(p.g), steps = (p.K + 63) >> 6;
     const unsigned int tab0 = lds_address(lds), lds0 = tab0 + TAB;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) *reinterpret_cast<float2*>(lds + b * 2048 + tid * 8) = make_float2(p.tab[b][tid & 15], p.tab[b][tid >> 4]);
+    for (int i = tid; i < 2 << 2 * NB; i += 256) {
+        const float* book = p.tab[i >> 2 * NB];
+        *reinterpret_cast<float2*>(lds + i * 8) = make_float2(book[i & ((1 << NB) - 1)], book[i >> NB & ((1 << NB) - 1)]);
+    }
 
     // x: chunks of 16 bytes straight into LDS
     const unsigned int xcol = (unsigned int)((tid ^ tid >> 4) & 7) << 4;   // (rows 32 apart lie alike)
-    unsigned int ox[8];
+    unsigned int ox[XL];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ox[i] = (unsigned int)min(i * 32 + (tid >> 3), p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + xcol;
+    for (int i = 0; i < XL; ++i) ox[i] = (unsigned int)min(i * 32 + (tid >> 3), p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + xcol;
     const Window xw = window(p.x + (long long)m0 * p.ldx, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)(p.ldx * 2) + (unsigned int)p.K * 2);
     auto load_x = [&](int t, int i) { load_to_lds(xw, ox[i], t * 128, lds0 + (t & 1) * STAGE + (wave << 10) + i * 4096); };
     // w: an item is sixteen codes of a row, four items a row and step, F of a thread
     const int rows = min(BN, p.N - n0), k16 = (tid & 3) * 16;
-    const unsigned int prow = (unsigned int)(p.K >> 1), wrow = (unsigned int)(p.K >> lg) * 2u;
+    const unsigned int prow = (unsigned int)(p.K >> 3) * NB, wrow = (unsigned int)(p.K >> lg) * 2u;
     const Window pw = window(p.payload + (long long)n0 * prow, (unsigned int)rows * prow), ww = window(p.words + (long long)n0 * (p.K >> lg), (unsigned int)rows * wrow);
     unsigned int op[F], ow[F][WORDS];
 #pragma unroll
     for (int i = 0; i < F; ++i) {
         const unsigned int r = (unsigned int)min(i * 64 + (tid >> 2), rows - 1);
-        op[i] = r * prow + (unsigned int)(k16 >> 1);
+        op[i] = r * prow + (unsigned int)(k16 >> 3) * NB;
 #pragma unroll
         for (int h = 0; h < WORDS; ++h) ow[i][h] = r * wrow + (unsigned int)((k16 >> lg) + h) * 2u;
     }
+    unsigned int put[2], putting[2] = {0, 0};                           // where this thread's weights go (rows 64 apart lie alike)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) put[h] = lds0 + BM * 128 + (unsigned int)(tid >> 2) * 128 + (unsigned int)((((tid & 3) * 2 + h) ^ (tid >> 3 & 7)) << 4);
     // Elements of the last step beyond K: x is asked for nowhere, and zeros arrive; so are the scale words, whose scale is 0.
-    const bool odd = (p.K & 63) != 0;
+    // Where K ends in the middle of an item (g = 8 alone), no byte beyond its codes is read: the last step's items are asked for one eight earlier,
+    // this one's too, which has its eight in its second half then; the others' places are moved back by as much.
+    const bool odd = (p.K & 63) != 0, half = G8 && (p.K & 15) != 0;
     auto end_x = [&](int t) {
         if (odd && t == steps - 1) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ox[i] = t * 128 + (int)xcol < p.K * 2 ? ox[i] : NOWHERE;
+            for (int i = 0; i < XL; ++i) ox[i] = t * 128 + (int)xcol < p.K * 2 ? ox[i] : NOWHERE;
         }
     };
     auto end_w = [&](int t) {
@@ -344,19 +384,40 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
             for (int i = 0; i < F; ++i)
 #pragma unroll
                 for (int h = 0; h < WORDS; ++h) ow[i][h] = t * 64 + k16 + 8 * h < p.K ? ow[i][h] : NOWHERE;
+            if (half) {
+                const bool mine = t * 64 + k16 + 8 == p.K;
+#pragma unroll
+                for (int i = 0; i < F; ++i) {
+                    op[i] += mine ? 0u : (unsigned int)NB;
+                    ow[i][WORDS - 1] = mine ? ow[i][0] : ow[i][WORDS - 1];
+                    ow[i][0] = mine ? NOWHERE : ow[i][0];
+                }
+                const unsigned int first = put[0];
+                put[0] = mine ? put[1] : first;
+                put[1] = mine ? first : put[1];
+            }
         }
     };
-    struct Item { unsigned int c[2], w[WORDS]; };
+    struct Item { unsigned int c[CW], w[WORDS]; };
     auto load_w = [&](Item& z, int t, int i) {
-        const auto c = __builtin_amdgcn_raw_buffer_load_b64(resource(pw), (int)op[i], t * 32, 0);
-        z.c[0] = c[0]; z.c[1] = c[1];
+        const int at = t * 8 * NB - (half && t == steps - 1 ? NB : 0);
+        if constexpr (NB / 2 == 1) z.c[0] = (unsigned int)__builtin_amdgcn_raw_buffer_load_b32(resource(pw), (int)op[i], at, 0);
+        if constexpr (NB / 2 == 2) {
+            const auto c = __builtin_amdgcn_raw_buffer_load_b64(resource(pw), (int)op[i], at, 0);
+            z.c[0] = c[0]; z.c[1] = c[1];
+        }
+        if constexpr (NB / 2 == 3) {
+            const auto c = __builtin_amdgcn_raw_buffer_load_b96(resource(pw), (int)op[i], at, 0);
+            z.c[0] = c[0]; z.c[1] = c[1]; z.c[2] = c[2];
+        }
+        if constexpr (NB % 2 == 1) z.c[CW - 1] = __builtin_amdgcn_raw_buffer_load_b16(resource(pw), (int)op[i], at + NB / 2 * 4, 0);
 #pragma unroll
         for (int h = 0; h < WORDS; ++h) z.w[h] = __builtin_amdgcn_raw_buffer_load_b16(resource(ww), (int)ow[i][h], t * (128 >> lg), 0);
     };
 
-    v16f acc[4][F];
+    v16f acc[E][F];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < E; ++a)
 #pragma unroll
         for (int b = 0; b < F; ++b)
 #pragma unroll
@@ -364,19 +425,17 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
 
     typedef __attribute__((address_space(3))) v4i* ldsi;
     typedef __attribute__((address_space(3))) v2f* ldsp;
-    unsigned int put[2], putting[2] = {0, 0};                           // where this thread's weights go (rows 64 apart lie alike)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) put[h] = lds0 + BM * 128 + (unsigned int)(tid >> 2) * 128 + (unsigned int)((((tid & 3) * 2 + h) ^ (tid >> 3 & 7)) << 4);
     v2f v[2][4];
     float scale[2];
     unsigned int book = 0, mag = 0, ex = 0, frac = 0;
     // eight weights (half h of item z; o = 0 or 1 in turn): the e-th of eight parts of the look-ups and the scale
     auto look_up = [&](const Item& z, int h, int o, int e) {
         const unsigned int w = z.w[h & (WORDS - 1)];
-        if (e == 0) book = tab0 | (w >> p.sel_pos & (unsigned int)p.sel_mask) << 11;
+        if (e == 0) book = tab0 | (w >> p.sel_pos & (unsigned int)p.sel_mask) << (2 * NB + 3);
         if (!(e & 1)) {
-            const unsigned int m = e == 0 ? z.c[h] << 3 : z.c[h] >> (4 * e - 3);
-            v[o][e >> 1] = *(ldsp)(uintptr_t)((m & 0x7F8u) | book);
+            const int at = NB * (8 * h + e) - 3, i = at < 0 ? 0 : at >> 5, sh = at & 31;    // the pair's bits, moved to bit 3
+            const unsigned int m = at < 0 ? z.c[0] << -at : sh + 2 * NB + 3 <= 32 || i + 1 >= CW ? z.c[i] >> sh : __builtin_amdgcn_alignbit(z.c[i + 1 < CW ? i + 1 : 0], z.c[i], (unsigned int)sh);
+            v[o][e >> 1] = *(ldsp)(uintptr_t)((m & (unsigned int)(BOOK - 8)) | book);
         }
         if (e == 1) { mag = (w >> p.mag_shift) & (unsigned int)p.mag_mask; ex = mag >> p.man_bits; }
         if (e == 3) { frac = (mag & (unsigned int)p.man_mask) | min(ex, 1u) << p.man_bits; ex = max(ex, 1u); }
@@ -397,12 +456,12 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     unsigned int at[4];                                                 // the s-th sixteen elements of this lane's row, without the row
 #pragma unroll
     for (int s = 0; s < 4; ++s) at[s] = lds0 + (unsigned int)r32 * 128 + ((unsigned int)(((lane >> 5) ^ (r32 >> 1 & 7)) << 4) ^ (unsigned int)(s << 5));
-    v4i fx[2][4], fw[2][F];
+    v4i fx[2][E], fw[2][F];
     unsigned int rx = 0, rw = 0;
     auto from = [&](unsigned int stage, int s) { rx = at[s] + (stage + wm * 128); rw = at[s] + (stage + (BM + wn) * 128); };
-    auto read = [&](int s, int i) {                                     // the i-th of F + 4 reads
+    auto read = [&](int s, int i) {                                     // the i-th of F + E reads
         if (i < F) fw[s & 1][i] = *(ldsi)(uintptr_t)(rw + i * 4096);
-        else if (i < F + 4) fx[s & 1][i - F] = *(ldsi)(uintptr_t)(rx + (i - F) * 4096);
+        else if (i < F + E) fx[s & 1][i - F] = *(ldsi)(uintptr_t)(rx + (i - F) * 4096);
     };
     auto multiply = [&](int s, int i) {
         const int a = i / F, b = i % F;
@@ -413,8 +472,10 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     auto settle = [&](Item (&z)[F]) {                                   // what has arrived is used as such (and not waited for again behind later loads)
 #pragma unroll
         for (int i = 0; i < F; ++i) {
-            asm volatile("" : "+v"(z[i].c[0]), "+v"(z[i].c[1]), "+v"(z[i].w[0]));
-            if (G8) asm volatile("" : "+v"(z[i].w[WORDS - 1]));
+#pragma unroll
+            for (int k = 0; k < CW; ++k) asm volatile("" : "+v"(z[i].c[k]));
+#pragma unroll
+            for (int h = 0; h < WORDS; ++h) asm volatile("" : "+v"(z[i].w[h]));
         }
     };
     __syncthreads();                                                    // the codebooks are there
@@ -422,17 +483,17 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     for (int t = 0; t < 2; ++t) {
         end_x(t);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) load_x(t, i);
+        for (int i = 0; i < XL; ++i) load_x(t, i);
     }
     end_w(0);
 #pragma unroll
     for (int i = 0; i < F; ++i) load_w(next[i], 0, i);
+    putting[0] = put[0]; putting[1] = put[1];
     end_w(1);
 #pragma unroll
     for (int i = 0; i < F; ++i) load_w(now[i], 1, i);
-    putting[0] = put[0]; putting[1] = put[1];
     // A quarter of a step's work is F / 2 eights; with F = 3 the second of them is looked up, and half formed.
-    constexpr int PART = 4 * F;
+    constexpr int PART = 4 * F;                                         // parts of eights in a quarter
 #pragma unroll
     for (int g = 0; g < 2 * F; ++g) {
 #pragma unroll
@@ -440,7 +501,7 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
 #pragma unroll
         for (int e = 0; e < 8; ++e) form(g >> 1, g & 1, g & 1, e);
     }
-    putting[0] += STAGE; putting[1] += STAGE;
+    putting[0] = put[0] + STAGE; putting[1] = put[1] + STAGE;
 #pragma unroll
     for (int e = 0; e < 8; ++e) look_up(now[0], 0, 0, e);
 #pragma unroll
@@ -454,7 +515,7 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     settle(now);
     from(0, 0);
 #pragma unroll
-    for (int i = 0; i < F + 4; ++i) read(0, i);
+    for (int i = 0; i < F + E; ++i) read(0, i);
     for (int t = 0; t < steps; ++t) {
         const unsigned int here = (t & 1) * STAGE, there = STAGE - here;
         // sixteen elements of K, and a quarter of the work between two barriers: behind a step's last sixteen elements the first quarter of the
@@ -470,15 +531,22 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
 #pragma unroll
             for (int i = 0; i < SLOTS; ++i) {
                 multiply(s, i);
-                if (F == 4 ? (i & 1) == 0 : i < F + 4) read((s + 1) & 3, F == 4 ? i >> 1 : i);
-                const int f = Q * SLOTS + i, g = f >> 3, e = f & 7;     // the eight whose products are formed; the one after it is looked up
-                form(g >> 1, g & 1, g & 1, e);
-                if (f == 4 * SLOTS - 8) { wait_loads(); settle(next); }
-                if (g < 2 * F - 1) look_up(now[(g + 1) >> 1], (g + 1) & 1, (g + 1) & 1, e);
-                else look_up(next[0], 0, 0, e);
-                if (s == 3 && i * 8 / SLOTS != (i + 1) * 8 / SLOTS) load_x(t + 2, i * 8 / SLOTS);
-                if (s < 2 && i % 8 == 3) { if (s * (SLOTS / 8) + i / 8 < F) load_w(next[s * (SLOTS / 8) + i / 8], t + 2, s * (SLOTS / 8) + i / 8); }
-                if constexpr (F == 3 && s == 1) if (i == 8) load_w(next[2], t + 2, 2);
+                // the reads, dealt out over the instructions
+#pragma unroll
+                for (int k = i * (F + E) / SLOTS; k < (i + 1) * (F + E) / SLOTS; ++k) read((s + 1) & 3, k);
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) {
+                    const int f = (Q * SLOTS + i) * EACH + k, g = f >> 3, e = f & 7;    // the eight whose products are formed; the one after it is looked up
+                    form(g >> 1, g & 1, g & 1, e);
+                    if (f == 16 * F - 8) { wait_loads(); settle(next); }
+                    if (g < 2 * F - 1) look_up(now[(g + 1) >> 1], (g + 1) & 1, (g + 1) & 1, e);
+                    else look_up(next[0], 0, 0, e);
+                }
+                if (s == 3 && i * XL / SLOTS != (i + 1) * XL / SLOTS) load_x(t + 2, i * XL / SLOTS);
+                if (s < 2) {                                            // (the first two quarters ask for the next codes)
+#pragma unroll
+                    for (int k = 0; k < F; ++k) if (s * SLOTS + i == (2 * k + 1) * SLOTS / F) load_w(next[k], t + 2, k);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -494,7 +562,7 @@ __global__ __launch_bounds__(256) void packed_large_kernel(const PackedMmParams 
     }
     wait_loads();
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < E; ++a)
 #pragma unroll
         for (int b = 0; b < F; ++b)
 #pragma unroll
@@ -509,47 +577,51 @@ template <int NB, int FM, int U, int W> static hipError_t rows_go(const PackedMm
     hipLaunchKernelGGL(fn, dim3((unsigned)((p.N + 15) / 16)), dim3(W * 64), 0, st, p);
     return hipGetLastError();
 }
-template <int NB, int BM, int BN, int WR, int WC> static hipError_t tile_go(const PackedMmParams& p, hipStream_t st)
+template <int NB, int FM, int FN, int S> static hipError_t split_go(const PackedMmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128;
-    if (bytes > 64 * 1024 - 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&packed_tile_kernel<NB, BM, BN, WR, WC>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((packed_tile_kernel<NB, BM, BN, WR, WC>), dim3((unsigned)(tm * tn)), dim3(WR * WC * 64), bytes, st, p, tm, tn, 8);
+    const int tm = (p.M + 32 * FM - 1) / (32 * FM), tn = (p.N + 32 * FN - 1) / (32 * FN), bytes = 8 * (S > FN ? S : FN) * FM * 4096;
+    auto fn = p.g == 8 ? &packed_split_kernel<NB, FM, FN, S, 4> : p.g == 16 ? &packed_split_kernel<NB, FM, FN, S, 2> : &packed_split_kernel<NB, FM, FN, S, 1>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(512), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int F> static hipError_t large_go(const PackedMmParams& p, hipStream_t st)
+template <int NB, int E, int F> static hipError_t wide_go(const PackedMmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + 255) / 256, tn = (p.N + 64 * F - 1) / (64 * F), bytes = 4096 + 2 * (256 + 64 * F) * 128;
-    auto fn = p.g == 8 ? &packed_large_kernel<F, true> : &packed_large_kernel<F, false>;
+    const int tm = (p.M + 64 * E - 1) / (64 * E), tn = (p.N + 64 * F - 1) / (64 * F), bytes = (16 << 2 * NB) + 2 * (64 * E + 64 * F) * 128;
+    static_assert((16 << 2 * NB) + 2 * (64 * E + 64 * F) * 128 <= 160 * 1024, "the tables and two steps fit into LDS");
+    auto fn = p.g == 8 ? &packed_wide_kernel<NB, E, F, true> : &packed_wide_kernel<NB, E, F, false>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(256), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-// One workgroup a compute unit: the width whose last round is filled better.  A tile of 192 columns forms and reads more for a product: 2048 x
-// 11008 x 4096 takes 242 us by it (464 tiles, two rounds) and 256 us by the wider (344 tiles, two rounds), 4096 x 4096 x 4096 208 us (352
-// tiles, two rounds) and 145 us (256 tiles, one).
-static hipError_t large_pick(const PackedMmParams& p, int n_cu, hipStream_t st)
-{
-    auto cost = [&](int f, int each) {
-        const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 64 * f - 1) / (64 * f));
-        return (tiles + n_cu - 1) / n_cu * f * each;
-    };
-    return cost(4, 20) <= cost(3, 25) ? large_go<4>(p, st) : large_go<3>(p, st);
-}
+// The kernel that is expected to take least, from how many workgroups a compute unit gets.  Microseconds at K = 4096 on 256 compute units, 4-bit
+// codes, by c workgroups each: the narrow tiles 8 c + 2 (32 x 32), 11 c + 2 (64 x 32), 20.5 c (64 x 64), 19.5 c (128 x 32); the wide ones 64 for one
+// and 51 c for more (128 x 128), 110 c (256 x 192), 128 c (256 x 256; 146 when every unit has one).  Measured, the best and the next: 32 x 11008 x
+// 4096 17.8 (32 x 32) and 19.6; 64 x 11008 x 4096 20.9 (64 x 64) and 23.0; 128 x 4096 x 4096 14.5 (64 x 32) and 18.7; 512 x 4096 x 4096 39 (128 x 32)
+// and 42; 1024 x 4096 x 4096 71 (128 x 128) and 77; 2048 x 11008 x 4096 212 (256 x 192) and 244; 4096 x 4096 x 4096 146 (256 x 256) and 199.  Codes
+// of 3 and 5 bits take up to a quarter more, in the same order.  Few rows: a workgroup of 16 columns reads x itself; one row through
+// 4096 x 11008 takes 11.7 us with the call, 17 to 20 by the narrow tiles.  Tables of pairs of 6-bit codes fit beside 128 x 128 tiles only.
 template <int NB> static hipError_t packed_pick(const PackedMmParams& p, int n_cu, hipStream_t st)
 {
-    auto tiles = [&](int bm, int bn) { return (long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn); };
-    if (p.M <= 16) return rows_go<NB, 1, 3, 16>(p, st);
-    if (p.M <= 32) return rows_go<NB, 2, 2, 8>(p, st);
-    if (tiles(256, 256) >= n_cu) {
-        if constexpr (NB == 4) return large_pick(p, n_cu, st);
-        else return tile_go<NB, 256, 256, 2, 4>(p, st);
+    if (p.M <= 16) return rows_go<NB, 1, 3, 8>(p, st);
+    auto each = [&](int bm, int bn) { return (float)(((long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) + n_cu - 1) / n_cu); };
+    const float c22 = each(128, 128), never = 3.4e38f;
+    const float cost[7] = {8.0f * each(32, 32) + 1.7f, 11.0f * each(64, 32) + 2.0f, 20.5f * each(64, 64), 19.5f * each(128, 32),
+                           p.K < 64 ? never : c22 <= 1.0f ? 64.0f : 51.0f * c22, p.K < 64 || NB > 5 ? never : 110.0f * each(256, 192), p.K < 64 || NB > 5 ? never : 128.0f * each(256, 256)};
+    int best = 0;
+    for (int i = 1; i < 7; ++i) best = cost[i] < cost[best] ? i : best;
+    switch (best) {
+    case 0: return split_go<NB, 1, 1, 1>(p, st);
+    case 1: return split_go<NB, 2, 1, 1>(p, st);
+    case 2: return split_go<NB, 2, 2, 1>(p, st);
+    case 3: return split_go<NB, 4, 1, 1>(p, st);
+    case 4: return wide_go<NB, 2, 2>(p, st);
+    default:
+        if constexpr (NB > 5) return hipErrorInvalidValue;
+        else return best == 5 ? wide_go<NB, 4, 3>(p, st) : wide_go<NB, 4, 4>(p, st);
     }
-    if (tiles(128, 128) >= n_cu) return tile_go<NB, 128, 128, 2, 2>(p, st);
-    return tile_go<NB, 64, 64, 2, 2>(p, st);
 }
 
 }  // namespace sopk

@@ -497,3 +497,16 @@ def test_refusals():
                                   (8200, 2049, 320, 64, 4, (0, 4, 3, 8), True, 2)])
 def test_packed_product_of_large_layers(case):
     test_packed_product(case)
+
+
+# the kernels that share a wide output out, and that deal K out, by code width: K ends in the middle of a step, of sixteen codes and on a step
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("M, N, K, g", [(1020, 4090, 136, 8), (1020, 4090, 72, 8), (1000, 11000, 152, 8), (4000, 4090, 88, 8), (1020, 4090, 176, 16), (4000, 4090, 64, 64), (1000, 11000, 320, 32)])
+def test_packed_product_of_wide_outputs(M, N, K, g, n):
+    test_packed_product((M, N, K, g, n, (1, 5, 5, 12), True, 1))
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("M, N, K, g", [(20, 100, 8, 8), (17, 33, 1096, 8), (65, 1001, 584, 8), (128, 4097, 600, 8), (128, 4097, 608, 16), (64, 11008, 1040, 16), (61, 11008, 72, 8), (511, 4096, 576, 64), (505, 4090, 520, 8)])
+def test_packed_product_of_some_rows(M, N, K, g, n):
+    test_packed_product((M, N, K, g, n, (0, 4, 3, 8), True, 0))
