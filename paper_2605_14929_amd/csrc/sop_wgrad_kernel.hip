@@ -312,6 +312,131 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
                          v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
 }
 
+// ---- small gradients, the rows dealt out: 32 FN x 64 of dw a workgroup, its eight wavefronts taking 64 rows in turn, each in a place of its own
+// in LDS (no barrier before the sums are joined, in the order of the wavefronts).  The next rows are asked for when these have been read.
+// Chunk c of row m stands at position c ^ 4 (m / 2 & 1) (dy, rows of 128 bytes; of 64: c), c ^ 2 (m / 4 & 1) (x, rows of 64).
+template <int FN, bool X5>
+__global__ __launch_bounds__(512) void wgrad_split_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
+{
+    constexpr int W = 8, FK = 2, BN = 32 * FN, BK = 64, CD = 4 * FN, LD = 4 * FN, LX = 4, XAT = 128 * BN, SAT = XAT + 64 * BK, SUMS = FN * FK * 4096, OWN = SAT + 256 > SUMS ? SAT + 256 : SUMS;
+    extern __shared__ __align__(16) unsigned char lds[];
+    int tn, tk;
+    tile_of(blockIdx.x, tiles_n * tiles_k, tiles_n, tiles_k, group, tn, tk);
+    const int n0 = tn * BN, k0 = tk * BK, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g16 = lane >> 4 & 1, h = lane >> 5;
+    const int steps = (p.M + 63) >> 6;
+    unsigned char* own = lds + wave * OWN;
+    const unsigned int own0 = lds_address(own);
+    auto turn_d = [](int m) { return FN == 2 ? (m >> 1 & 1) << 2 : 0; };
+    auto turn_x = [](int m) { return (m >> 2 & 1) << 1; };
+    unsigned int od[LD], ox[LX];                                        // (as above)
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+        const int m = lane / CD + i * (64 / CD), n = min(n0 + ((lane % CD) ^ turn_d(m)) * 8, (p.N - 1) & ~7);
+        od[i] = ((unsigned int)m * (unsigned int)p.lddy + (unsigned int)n) * 2u;
+    }
+#pragma unroll
+    for (int i = 0; i < LX; ++i) {
+        const int m = (lane >> 2) + i * 16, k = min(k0 + ((lane & 3) ^ turn_x(m)) * 16, (p.K - 1) & ~15);
+        ox[i] = (unsigned int)m * (unsigned int)p.ldx + (unsigned int)k;
+    }
+    const unsigned int wide_n = (unsigned int)((p.N + 7) & ~7) * 2u, wide_k = (unsigned int)((p.K + 15) & ~15);
+    auto load = [&](int t) {                                            // rows beyond the last arrive as zeros
+        const long long m0 = (long long)t * 64;
+        const unsigned int last = (unsigned int)min(64, p.M - (int)m0) - 1;
+        const Window d = window(p.dy + m0 * p.lddy, last * (unsigned int)p.lddy * 2u + wide_n);
+        const Window x = window(p.x + m0 * p.ldx, last * (unsigned int)p.ldx + wide_k);
+        load_word_to_lds(window(p.xs + m0 * p.ldxs, last * (unsigned int)p.ldxs + (unsigned int)p.ldxs), min((unsigned int)lane, last) * (unsigned int)p.ldxs + (unsigned int)(k0 >> 7 & ~3), 0, own0 + SAT);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) load_to_lds(d, od[i], 0, own0 + i * 1024);
+#pragma unroll
+        for (int i = 0; i < LX; ++i) load_to_lds(x, ox[i], 0, own0 + XAT + i * 1024);
+    };
+    unsigned int ad[FN], ax[FK];
+#pragma unroll
+    for (int a = 0; a < FN; ++a) {
+        const int c = 4 * a + 2 * g16 + (i16 >> 1 & 1), m = 8 * h + (i16 >> 2);     // (m + 4 stands alike)
+        ad[a] = own0 + (unsigned int)(m * (BN * 2) + ((c ^ turn_d(m)) << 4) + (i16 & 1) * 8);
+    }
+#pragma unroll
+    for (int b = 0; b < FK; ++b) {
+        const int c = 2 * b + g16, m = 8 * h + (i16 >> 1);
+        ax[b] = own0 + (unsigned int)(XAT + m * BK + ((c ^ turn_x(m)) << 4) + (i16 & 1) * 8);
+    }
+    typedef __attribute__((address_space(3))) v4s* lds16;
+    typedef __attribute__((address_space(3))) v2i* lds8;
+    v16f acc[FN][FK];
+#pragma unroll
+    for (int a = 0; a < FN; ++a)
+#pragma unroll
+        for (int b = 0; b < FK; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.0f;
+    if (wave < steps) load(wave);
+    for (int t = wave; t < steps; t += W) {
+        v4s d[4][FN][2];
+        v2i c[4][FK];
+        v4f sc[4][2];
+        wait_loads();
+        {                                                               // the scale word of this lane's row becomes its number
+            const unsigned int w = *reinterpret_cast<const unsigned int*>(own + SAT + lane * 4);
+            *reinterpret_cast<float*>(own + SAT + lane * 4) = e8m0_value(w >> (8 * ((k0 >> 7) & 3)) & 255u);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+#pragma unroll
+            for (int a = 0; a < FN; ++a)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) d[s][a][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds16)(uintptr_t)(ad[a] + s * (32 * BN) + i * (8 * BN)));
+#pragma unroll
+            for (int b = 0; b < FK; ++b) c[s][b] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds8)(uintptr_t)(ax[b] + s * (16 * BK)));
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // (the numbers are written)
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) sc[s][i] = *reinterpret_cast<const v4f*>(own + SAT + s * 64 + h * 32 + i * 16);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // (the reads have ended: the place is free)
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + W < steps) load(t + W);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            v8bf x[FK];
+#pragma unroll
+            for (int b = 0; b < FK; ++b) {
+                v4i r;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {                           // rows 4i .. 4i + 3
+                    r[2 * i] = two_rows<X5, false>(c[s][b][i], sc[s][i][0], sc[s][i][1]);
+                    r[2 * i + 1] = two_rows<X5, true>(c[s][b][i], sc[s][i][2], sc[s][i][3]);
+                }
+                x[b] = __builtin_bit_cast(v8bf, r);
+            }
+#pragma unroll
+            for (int a = 0; a < FN; ++a) {
+                const v8bf y = __builtin_bit_cast(v8bf, __builtin_shufflevector(d[s][a][0], d[s][a][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int b = 0; b < FK; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[b], y, acc[a][b], 0, 0, 0);
+            }
+        }
+    }
+    v4f* part = reinterpret_cast<v4f*>(own);                            // [square][quarter][lane], this wavefront's
+#pragma unroll
+    for (int a = 0; a < FN; ++a)
+#pragma unroll
+        for (int b = 0; b < FK; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                part[((a * FK + b) * 4 + i) * 64 + lane] = v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]};
+    __syncthreads();
+    for (int t = wave; t < FN * FK * 4; t += W) {
+        const int a = (t >> 2) / FK, b = (t >> 2) % FK, i = t & 3;
+        v4f s = reinterpret_cast<const v4f*>(lds)[t * 64 + lane];
+#pragma unroll
+        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[t * 64 + lane];
+        store_dw(p, n0 + a * 32 + (lane & 31), k0 + b * 32 + 8 * i + 4 * h, s);
+    }
+}
+
 // ---- large gradients: 256 x 256 of dw by four wavefronts, one on a SIMD, each 128 x 128 of it.  As above, but a wavefront overlaps its own
 // work.  While sixteen rows are multiplied (sixteen matrix instructions), behind each of them stands a sixteenth of: the reads of the next
 // sixteen rows of dy, the reads of the codes after the next, the conversion of the next codes, the loads of the step after the next.  A
@@ -477,6 +602,14 @@ template <bool X5> static hipError_t wgrad_large_go(const WgradParams& p, hipStr
     return hipGetLastError();
 }
 
+template <int FN, bool X5> static hipError_t wgrad_split_go(const WgradParams& p, hipStream_t st)
+{
+    const int tn = (p.N + 32 * FN - 1) / (32 * FN), tk = (p.K + 63) / 64, own = 4096 * FN + 4096 + 256, bytes = 8 * (own > FN * 8192 ? own : FN * 8192);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&wgrad_split_kernel<FN, X5>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((wgrad_split_kernel<FN, X5>), dim3((unsigned)(tn * tk)), dim3(512), bytes, st, p, tn, tk, 8);
+    return hipGetLastError();
+}
 template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_turn_go(const WgradParams& p, hipStream_t st)
 {
     const int tn = (p.N + BN - 1) / BN, tk = (p.K + BK - 1) / BK, bytes = 3 * (64 * BN * 2 + 64 * BK + BK / 128 * 256) + 3 * 256;
@@ -497,11 +630,23 @@ template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_go(co
     hipLaunchKernelGGL((wgrad_kernel<BN, BK, WR, WC, X5>), dim3((unsigned)(tn * tk)), dim3(WR * WC * 64), bytes, st, p, tn, tk, 8);
     return hipGetLastError();
 }
+// The kernel that is expected to take least, from how many workgroups c a compute unit gets and how many times 64 rows there are (t).
+// Microseconds on 256 compute units, 32-bit results: the rows dealt out 1.4 + c (1.2 + 0.16 t) (32 x 64) and 1.2 + c (2.9 + 0.21 t) (64 x 64);
+// 128 x 128 4.4 + 0.82 t for one and c (4 + 0.6 t) for more; 256 x 256 c (25 + 1.65 t).  Measured (rows x N x K), the best and the next:
+// 8192 x 512 x 512 24 (32 x 64) and 33, by 128 x 128 107; 8192 x 1024 x 1024 32 (64 x 64) and 49; 777 x 1531 x 5024 23 (128 x 128) and 32;
+// 2048 x 4096 x 4096 72 (256 x 256) and 92; 64 x 11008 x 4096 49 (128 x 128) and 57, 180 MB of results.
 template <bool X5> static hipError_t wgrad_pick(const WgradParams& p, int n_cu, hipStream_t st)
 {
     auto tiles = [&](int a, int b) { return (long long)((p.N + a - 1) / a) * ((p.K + b - 1) / b); };
     const bool on16 = (reinterpret_cast<uintptr_t>(p.dy) & 15) == 0 && (p.lddy & 7) == 0 && p.lddy <= 1 << 22;
-    if (p.M > 0 && on16) return tiles(256, 256) >= n_cu ? wgrad_large_go<X5>(p, st) : wgrad_turn_go<128, 128, 2, 2, X5>(p, st);
+    if (p.M > 0 && on16) {
+        auto each = [&](int a, int b) { return (float)((tiles(a, b) + n_cu - 1) / n_cu); };
+        const float t = (float)((p.M + 63) / 64), c44 = each(128, 128);
+        const float cost[4] = {1.4f + each(32, 64) * (1.2f + 0.16f * t), 1.2f + each(64, 64) * (2.9f + 0.21f * t), c44 <= 1.0f ? 4.4f + 0.82f * t : c44 * (4.0f + 0.6f * t), each(256, 256) * (25.0f + 1.65f * t)};
+        int best = 0;
+        for (int i = 1; i < 4; ++i) best = cost[i] < cost[best] ? i : best;
+        return best == 0 ? wgrad_split_go<1, X5>(p, st) : best == 1 ? wgrad_split_go<2, X5>(p, st) : best == 2 ? wgrad_turn_go<128, 128, 2, 2, X5>(p, st) : wgrad_large_go<X5>(p, st);
+    }
     if (tiles(256, 256) >= n_cu) return wgrad_go<256, 256, 2, 4, X5>(p, st);
     if (tiles(128, 128) >= n_cu) return wgrad_go<128, 128, 2, 2, X5>(p, st);
     return wgrad_go<64, 128, 2, 2, X5>(p, st);

@@ -510,3 +510,47 @@ def test_packed_product_of_wide_outputs(M, N, K, g, n):
 @pytest.mark.parametrize("M, N, K, g", [(20, 100, 8, 8), (17, 33, 1096, 8), (65, 1001, 584, 8), (128, 4097, 600, 8), (128, 4097, 608, 16), (64, 11008, 1040, 16), (61, 11008, 72, 8), (511, 4096, 576, 64), (505, 4090, 520, 8)])
 def test_packed_product_of_some_rows(M, N, K, g, n):
     test_packed_product((M, N, K, g, n, (0, 4, 3, 8), True, 0))
+
+
+# rows of dy on 16 bytes, its columns no multiple of 8: the rows dealt out (32 x 64 and 64 x 64 of dw a workgroup), 128 x 128 and 256 x 256 (sums of at
+# most 128 M, which binary32 holds exactly)
+@pytest.mark.parametrize("fmt", ["E4M3", "E5M2"])
+@pytest.mark.parametrize("M, N, K", [(1, 1, 1), (63, 33, 65), (65, 100, 130), (129, 31, 127), (513, 257, 515), (1100, 300, 500), (2100, 1001, 1000), (65, 1531, 2100), (130, 1027, 4100), (1025, 4090, 4000)])
+def test_weight_gradient_of_spaced_rows(M, N, K, fmt):
+    import torch
+    rng = np.random.default_rng(12)
+    xc, xs = _integers(rng, M, K, 1, fmt)
+    dy = rng.integers(-8, 9, (M, N)).astype(np.float32)
+    ref = (torch.from_numpy(dy).cuda().double().t() @ torch.from_numpy(OL.values(xc, xs, 1, fmt)).cuda()).cpu().numpy()
+    x, d = _f8(xc, xs, 1, fmt), _t(dy, "bf16", 8 + -N % 8)
+    assert np.array_equal(_np(ctx().fp8_weight_grad(d, x)), ref)
+    out = torch.ones((N, K + 1), device="cuda")
+    ctx().fp8_weight_grad(d, x, out=out[:, :K], accumulate=True)
+    assert np.array_equal(_np(out[:, :K]), ref + 1) and np.all(_np(out[:, K:]) == 1)
+
+
+@pytest.mark.parametrize("M, N, K", [(3, 40, 200), (70, 300, 600), (777, 1024, 1100), (65, 1536, 2100), (1025, 4096, 4000)])
+def test_missing_numbers_stay_in_their_block(M, N, K):
+    """A scale that is no number, or a code that is none, makes what it takes part in no number, and nothing else."""
+    import torch
+    rng = np.random.default_rng(13)
+    xc, xs = _integers(rng, M, K, 1)
+    wc, ws = _integers(rng, N, K, 128)
+    xs[M // 2, 1] = 255                                                 # columns 128 .. 255 of a row of x
+    xc[M - 1, K - 1] = 0x7F                                             # one element
+    x = _f8(xc, xs, 1, "E4M3")
+    dy = rng.integers(-8, 9, (M, N)).astype(np.float32)
+    dw = _np(ctx().fp8_weight_grad(_t(dy, "bf16"), x))
+    gone = np.zeros(K, bool)
+    gone[128:256] = True
+    gone[K - 1] = True
+    assert np.isnan(dw[:, gone]).all() and np.isfinite(dw[:, ~gone]).all()
+    for dtype in (torch.float32, torch.bfloat16):
+        y = _np(ctx().fp8_matmul(x, _f8(wc, ws, 128, "E4M3"), dtype=dtype))
+        rows = np.isin(np.arange(M), [M // 2, M - 1])
+        assert np.isnan(y[rows]).all() and np.isfinite(y[~rows]).all()
+    ws[0, 1] = 255                                                      # rows 0 .. 127 of w
+    good = _f8(*_integers(rng, M, K, 1), 1, "E4M3")
+    for dtype in (torch.float32, torch.bfloat16):
+        y = _np(ctx().fp8_matmul(good, _f8(wc, ws, 128, "E4M3"), dtype=dtype))
+        assert np.isnan(y[:, :128]).all() and np.isfinite(y[:, 128:]).all()
