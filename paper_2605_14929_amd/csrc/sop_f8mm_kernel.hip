@@ -29,17 +29,15 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
     const long long at = (long long)m * p.ldy + n;
     if (p.out_bf16) {
         uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + at;
-        if (n + 3 < p.N && (reinterpret_cast<uintptr_t>(y) & 7) == 0) {
-            *reinterpret_cast<uint2*>(y) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-        } else {
+        if (n + 3 < p.N) put_four(y, v);
+        else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) if (n + i < p.N) y[i] = (uint16_t)bf16_bits(v[i]);
         }
     } else {
         float* y = reinterpret_cast<float*>(p.y) + at;
-        if (n + 3 < p.N && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
-            *reinterpret_cast<v4f*>(y) = v;
-        } else {
+        if (n + 3 < p.N) put_four(y, v);
+        else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) if (n + i < p.N) y[i] = v[i];
         }
@@ -206,13 +204,16 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
         turn(KF);
         compute(KF);
     }
+    __syncthreads();                                                    // (LDS is free for the results)
+    v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
 #pragma unroll
     for (int a = 0; a < FM; ++a)
 #pragma unroll
-        for (int b = 0; b < FN; ++b)
+        for (int b = 0; b < FN; ++b) {
+            put_square(place, lane, acc[a][b]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * h, v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+            for (int i = 0; i < 4; ++i) store_y(p, m0 + wm + a * 32 + 8 * i + (lane >> 3), n0 + wn + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+        }
 }
 
 // ---- few tiles: FM x 16 rows of x by FN x 16 columns a workgroup, K dealt out to its W wavefronts, U steps at a time.  Operands go from
@@ -425,21 +426,17 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
     }
     wait_loads();
     __syncthreads();
-    v4f* part = reinterpret_cast<v4f*>(own);                            // [square][quarter][lane], this wavefront's
 #pragma unroll
     for (int a = 0; a < FM; ++a)
 #pragma unroll
-        for (int b = 0; b < FN; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                part[((a * FN + b) * 4 + i) * 64 + lane] = v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]};
+        for (int b = 0; b < FN; ++b) put_square(reinterpret_cast<v4f*>(own) + (a * FN + b) * 256, lane, acc[a][b]);
     __syncthreads();
-    for (int t = wave; t < FM * FN * 4; t += W) {
-        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3;
-        v4f s = reinterpret_cast<const v4f*>(lds)[t * 64 + lane];
+    for (int t = wave; t < FM * FN * 4; t += W) {                         // a quarter of a square
+        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3, at = (t >> 2) * 256 + quarter_slot(i, lane);
+        v4f s = reinterpret_cast<const v4f*>(lds)[at];
 #pragma unroll
-        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[t * 64 + lane];
-        store_y(p, m0 + a * 32 + r32, n0 + b * 32 + 8 * i + 4 * h, s);
+        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[at];
+        store_y(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
     }
 }
 

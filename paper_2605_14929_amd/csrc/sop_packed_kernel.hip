@@ -80,9 +80,8 @@ __device__ __forceinline__ void store_y(const PackedMmParams& p, int m, int n, v
 {
     if (m >= p.M || n >= p.N) return;
     uint16_t* y = p.y + (long long)m * p.ldy + n;
-    if (n + 3 < p.N && (reinterpret_cast<uintptr_t>(y) & 7) == 0) {
-        *reinterpret_cast<uint2*>(y) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-    } else {
+    if (n + 3 < p.N) put_four(y, v);
+    else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) if (n + i < p.N) y[i] = (uint16_t)bf16_bits(v[i]);
     }
@@ -305,21 +304,17 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
     }
     wait_loads();
     __syncthreads();
-    v4f* part = reinterpret_cast<v4f*>(own);                            // [square][quarter][lane], this wavefront's
 #pragma unroll
     for (int a = 0; a < FM; ++a)
 #pragma unroll
-        for (int b = 0; b < FN; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                part[((a * FN + b) * 4 + i) * 64 + lane] = v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]};
+        for (int b = 0; b < FN; ++b) put_square(reinterpret_cast<v4f*>(own) + (a * FN + b) * 256, lane, acc[a][b]);
     __syncthreads();
-    for (int t = wave; t < FM * FN * 4; t += W) {
-        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3;
-        v4f s = reinterpret_cast<const v4f*>(lds)[t * 64 + lane];
+    for (int t = wave; t < FM * FN * 4; t += W) {                         // a quarter of a square
+        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3, at = (t >> 2) * 256 + quarter_slot(i, lane);
+        v4f s = reinterpret_cast<const v4f*>(lds)[at];
 #pragma unroll
-        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[t * 64 + lane];
-        store_y(p, m0 + a * 32 + r32, n0 + b * 32 + 8 * i + 4 * h, s);
+        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[at];
+        store_y(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
     }
 }
 
@@ -561,14 +556,16 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
         part(std::integral_constant<int, 3>{});
     }
     wait_loads();
+    __syncthreads();                                                    // (LDS is free for the results)
+    v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
 #pragma unroll
     for (int a = 0; a < E; ++a)
 #pragma unroll
-        for (int b = 0; b < F; ++b)
+        for (int b = 0; b < F; ++b) {
+            put_square(place, lane, acc[a][b]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                store_y(p, m0 + wm + a * 32 + r32, n0 + wn + b * 32 + 8 * i + 4 * (lane >> 5),
-                        v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+            for (int i = 0; i < 4; ++i) store_y(p, m0 + wm + a * 32 + 8 * i + (lane >> 3), n0 + wn + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+        }
 }
 
 template <int NB, int FM, int U, int W> static hipError_t rows_go(const PackedMmParams& p, hipStream_t st)

@@ -32,16 +32,16 @@ __device__ __forceinline__ void store_dw(const WgradParams& p, int n, int k, v4f
 #pragma unroll
             for (int i = 0; i < 4; ++i) if (k + i < p.K) v[i] += __uint_as_float((unsigned int)w[i] << 16);
         }
-        if (four && (reinterpret_cast<uintptr_t>(w) & 7) == 0) *reinterpret_cast<uint2*>(w) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        if (four) put_four(w, v);
         else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) if (k + i < p.K) w[i] = (uint16_t)bf16_bits(v[i]);
         }
     } else {
         float* w = reinterpret_cast<float*>(p.dw) + at;
-        if (four && (reinterpret_cast<uintptr_t>(w) & 15) == 0) {
-            if (p.accumulate) v += *reinterpret_cast<const v4f*>(w);
-            *reinterpret_cast<v4f*>(w) = v;
+        if (four) {
+            if (p.accumulate) v += reinterpret_cast<const FourWords*>(w)->v;
+            put_four(w, v);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) if (k + i < p.K) w[i] = p.accumulate ? v[i] + w[i] : v[i];
@@ -302,14 +302,16 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
         unsigned char* u = now;
         now = next; next = after; after = u;
     }
+    __syncthreads();                                                    // (LDS is free for the results)
+    v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
 #pragma unroll
     for (int a = 0; a < FA; ++a)
 #pragma unroll
-        for (int b = 0; b < FB; ++b)
+        for (int b = 0; b < FB; ++b) {
+            put_square(place, lane, acc[a][b]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                store_dw(p, n0 + wn + a * 32 + (lane & 31), k0 + wk + b * 32 + 8 * i + 4 * h,
-                         v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+            for (int i = 0; i < 4; ++i) store_dw(p, n0 + wn + a * 32 + 8 * i + (lane >> 3), k0 + wk + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+        }
 }
 
 // ---- small gradients, the rows dealt out: 32 FN x 64 of dw a workgroup, its eight wavefronts taking 64 rows in turn, each in a place of its own
@@ -419,21 +421,17 @@ __global__ __launch_bounds__(512) void wgrad_split_kernel(const WgradParams p, i
             }
         }
     }
-    v4f* part = reinterpret_cast<v4f*>(own);                            // [square][quarter][lane], this wavefront's
 #pragma unroll
     for (int a = 0; a < FN; ++a)
 #pragma unroll
-        for (int b = 0; b < FK; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                part[((a * FK + b) * 4 + i) * 64 + lane] = v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]};
+        for (int b = 0; b < FK; ++b) put_square(reinterpret_cast<v4f*>(own) + (a * FK + b) * 256, lane, acc[a][b]);
     __syncthreads();
-    for (int t = wave; t < FN * FK * 4; t += W) {
-        const int a = (t >> 2) / FK, b = (t >> 2) % FK, i = t & 3;
-        v4f s = reinterpret_cast<const v4f*>(lds)[t * 64 + lane];
+    for (int t = wave; t < FN * FK * 4; t += W) {                         // a quarter of a square
+        const int a = (t >> 2) / FK, b = (t >> 2) % FK, i = t & 3, at = (t >> 2) * 256 + quarter_slot(i, lane);
+        v4f s = reinterpret_cast<const v4f*>(lds)[at];
 #pragma unroll
-        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[t * 64 + lane];
-        store_dw(p, n0 + a * 32 + (lane & 31), k0 + b * 32 + 8 * i + 4 * h, s);
+        for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[at];
+        store_dw(p, n0 + a * 32 + 8 * i + (lane >> 3), k0 + b * 32 + 4 * (lane & 7), s);
     }
 }
 
@@ -583,14 +581,16 @@ __global__ __launch_bounds__(256) void wgrad_large_kernel(const WgradParams p, i
         r = r1;
     }
     wait_loads();
+    __syncthreads();                                                    // (LDS is free for the results)
+    v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
 #pragma unroll
     for (int a = 0; a < 4; ++a)
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < 4; ++b) {
+            put_square(place, lane, acc[a][b]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                store_dw(p, n0 + wn + a * 32 + (lane & 31), k0 + wk + b * 32 + 8 * i + 4 * h,
-                         v4f{acc[a][b][4 * i], acc[a][b][4 * i + 1], acc[a][b][4 * i + 2], acc[a][b][4 * i + 3]});
+            for (int i = 0; i < 4; ++i) store_dw(p, n0 + wn + a * 32 + 8 * i + (lane >> 3), k0 + wk + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+        }
 }
 
 template <bool X5> static hipError_t wgrad_large_go(const WgradParams& p, hipStream_t st)
@@ -632,9 +632,9 @@ template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_go(co
 }
 // The kernel that is expected to take least, from how many workgroups c a compute unit gets and how many times 64 rows there are (t).
 // Microseconds on 256 compute units, 32-bit results: the rows dealt out 1.4 + c (1.2 + 0.16 t) (32 x 64) and 1.2 + c (2.9 + 0.21 t) (64 x 64);
-// 128 x 128 4.4 + 0.82 t for one and c (4 + 0.6 t) for more; 256 x 256 c (25 + 1.65 t).  Measured (rows x N x K), the best and the next:
+// 128 x 128 4.4 + 0.82 t for one and c (4 + 0.6 t) for more; 256 x 256 c (19 + 1.65 t).  Measured (rows x N x K), the best and the next:
 // 8192 x 512 x 512 24 (32 x 64) and 33, by 128 x 128 107; 8192 x 1024 x 1024 32 (64 x 64) and 49; 777 x 1531 x 5024 23 (128 x 128) and 32;
-// 2048 x 4096 x 4096 72 (256 x 256) and 92; 64 x 11008 x 4096 49 (128 x 128) and 57, 180 MB of results.
+// 2048 x 4096 x 4096 72 (256 x 256) and 92; 500 x 8192 x 4096 67 (256 x 256) and 71.
 template <bool X5> static hipError_t wgrad_pick(const WgradParams& p, int n_cu, hipStream_t st)
 {
     auto tiles = [&](int a, int b) { return (long long)((p.N + a - 1) / a) * ((p.K + b - 1) / b); };
@@ -642,7 +642,7 @@ template <bool X5> static hipError_t wgrad_pick(const WgradParams& p, int n_cu, 
     if (p.M > 0 && on16) {
         auto each = [&](int a, int b) { return (float)((tiles(a, b) + n_cu - 1) / n_cu); };
         const float t = (float)((p.M + 63) / 64), c44 = each(128, 128);
-        const float cost[4] = {1.4f + each(32, 64) * (1.2f + 0.16f * t), 1.2f + each(64, 64) * (2.9f + 0.21f * t), c44 <= 1.0f ? 4.4f + 0.82f * t : c44 * (4.0f + 0.6f * t), each(256, 256) * (25.0f + 1.65f * t)};
+        const float cost[4] = {1.4f + each(32, 64) * (1.2f + 0.16f * t), 1.2f + each(64, 64) * (2.9f + 0.21f * t), c44 <= 1.0f ? 4.4f + 0.82f * t : c44 * (4.0f + 0.6f * t), each(256, 256) * (19.0f + 1.65f * t)};
         int best = 0;
         for (int i = 1; i < 4; ++i) best = cost[i] < cost[best] ? i : best;
         return best == 0 ? wgrad_split_go<1, X5>(p, st) : best == 1 ? wgrad_split_go<2, X5>(p, st) : best == 2 ? wgrad_turn_go<128, 128, 2, 2, X5>(p, st) : wgrad_large_go<X5>(p, st);
