@@ -89,6 +89,8 @@ __device__ __forceinline__ void store_y(const PackedMmParams& p, int m, int n, v
 
 // ---- few rows of x: FM x 16 of them by 16 columns a workgroup, K dealt out to its W wavefronts, 128 elements a step, U steps of a
 // wavefront in flight: a lane takes 32 neighbouring codes of its row, eight for each of four matrix instructions, and the same elements of x.
+// One row through 4096 x 11008 (28 MB of codes and scale words) takes 11.5 us, through 28672 x 8192 (147 MB) 48; more steps in flight or more
+// wavefronts take as long (12.2 for four steps): a weight's four to five instructions and its look-up in LDS bound it, sixteen rows (18.3) their loads too.
 // WPL: scale words of 32 codes (4, 2 or 1 for g = 8, 16 and more).
 template <int NB, int FM, int U, int W, int WPL>
 __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParams p)
@@ -142,23 +144,26 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
     };
     put_codebooks<NB>(p, tab, tid);
     __syncthreads();
-    int t = wave;
-    for (; t + (U - 1) * W < whole; t += U * W) {
+    // U steps in flight all the time; what the last batch has beyond the wavefront's steps is asked for again and not added
+    const int mine = wave < whole ? (whole - wave + W - 1) / W : 0, batches = (mine + U - 1) / U;
+    if (mine) {
         Step z[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) load(t + u * W, z[u]);
-        __builtin_amdgcn_sched_barrier(0);                              // (every load of the U steps is asked for before the first is used)
-#pragma unroll
-        for (int u = 0; u < U; ++u) add(z[u]);
-    }
+        for (int u = 0; u < U; ++u) load(wave + min(u, mine - 1) * W, z[u]);
 #pragma unroll 1
-    for (; t < whole; t += W) {
-        Step z;
-        load(t, z);
-        add(z);
+        for (int b = 1; b < batches; ++b) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                add(z[u]);
+                load(wave + min(b * U + u, mine - 1) * W, z[u]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) if ((batches - 1) * U + u < mine) add(z[u]);
     }
-    if (t == whole && t < steps) {                                      // the last step of a K that is no multiple of 128: one wavefront's
-        const int k = t * 128 + q * 32;
+    if (whole < steps && wave == whole % W) {                                      // the last step of a K that is no multiple of 128: one wavefront's
+        const int k = whole * 128 + q * 32;
 #pragma unroll 1
         for (int s = 0; s < 4; ++s) {
             const bool in = k + 8 * s < p.K;
@@ -598,11 +603,11 @@ template <int NB, int E, int F> static hipError_t wide_go(const PackedMmParams& 
 // and 51 c for more (128 x 128), 110 c (256 x 192), 128 c (256 x 256; 146 when every unit has one).  Measured, the best and the next: 32 x 11008 x
 // 4096 17.8 (32 x 32) and 19.6; 64 x 11008 x 4096 20.9 (64 x 64) and 23.0; 128 x 4096 x 4096 14.5 (64 x 32) and 18.7; 512 x 4096 x 4096 39 (128 x 32)
 // and 42; 1024 x 4096 x 4096 71 (128 x 128) and 77; 2048 x 11008 x 4096 212 (256 x 192) and 244; 4096 x 4096 x 4096 146 (256 x 256) and 199.  Codes
-// of 3 and 5 bits take up to a quarter more, in the same order.  Few rows: a workgroup of 16 columns reads x itself; one row through
-// 4096 x 11008 takes 11.7 us with the call, 17 to 20 by the narrow tiles.  Tables of pairs of 6-bit codes fit beside 128 x 128 tiles only.
+// of 3 and 5 bits take up to a quarter more, in the same order.  Up to 16 rows a workgroup takes 16 columns and reads x
+// itself: one row through 4096 x 11008 11.5 us, 20.9 by tiles of 32 x 32.  Tables of pairs of 6-bit codes fit beside 128 x 128 tiles only.
 template <int NB> static hipError_t packed_pick(const PackedMmParams& p, int n_cu, hipStream_t st)
 {
-    if (p.M <= 16) return rows_go<NB, 1, 3, 8>(p, st);
+    if (p.M <= 16) return rows_go<NB, 1, 2, 8>(p, st);
     auto each = [&](int bm, int bn) { return (float)(((long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) + n_cu - 1) / n_cu); };
     const float c22 = each(128, 128), never = 3.4e38f;
     const float cost[7] = {8.0f * each(32, 32) + 1.7f, 11.0f * each(64, 32) + 2.0f, 20.5f * each(64, 64), 19.5f * each(128, 32),
