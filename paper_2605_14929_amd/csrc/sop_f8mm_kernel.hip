@@ -44,6 +44,20 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
     }
 }
 
+// The last step of a K that is no multiple of 128: a row is read up to a multiple of 16, and what lies beyond K becomes zeros in LDS, `rows` rows
+// that thread `me` of `n` shares.
+__device__ __forceinline__ void clear_beyond(unsigned char* tile, int rows, int left, int me, int n)
+{
+#pragma unroll 4
+    for (int c = me; c < rows * 8; c += n) {
+        const int r = c >> 3, keep = left - (((c ^ r >> 1) & 7) << 4);
+        if (keep < 16) {
+            v4i* at = reinterpret_cast<v4i*>(tile + c * 16);
+            *at = keep_bytes(*at, keep);
+        }
+    }
+}
+
 // ---- tiles: BM x BN of y by WR x WC wavefronts, 128 elements along K a step, two steps in LDS.  A wavefront's part is made of 32 x 32
 // squares.  In LDS a row is eight chunks of 16 bytes, chunk c at position c ^ (row / 2 & 7): LDS serves a 16-byte read sixteen lanes at
 // a time (0-3, 12-15, 20-23 and 24-27, then the others of the first 32, ...), whose rows so fall on different banks.
@@ -73,8 +87,9 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
         const int c = i * NT + tid, r = c >> 3;
         ow[i] = (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw + (((c ^ r >> 1) & 7) << 4);
     }
-    const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
-    const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
+    const unsigned int readable = (unsigned int)((p.K + 15) & ~15);
+    const Window xw = window(xb, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)p.ldx + readable);
+    const Window ww = window(wb, (unsigned int)(min(BN, p.N - n0) - 1) * (unsigned int)p.ldw + readable);
     auto load = [&](int kt) {
         const unsigned int to = lds_address(lds) + (kt & 1) * STAGE + (wave << 10);
 #pragma unroll
@@ -177,29 +192,22 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
                          lds_address(lds) + 2 * STAGE + (wave & 3) * 256);
     };
     scales(0);
-    if (KF) load(0);
+    if (KB) load(0);
     if (AHEAD) ask_ahead(2);
     for (int kt = 0; kt < KF; ++kt) {
         wait_loads<AHEAD ? 1 : 0>();                                    // (all but the word asked for last)
         __syncthreads();                                                // this step has arrived, and nobody reads the other half any more
-        if (kt + 1 < KF) load(kt + 1);
+        if (kt + 1 < KB) load(kt + 1);
         if (AHEAD) ask_ahead(kt + 3);
         turn(kt);
         compute(kt);
     }
-    if (AHEAD) wait_loads();
-    if (KF < KB) {                                                      // the last step of an odd K: elements beyond it count as zeros
-        unsigned char* to = lds + (KF & 1) * STAGE;
-        const int left = p.K & 127;
-#pragma unroll 1
-        for (int c = tid; c < (BM + BN) * 8; c += NT) {
-            const bool of_x = c < BM * 8;
-            const int d = of_x ? c : c - BM * 8, r = d >> 3, col = ((d ^ r >> 1) & 7) << 4, n = left - col;
-            const unsigned char* row = of_x ? xb + (long long)min(r, p.M - 1 - m0) * p.ldx : wb + (long long)min(r, p.N - 1 - n0) * p.ldw;
-            v4i v = {0, 0, 0, 0};
-            if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + col), n);
-            *reinterpret_cast<v4i*>(to + c * 16) = v;
-        }
+    wait_loads();
+    if (KF < KB) {
+        __syncthreads();
+        unsigned char* at = lds + (KF & 1) * STAGE;
+        clear_beyond(at, BM, p.K & 127, tid, NT);
+        clear_beyond(at + BM * 128, BN, p.K & 127, tid, NT);
         __syncthreads();
         turn(KF);
         compute(KF);
@@ -279,29 +287,38 @@ __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, i
                 for (int b = 0; b < FN; ++b) acc[a][b] = mfma_f8<XF>(w[b], x[a], acc[a][b], sw[b], sx[a]);
         }
     };
-    int kt = wave;
-    for (; kt + (U - 1) * W < KF; kt += U * W) {                        // U steps in flight
-        v8i x[U][FM], w[U][FN];
-        int sx[U][FM], sw[U][FN];
+    struct Step { v8i x[FM], w[FN]; int sx[FM], sw[FN]; };
+    auto load = [&](int kt, Step& z) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int b = 0; b < FN; ++b) { z.w[b] = whole(wr[b], kt); z.sw[b] = wsr[b][(long long)kt * p.ws_k]; }
 #pragma unroll
-            for (int b = 0; b < FN; ++b) { w[u][b] = whole(wr[b], kt + u * W); sw[u][b] = wsr[b][(long long)(kt + u * W) * p.ws_k]; }
+        for (int a = 0; a < FM; ++a) { z.x[a] = whole(xr[a], kt); z.sx[a] = xsr[a][kt]; }
+    };
+    // U steps in flight all the time; what the last batch has beyond the wavefront's steps is asked for again and not added
+    const int mine = wave < KF ? (KF - wave + W - 1) / W : 0, batches = (mine + U - 1) / U;
+    if (mine) {
+        Step z[U];
 #pragma unroll
-            for (int a = 0; a < FM; ++a) { x[u][a] = whole(xr[a], kt + u * W); sx[u][a] = xsr[a][kt + u * W]; }
+        for (int u = 0; u < U; ++u) load(wave + min(u, mine - 1) * W, z[u]);
+#pragma unroll 1
+        for (int c = 1; c < batches; ++c) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                add(z[u].x, z[u].w, z[u].sx, z[u].sw);
+                load(wave + min(c * U + u, mine - 1) * W, z[u]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) add(x[u], w[u], sx[u], sw[u]);
+        for (int u = 0; u < U; ++u) if ((batches - 1) * U + u < mine) add(z[u].x, z[u].w, z[u].sx, z[u].sw);
     }
-#pragma unroll 1
-    for (; kt < KB; kt += W) {
-        v8i x[FM], w[FN];
-        int sx[FM], sw[FN];
+    if (KF < KB && wave == KF % W) {
+        Step z;
 #pragma unroll
-        for (int b = 0; b < FN; ++b) { w[b] = kt < KF ? whole(wr[b], kt) : rest(wr[b]); sw[b] = wsr[b][(long long)kt * p.ws_k]; }
+        for (int b = 0; b < FN; ++b) { z.w[b] = rest(wr[b]); z.sw[b] = wsr[b][(long long)KF * p.ws_k]; }
 #pragma unroll
-        for (int a = 0; a < FM; ++a) { x[a] = kt < KF ? whole(xr[a], kt) : rest(xr[a]); sx[a] = xsr[a][kt]; }
-        add(x, w, sx, sw);
+        for (int a = 0; a < FM; ++a) { z.x[a] = rest(xr[a]); z.sx[a] = xsr[a][KF]; }
+        add(z.x, z.w, z.sx, z.sw);
     }
 #pragma unroll
     for (int a = 0; a < FM; ++a)
@@ -341,8 +358,9 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
         const int r = i * 8 + (lane >> 3), col = ((lane ^ r >> 1) & 7) << 4;
         off[i] = i < 4 * FM ? (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx + col : (unsigned int)min(r - 32 * FM, p.N - 1 - n0) * (unsigned int)p.ldw + col;
     }
-    const Window xw = window(xb, (unsigned int)(min(32 * FM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)KF * 128);
-    const Window ww = window(wb, (unsigned int)(min(32 * FN, p.N - n0) - 1) * (unsigned int)p.ldw + (unsigned int)KF * 128);
+    const unsigned int readable = (unsigned int)((p.K + 15) & ~15);
+    const Window xw = window(xb, (unsigned int)(min(32 * FM, p.M - m0) - 1) * (unsigned int)p.ldx + readable);
+    const Window ww = window(wb, (unsigned int)(min(32 * FN, p.N - n0) - 1) * (unsigned int)p.ldw + readable);
     unsigned int sx[FM], sw[FN], nx[FM], nw[FN];
     const unsigned char* xsr[FM];
     const unsigned char* wsr[FN];
@@ -355,20 +373,8 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
         for (int a = 0; a < FM; ++a) nx[a] = xsr[a][kt];
 #pragma unroll
         for (int b = 0; b < FN; ++b) nw[b] = wsr[b][(long long)kt * p.ws_k];
-        if (kt < KF) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) load_to_lds(i < 4 * FM ? xw : ww, off[i], kt * 128, own0 + i * 1024);
-        } else {                                                        // the last step of an odd K: elements beyond it count as zeros
-            const int left = p.K & 127;
-#pragma unroll 1
-            for (int c = lane; c < ROWS * 8; c += 64) {
-                const int r = c >> 3, col = ((c ^ r >> 1) & 7) << 4, n = left - col;
-                const unsigned char* row = r < 32 * FM ? xb + (long long)min(r, p.M - 1 - m0) * p.ldx : wb + (long long)min(r - 32 * FM, p.N - 1 - n0) * p.ldw;
-                v4i v = {0, 0, 0, 0};
-                if (n > 0) v = keep_bytes(*reinterpret_cast<const v4i*>(row + (long long)KF * 128 + col), n);
-                *reinterpret_cast<v4i*>(own + c * 16) = v;
-            }
-        }
+        for (int i = 0; i < LOADS; ++i) load_to_lds(i < 4 * FM ? xw : ww, off[i], kt * 128, own0 + i * 1024);
     };
     v16f acc[FM][FN];
 #pragma unroll
@@ -391,6 +397,7 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
         for (int a = 0; a < FM; ++a) { sx[a] = nx[a]; asm volatile("" : "+v"(sx[a])); }
 #pragma unroll
         for (int b = 0; b < FN; ++b) { sw[b] = nw[b]; asm volatile("" : "+v"(sw[b])); }
+        if (kt == KF) clear_beyond(own, ROWS, p.K & 127, lane, 64);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -472,11 +479,12 @@ template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t ro
 // bf16 results: by c workgroups each, the narrow tiles take 4 c + 2 (32 x 32), 6.5 c + 1.5 (32 x 64), 9.3 c + 1 (64 x 64); tiles of 64 x 128 22 for
 // one and 14.2 c for more, of 128 x 128 30 for one and 41 for every two, of 256 x 256 66 c.  Where the choice falls wrong it costs little: measured,
 // the best and the next at 300 x 4096 x 4096: 19.0 and 20.1 us; 1024 x 4096 x 4096: 27.2 (64 x 128) and 30.5 (128 x 128); 777 x 5000 x 3000: 30.7
-// (128 x 128) and 34.7; 1024 x 11008 x 4096: 66 (256 x 256) and 76 (64 x 128).  Up to eight rows operands go straight to
-// registers, four steps in flight: 9.8 us for one row through 4096 x 11008, 10.6 by 32 x 32 tiles; sixteen rows 12.7 and 11.1.
+// (128 x 128) and 34.7; 1024 x 11008 x 4096: 66 (256 x 256) and 76 (64 x 128).  Up to four rows operands go straight to
+// registers, two steps in flight: one row through 28672 x 8192 takes 41 us, 45 by 32 x 32 tiles, through 4096 x 11008 9.8 and 10.1; eight rows
+// through 11008 x 4096 12.7 and 9.7.
 template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int n_cu, hipStream_t st)
 {
-    if (p.M <= 8) return rows_go<1, 1, 4, 8, XF, EXACT>(p, st);
+    if (p.M <= 4) return rows_go<1, 1, 2, 8, XF, EXACT>(p, st);
     auto each = [&](int bm, int bn) { return (float)(((long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) + n_cu - 1) / n_cu); };
     const float c11 = each(32, 32), c12 = each(32, 64), c22 = each(64, 64), c24 = each(64, 128), c44 = each(128, 128), c88 = each(256, 256);
     const float cost[6] = {4.0f * c11 + 2.0f, 6.5f * c12 + 1.5f, 9.3f * c22 + 1.0f, c24 <= 1.0f ? 22.0f : 14.2f * c24, c44 <= 1.0f ? 30.0f : 20.5f * (c44 + (float)((long long)c44 & 1)),
