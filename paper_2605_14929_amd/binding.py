@@ -309,8 +309,9 @@ def _up(n, unit):
 
 
 def _spaced(t, unit, what):
-    """A 2-D tensor of bytes as the library reads it: rows a multiple of `unit` bytes apart that may be read to a multiple of `unit`.
-    The tensor itself if it is laid out so, else a copy that is; and the distance of its rows."""
+    """A 2-D tensor of bytes as the library reads it: rows that start on a multiple of `unit` bytes (and may so be read to one: such a piece
+    with a byte of the tensor in it lies on a page of its memory).  The tensor itself if it is laid out so, else a copy that is; and the
+    distance of its rows."""
     import torch
     if t.dim() != 2 or t.element_size() != 1 or not t.is_cuda:
         raise SopError(1, f"{what} must be a 2-D CUDA tensor of one byte an element")
@@ -318,8 +319,7 @@ def _spaced(t, unit, what):
     ld, step = t.stride()
     if R <= 1:
         ld = _up(Cc, unit)
-    if (step == 1 or Cc <= 1) and ld >= Cc and ld % unit == 0 and t.data_ptr() % unit == 0 and \
-            (Cc % unit == 0 or t.untyped_storage().nbytes() - t.storage_offset() >= (R - 1) * ld + _up(Cc, unit)):
+    if (step == 1 or Cc <= 1) and ld >= Cc and ld % unit == 0 and t.data_ptr() % unit == 0:
         return t, ld
     ld = _up(Cc, unit)
     buf = torch.zeros((R, ld), dtype=torch.uint8, device=t.device)
@@ -330,8 +330,7 @@ def _spaced(t, unit, what):
 def _room(torch, R, Cc, unit, dtype, device):
     """An uninitialised [R, Cc] of bytes laid out so, and the distance of its rows."""
     ld = -(-Cc // unit) * unit
-    t = torch.empty((R, ld), dtype=dtype, device=device)
-    return (t if ld == Cc else t[:, :Cc]), ld
+    return torch.empty_strided((R, Cc), (ld, 1), dtype=dtype, device=device), ld
 
 
 class Fp8Blocks:
