@@ -1,6 +1,7 @@
 """MI355X-native pair search of "Scaled Outer Product": thin Python binding over libsop_hip.so.
 
-Every step of the search runs in the HIP kernels of the shared library; this package only loads
+Every step of the search, and the products of linear layers with narrow operands (8-bit floats under block
+scales, packed codebook weights), run in the HIP kernels of the shared library; this package only loads
 it, marshals arguments and hands PyTorch device pointers and streams across the C boundary.
 There is no CPU fallback: importing works anywhere, calling needs the built library and a GPU.
 """

@@ -189,7 +189,8 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
 // ---- narrow tiles, K dealt out: 32 FM x 32 FN of y a workgroup, its eight wavefronts taking steps of 64 S elements in turn.  A wavefront has its
 // step of x in a place of its own in LDS (no barrier before the sums are joined), and forms the weights in the registers that the matrix
 // instructions read: a lane takes 32 neighbouring codes of its row, eight for each of four instructions, and the same elements of x.  The next
-// step is asked for when this one's operands have been read.
+// step is asked for when this one's operands have been read.  128 x 4096 x 4096 of 4-bit codes takes 14.5 us (wide tiles of 128 x 128: 60), 32 x 11008
+// x 4096 17.8: forming the weights once for 32 to 128 rows bounds it.
 template <int NB, int FM, int FN, int S, int WPL>
 __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
@@ -328,8 +329,9 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
 // two barriers (4 E F matrix instructions) every thread forms 16 F weights of the step after the next, eight by eight: behind each matrix
 // instruction stand a part of the look-ups and of the scale word of an eight, and a part of the products of the eight before.  A matrix
 // instruction (32 cycles) hides seven others of its wavefront, so what a weight costs in instructions is what counts: two codes
-// are looked up at once, in a table of the 4^NB pairs of either codebook.  Before its last sixteen elements through a step comes its barrier: the
-// next step is there, this one's place is free.
+// are looked up at once, in a table of the 4^NB pairs of either codebook.  Before a step's last sixteen elements comes its barrier: the
+// next step is there, this one's place is free.  2048 x 11008 x 4096 of 4-bit codes takes 202 us, 913 TFLOP/s: matrix instructions are busy 40 % of the
+// cycles, the look-ups and products of the weights, once a tile, fill the others.
 template <int NB, int E, int F, bool G8>
 __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
