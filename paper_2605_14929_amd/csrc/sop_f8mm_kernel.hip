@@ -61,9 +61,10 @@ __device__ __forceinline__ void clear_beyond(unsigned char* tile, int rows, int 
 // ---- tiles: BM x BN of y by WR x WC wavefronts, 128 elements along K a step, two steps in LDS.  A wavefront's part is made of 32 x 32
 // squares.  In LDS a row is eight chunks of 16 bytes, chunk c at position c ^ (row / 2 & 7): LDS serves a 16-byte read sixteen lanes at
 // a time (0-3, 12-15, 20-23 and 24-27, then the others of the first 32, ...), whose rows so fall on different banks.  256 x 256 by eight
-// wavefronts: 8192 x 28672 x 8192 takes 1758 us (2190 TFLOP/s), 4096 x 4096 x 11008 162 us (2280).  The matrix instructions are busy half of the
-// cycles then, with no bank conflict: a step's loads, one step ahead (a third step has no room in LDS), are what wavefronts wait for.  Four
-// wavefronts of 128 x 128 with loads dealt out over a step were no faster once the operands change from call to call.
+// wavefronts: 8192 x 28672 x 8192 takes 1600 us (2410 TFLOP/s), 4096 x 4096 x 11008 157 us (2350).  With 128 of 256 compute units at work and power to
+// spare, a step takes 1.65 us: its loads alone 1.1 (64 KB a compute unit, with two steps in flight or one), its operands' reads and matrix instructions alone
+// 1.5, of which the instructions are 0.95.  Operands read two matrix instructions ahead, half of the workgroup a half-step behind the other, four
+// wavefronts of 128 x 128, and lines asked for into L2 ahead of the loads all took as long or longer.
 template <int BM, int BN, int WR, int WC, int XF, bool EXACT>
 __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
@@ -181,28 +182,14 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
         }
     };
 
-    // Wide tiles: the lines of three steps on come to L2 ahead of the loads that want them.  A row's line is asked for by one of the tiles in
-    // flight on this XCD that read it (four beside each other read the same rows of x, eight the same of w, the step says whose turn it is); the
-    // word that comes of it is dropped.  8192 x 8192 x 8192 takes 494 us so, 550 without; 4096 x 11008 x 4096 198 and 206.
-    constexpr bool AHEAD = BM == 256 && BN == 256;
-    auto ask_ahead = [&](int kt) {
-        const bool of_x = wave < WR * WC / 2;
-        const bool ours = kt < KF && (of_x ? ((tn ^ kt) & 3) == 0 : ((tm ^ kt) & 7) == 0);
-        Window a = of_x ? xw : ww;
-        a.r[2] = ours ? a.r[2] : 0;
-        const int r = tid & 255;
-        load_word_to_lds(a, of_x ? (unsigned int)min(r, p.M - 1 - m0) * (unsigned int)p.ldx : (unsigned int)min(r, p.N - 1 - n0) * (unsigned int)p.ldw, kt * 128,
-                         lds_address(lds) + 2 * STAGE + (wave & 3) * 256);
-    };
     scales(0);
     if (KB) load(0);
-    if (AHEAD) ask_ahead(2);
     for (int kt = 0; kt < KF; ++kt) {
-        wait_loads<AHEAD ? 1 : 0>();                                    // (all but the word asked for last)
+        wait_loads();
         __syncthreads();                                                // this step has arrived, and nobody reads the other half any more
+        turn(kt);                                                       // (before the loads: to have its words is to wait for all that was asked for)
+        __builtin_amdgcn_sched_barrier(0);
         if (kt + 1 < KB) load(kt + 1);
-        if (AHEAD) ask_ahead(kt + 3);
-        turn(kt);
         compute(kt);
     }
     wait_loads();
@@ -454,7 +441,7 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
 
 template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t tile_go(const F8MmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128 + (BM == 256 && BN == 256 ? 1024 : 0);
+    const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128;
     auto fn = &f8mm_tile_kernel<BM, BN, WR, WC, XF, EXACT>;
     if (bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -481,10 +468,10 @@ template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t ro
     return hipGetLastError();
 }
 // The kernel that is expected to take least, from how many workgroups a compute unit gets.  Microseconds at K = 4096 on 256 compute units,
-// bf16 results: by c workgroups each, the narrow tiles take 4 c + 2 (32 x 32), 6.5 c + 1.5 (32 x 64), 9.3 c + 1 (64 x 64); tiles of 64 x 128 22 for
-// one and 14.2 c for more, of 128 x 128 30 for one and 41 for every two, of 256 x 256 66 c.  Where the choice falls wrong it costs little: measured,
-// the best and the next at 300 x 4096 x 4096: 19.0 and 20.1 us; 1024 x 4096 x 4096: 27.2 (64 x 128) and 30.5 (128 x 128); 777 x 5000 x 3000: 30.7
-// (128 x 128) and 34.7; 1024 x 11008 x 4096: 66 (256 x 256) and 76 (64 x 128).  Up to four rows operands go straight to
+// bf16 results: by c workgroups each, the narrow tiles take 4 c + 2 (32 x 32), 6.5 c + 1.5 (32 x 64), 9.3 c + 1 (64 x 64); tiles of 64 x 128 23 for
+// one and 13.5 c for more, of 128 x 128 29 for one and 38.5 for every two, of 256 x 256 60 c.  Where the choice falls wrong it costs little: measured,
+// the best and the next at 300 x 4096 x 4096: 19.0 and 20.1 us; 1024 x 4096 x 4096: 27.9 (64 x 128) and 30.5 (128 x 128); 777 x 5000 x 3000: 31
+// (128 x 128) and 37; 1024 x 11008 x 4096: 60 (256 x 256) and 70 (64 x 128).  Up to four rows operands go straight to
 // registers, two steps in flight: one row through 28672 x 8192 takes 41 us, 45 by 32 x 32 tiles, through 4096 x 11008 9.8 and 10.1; eight rows
 // through 11008 x 4096 12.7 and 9.7.
 template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int n_cu, hipStream_t st)
@@ -492,8 +479,8 @@ template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int n_cu
     if (p.M <= 4) return rows_go<1, 1, 2, 8, XF, EXACT>(p, st);
     auto each = [&](int bm, int bn) { return (float)(((long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) + n_cu - 1) / n_cu); };
     const float c11 = each(32, 32), c12 = each(32, 64), c22 = each(64, 64), c24 = each(64, 128), c44 = each(128, 128), c88 = each(256, 256);
-    const float cost[6] = {4.0f * c11 + 2.0f, 6.5f * c12 + 1.5f, 9.3f * c22 + 1.0f, c24 <= 1.0f ? 22.0f : 14.2f * c24, c44 <= 1.0f ? 30.0f : 20.5f * (c44 + (float)((long long)c44 & 1)),
-                           EXACT ? 3.4e38f : 66.0f * c88};
+    const float cost[6] = {4.0f * c11 + 2.0f, 6.5f * c12 + 1.5f, 9.3f * c22 + 1.0f, c24 <= 1.0f ? 23.0f : 13.5f * c24, c44 <= 1.0f ? 29.0f : 19.25f * (c44 + (float)((long long)c44 & 1)),
+                           EXACT ? 3.4e38f : 60.0f * c88};
     int best = 0;
     for (int i = 1; i < 6; ++i) best = cost[i] < cost[best] ? i : best;
     switch (best) {
