@@ -784,6 +784,12 @@ class Context:
 
     # ---- products of a linear layer with narrow operands (calls of a few microseconds: their Python side is kept short)
 
+    def _on(self, stream, call, *args, **kw):
+        """The call with `stream` (a handle) as torch's current stream: what it allocates is then that stream's too."""
+        import torch
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device)):
+            return call(*args, **kw)
+
     def _here(self, *matrices):
         for q in matrices:
             if q.device != self.device:
@@ -818,13 +824,15 @@ class Context:
     def fp8_quantize(self, x, rows: int = 1, fmt=E4M3, transposed: bool = False, stream=None) -> Fp8Blocks:
         """sop_fp8_quantize: x [M, K] float32 or bfloat16 into 8 bits (fmt: E4M3 / E5M2, or the torch type) with one power-of-two scale for
         each block of rows x 128.  transposed (rows = 128 only): the codes as a [K, M] matrix too."""
+        if stream is not None:
+            return self._on(stream, self.fp8_quantize, x, rows, fmt, transposed)
         dt, ldx = self._numbers(x, "x")
         if transposed and rows != 128:
             raise SopError(1, "a transposed copy is made of 128 x 128 blocks only")
         M, K = x.shape
         q = Fp8Blocks.empty(M, K, fmt, x.device, rows, transposed)
         s = self._lib.sop_fp8_quantize(self._h, x.data_ptr(), dt, M, K, ldx, q._m, q._t.codes if transposed else None, q._t.ld_codes if transposed else 0,
-                                       self._raw_stream(self.device) if stream is None else stream)
+                                       self._raw_stream(self.device))
         if s:
             _check(s, self._h)
         return q
@@ -832,6 +840,8 @@ class Context:
     def fp8_matmul(self, x: Fp8Blocks, w: Fp8Blocks, transposed: bool = False, dtype=None, out=None, stream=None):
         """sop_fp8_matmul: y = x w^T of x [M, K] (rows = 1) and w [N, K] (rows = 128); transposed: y = x w of x [M, N] and the same w by its
         codes_t (the input gradient).  dtype: bfloat16 (default) or float32; or `out`, a matrix of either type to write to."""
+        if stream is not None:
+            return self._on(stream, self.fp8_matmul, x, w, transposed, dtype, out)
         self._here(x, w)
         if transposed and w._t is None:
             raise SopError(1, "the transposed product needs the weight's codes_t (fp8_quantize(..., transposed=True))")
@@ -841,7 +851,7 @@ class Context:
             raise SopError(2, f"x has rows of {K} elements, the weight wants {Kw}")
         out, dt, ldy = self._result(out, M, N, dtype or self._bf16, x.codes)
         s = self._lib.sop_fp8_matmul(self._h, x._m, w._t if transposed else w._m, transposed, M, N, K, out.data_ptr(), dt, ldy,
-                                     self._raw_stream(self.device) if stream is None else stream)
+                                     self._raw_stream(self.device))
         if s:
             _check(s, self._h)
         return out
@@ -849,6 +859,8 @@ class Context:
     def fp8_weight_grad(self, dy, x: Fp8Blocks, dtype=None, out=None, accumulate: bool = False, stream=None):
         """sop_fp8_weight_grad: dw [N, K] = dy^T x from dy [M, N] bfloat16 and the 8-bit checkpoint x [M, K] (rows = 1); dtype: float32 (default)
         or bfloat16; accumulate: added to `out`."""
+        if stream is not None:
+            return self._on(stream, self.fp8_weight_grad, dy, x, dtype, out, accumulate)
         self._here(x)
         _, lddy = self._numbers(dy, "dy", True)
         (M, N), K = dy.shape, x.shape[1]
@@ -858,13 +870,15 @@ class Context:
             raise SopError(1, "accumulate needs out")
         out, dt, ldw = self._result(out, N, K, dtype or self._f32, dy)
         s = self._lib.sop_fp8_weight_grad(self._h, dy.data_ptr(), lddy, x._m, M, N, K, out.data_ptr(), dt, ldw, accumulate,
-                                          self._raw_stream(self.device) if stream is None else stream)
+                                          self._raw_stream(self.device))
         if s:
             _check(s, self._h)
         return out
 
     def fp8_gated(self, gate, up, fmt=E4M3, stream=None):
         """sop_fp8_gated: (h, gate8, up8) of gate, up [M, F]: h = silu(gate) * up in 8 bits, and the 8-bit checkpoints of gate and up."""
+        if stream is not None:
+            return self._on(stream, self.fp8_gated, gate, up, fmt)
         dt, ldg = self._numbers(gate, "gate")
         du, ldu = self._numbers(up, "up")
         if gate.shape != up.shape or dt != du:
@@ -873,13 +887,15 @@ class Context:
         dev = gate.device
         h, g8, u8 = Fp8Blocks.empty(M, F, fmt, dev), Fp8Blocks.empty(M, F, fmt, dev), Fp8Blocks.empty(M, F, fmt, dev)
         s = self._lib.sop_fp8_gated(self._h, gate.data_ptr(), ldg, up.data_ptr(), ldu, dt, M, F, h._m, g8._m, u8._m,
-                                    self._raw_stream(self.device) if stream is None else stream)
+                                    self._raw_stream(self.device))
         if s:
             _check(s, self._h)
         return h, g8, u8
 
     def fp8_gated_grad(self, gate8: Fp8Blocks, up8: Fp8Blocks, dh, fmt=E5M2, stream=None):
         """sop_fp8_gated_grad: (dgate, dup, dgate8, dup8) from the checkpoints of fp8_gated and dh [M, F]: numbers of dh's type, and 8 bits."""
+        if stream is not None:
+            return self._on(stream, self.fp8_gated_grad, gate8, up8, dh, fmt)
         self._here(gate8, up8)
         dt, ldd = self._numbers(dh, "dh")
         M, F = dh.shape
@@ -889,13 +905,15 @@ class Context:
         dgate, dup = dh.new_empty((M, F)), dh.new_empty((M, F))
         g8, u8 = Fp8Blocks.empty(M, F, fmt, dev), Fp8Blocks.empty(M, F, fmt, dev)
         s = self._lib.sop_fp8_gated_grad(self._h, gate8._m, up8._m, dh.data_ptr(), ldd, dt, M, F, dgate.data_ptr(), F, dup.data_ptr(), F, g8._m, u8._m,
-                                         self._raw_stream(self.device) if stream is None else stream)
+                                         self._raw_stream(self.device))
         if s:
             _check(s, self._h)
         return dgate, dup, g8, u8
 
     def packed_matmul(self, x, w: PackedWeights, out=None, stream=None):
         """sop_packed_matmul: y [M, N] bfloat16 = x w^T of x [M, K] bfloat16 and a packed layer."""
+        if stream is not None:
+            return self._on(stream, self.packed_matmul, x, w, out)
         self._here(w)
         _, ldx = self._numbers(x, "x", True)
         (M, K), (N, Kw) = x.shape, w.shape
@@ -904,7 +922,7 @@ class Context:
         out, dt, ldy = self._result(out, M, N, self._bf16, x)
         if dt != BF16:
             raise SopError(1, "out must be bfloat16")
-        s = self._lib.sop_packed_matmul(self._h, x.data_ptr(), ldx, w._w, M, out.data_ptr(), ldy, self._raw_stream(self.device) if stream is None else stream)
+        s = self._lib.sop_packed_matmul(self._h, x.data_ptr(), ldx, w._w, M, out.data_ptr(), ldy, self._raw_stream(self.device))
         if s:
             _check(s, self._h)
         return out

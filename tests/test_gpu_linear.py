@@ -554,3 +554,29 @@ def test_missing_numbers_stay_in_their_block(M, N, K):
     for dtype in (torch.float32, torch.bfloat16):
         y = _np(ctx().fp8_matmul(good, _f8(wc, ws, 128, "E4M3"), dtype=dtype))
         assert np.isnan(y[:, :128]).all() and np.isfinite(y[:, 128:]).all()
+
+
+def test_a_given_stream_holds_the_call_and_its_results():
+    """stream=handle: the kernels run there, ordered after what is queued there, and results are that stream's to allocate."""
+    import torch
+    cx = ctx()
+    rng = np.random.default_rng(14)
+    M, N, K = 50, 300, 520
+    x, w = _t(_spread(rng, M, K), "bf16"), _t(_spread(rng, N, K))
+
+    def step(**kw):
+        wq, q = cx.fp8_quantize(w, rows=128, transposed=True, **kw), cx.fp8_quantize(x, **kw)
+        y = cx.fp8_matmul(q, wq, **kw)
+        h, g8, u8 = cx.fp8_gated(y, y, **kw)
+        dg, du, dg8, du8 = cx.fp8_gated_grad(g8, u8, y, **kw)
+        return y, h.codes, dg, du8.codes, cx.fp8_weight_grad(y, q, **kw), cx.fp8_matmul(du8, wq, transposed=True, **kw)
+
+    plain = [_bytes(t.contiguous()) if t.element_size() == 1 else _np(t) for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(stream=side.cuda_stream)
+    side.synchronize()
+    for a, b in zip(plain, got):
+        assert np.array_equal(a, _bytes(b.contiguous()) if b.element_size() == 1 else _np(b))
+    for a, b in zip(plain, step(stream=0)):                             # the default stream
+        assert np.array_equal(a, _bytes(b.contiguous()) if b.element_size() == 1 else _np(b))
