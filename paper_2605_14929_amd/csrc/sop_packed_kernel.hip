@@ -330,7 +330,7 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
 // instruction stand a part of the look-ups and of the scale word of an eight, and a part of the products of the eight before.  A matrix
 // instruction (32 cycles) hides seven others of its wavefront, so what a weight costs in instructions is what counts: two codes
 // are looked up at once, in a table of the 4^NB pairs of either codebook.  Before a step's last sixteen elements comes its barrier: the
-// next step is there, this one's place is free.  2048 x 11008 x 4096 of 4-bit codes takes 202 us, 913 TFLOP/s: matrix instructions are busy 40 % of the
+// next step is there, this one's place is free.  2048 x 11008 x 4096 of 4-bit codes takes 203 us, 910 TFLOP/s: matrix instructions are busy 40 % of the
 // cycles, the look-ups and products of the weights, once a tile, fill the others.
 template <int NB, int E, int F, bool G8>
 __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)

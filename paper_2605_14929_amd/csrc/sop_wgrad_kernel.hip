@@ -9,7 +9,7 @@
 // both go to LDS as they are, straight from memory, and are turned by LDS's transposing reads (a sixteen-lane group reads four rows of
 // sixteen 16-bit, or eight rows of sixteen 8-bit elements and receives the columns); the checkpoint stays in 8 bits until then.
 // Otherwise a thread loads eight rows of two (dy) or four (x) columns, turns them in registers, and writes columns (8192 x 11008 x 4096 in the simple
-// form of that 1388 us, by the transposing reads 643).
+// form of that 1388 us, by the transposing reads 647).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -177,7 +177,7 @@ template <bool E5M2, bool HIGH> __device__ __forceinline__ int two_rows(int c, f
 
 // ---- rows of dy on 16 bytes.  64 rows a step, three steps in LDS: one being multiplied, one on its way or there, one being asked for.
 // In LDS a row is chunks of 16 bytes; chunk c of row m stands at position c ^ 4 (m & 3) (dy), c ^ 2 (m & 7) (x, rows of 256 bytes) or
-// c ^ 2 (m / 2 & 3) (x, rows of 128), so that the rows that 32 lanes read together fall on different banks.  777 x 1531 x 5024 takes 22.6 us: thirteen
+// c ^ 2 (m / 2 & 3) (x, rows of 128), so that the rows that 32 lanes read together fall on different banks.  777 x 1531 x 5024 takes 22 us: thirteen
 // steps of two workgroups a compute unit (12 us), 31 MB of results (6 us), and the first loads.
 template <int BN, int BK, int WR, int WC, bool X5>
 __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
@@ -441,8 +441,8 @@ __global__ __launch_bounds__(512) void wgrad_split_kernel(const WgradParams p, i
 // work.  While sixteen rows are multiplied (sixteen matrix instructions), behind each of them stands a sixteenth of: the reads of the next
 // sixteen rows of dy, the reads of the codes after the next, the conversion of the next codes, the loads of the step after the next.  A
 // wavefront issues an instruction in four cycles, so a matrix instruction (32 cycles) hides seven others: they are dealt out evenly.
-// Halfway through a step comes its barrier: the next step has arrived, the place of the step before is free.  8192 x 11008 x 4096 takes 643 us,
-// 1150 TFLOP/s (a large library product in bf16 1450); the matrix instructions are busy 57 % of the cycles at a clock that they lower.
+// Halfway through a step comes its barrier: the next step has arrived, the place of the step before is free.  8192 x 11008 x 4096 takes 647 us,
+// 1140 TFLOP/s (a large library product in bf16 1450); the matrix instructions are busy 57 % of the cycles at a clock that they lower.
 template <bool X5>
 __global__ __launch_bounds__(256) void wgrad_large_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
 {
@@ -636,7 +636,7 @@ template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_go(co
 // The kernel that is expected to take least, from how many workgroups c a compute unit gets and how many times 64 rows there are (t).
 // Microseconds on 256 compute units, 32-bit results: the rows dealt out 1.4 + c (1.2 + 0.16 t) (32 x 64) and 1.2 + c (2.9 + 0.21 t) (64 x 64);
 // 128 x 128 4.4 + 0.82 t for one and c (4 + 0.6 t) for more; 256 x 256 c (19 + 1.65 t).  Measured (rows x N x K), the best and the next:
-// 8192 x 512 x 512 24 (32 x 64) and 33, by 128 x 128 107; 8192 x 1024 x 1024 32 (64 x 64) and 49; 777 x 1531 x 5024 23 (128 x 128) and 32;
+// 8192 x 512 x 512 24 (32 x 64) and 33, by 128 x 128 107; 8192 x 1024 x 1024 32 (64 x 64) and 49; 777 x 1531 x 5024 23 (128 x 128) and 30;
 // 2048 x 4096 x 4096 72 (256 x 256) and 92; 500 x 8192 x 4096 67 (256 x 256) and 71.
 template <bool X5> static hipError_t wgrad_pick(const WgradParams& p, int n_cu, hipStream_t st)
 {
