@@ -35,8 +35,11 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
             for (int i = 0; i < 4; ++i) if (n + i < p.N) y[i] = (uint16_t)bf16_bits(v[i]);
         }
     } else {
+        // whole lines are written past the caches: 4096 x 11008 x 512 takes 65 us so, 79 otherwise; 1460 x 5296 x 288 14.9 and 14.6
+        const bool lines = ((reinterpret_cast<uintptr_t>(p.y) | (unsigned long long)p.ldy * 4) & 127) == 0;
         float* y = reinterpret_cast<float*>(p.y) + at;
-        if (n + 3 < p.N) put_four(y, v);
+        if (n + 3 < p.N && lines) __builtin_nontemporal_store(v, reinterpret_cast<v4f*>(y));
+        else if (n + 3 < p.N) put_four(y, v);
         else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) if (n + i < p.N) y[i] = v[i];
