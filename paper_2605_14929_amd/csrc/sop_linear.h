@@ -61,6 +61,22 @@ struct PackedMmParams {
 };
 
 #if defined(__HIPCC__)
+#define SOP_HD __host__ __device__ inline
+#else
+#define SOP_HD inline
+#endif
+/* What the wide packed kernel adds, the same for all lanes, to its lanes' offsets into its three windows at step t (64 elements along K each).  It asks
+ * for two steps more than there are.  A window's check compares a lane's offset with what the window has left beyond this sum, so the sum
+ * never passes the window's end, which with one row left is the end of K: the steps behind the last one ask for the last one again. */
+struct PackedStepAt { int x, codes, words; };                              // bytes
+SOP_HD PackedStepAt packed_step_at(int t, int steps, int nb, int lg, bool half)
+{
+    const bool end = t >= steps - 1;                                       // half: K ends in the middle of sixteen codes, and the last step's begin eight earlier
+    const int k = end ? steps - 1 : t;
+    return PackedStepAt{k * 128, k * 8 * nb - (half && end ? nb : 0), k * (128 >> lg)};
+}
+
+#if defined(__HIPCC__)
 namespace sopk {
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef int v4i __attribute__((ext_vector_type(4)));

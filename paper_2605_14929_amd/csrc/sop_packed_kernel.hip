@@ -354,7 +354,7 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
 #pragma unroll
     for (int i = 0; i < XL; ++i) ox[i] = (unsigned int)min(i * 32 + (tid >> 3), p.M - 1 - m0) * (unsigned int)(p.ldx * 2) + xcol;
     const Window xw = window(p.x + (long long)m0 * p.ldx, (unsigned int)(min(BM, p.M - m0) - 1) * (unsigned int)(p.ldx * 2) + (unsigned int)p.K * 2);
-    auto load_x = [&](int t, int i) { load_to_lds(xw, ox[i], t * 128, lds0 + (t & 1) * STAGE + (wave << 10) + i * 4096); };
+    auto load_x = [&](int t, int i) { load_to_lds(xw, ox[i], packed_step_at(t, steps, NB, lg, false).x, lds0 + (t & 1) * STAGE + (wave << 10) + i * 4096); };
     // w: an item is sixteen codes of a row, four items a row and step, F of a thread
     const int rows = min(BN, p.N - n0), k16 = (tid & 3) * 16;
     const unsigned int prow = (unsigned int)(p.K >> 3) * NB, wrow = (unsigned int)(p.K >> lg) * 2u;
@@ -402,7 +402,8 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
     };
     struct Item { unsigned int c[CW], w[WORDS]; };
     auto load_w = [&](Item& z, int t, int i) {
-        const int at = t * 8 * NB - (half && t == steps - 1 ? NB : 0);
+        const PackedStepAt step = packed_step_at(t, steps, NB, lg, half);
+        const int at = step.codes;
         if constexpr (NB / 2 == 1) z.c[0] = (unsigned int)__builtin_amdgcn_raw_buffer_load_b32(resource(pw), (int)op[i], at, 0);
         if constexpr (NB / 2 == 2) {
             const auto c = __builtin_amdgcn_raw_buffer_load_b64(resource(pw), (int)op[i], at, 0);
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
         }
         if constexpr (NB % 2 == 1) z.c[CW - 1] = __builtin_amdgcn_raw_buffer_load_b16(resource(pw), (int)op[i], at + NB / 2 * 4, 0);
 #pragma unroll
-        for (int h = 0; h < WORDS; ++h) z.w[h] = __builtin_amdgcn_raw_buffer_load_b16(resource(ww), (int)ow[i][h], t * (128 >> lg), 0);
+        for (int h = 0; h < WORDS; ++h) z.w[h] = __builtin_amdgcn_raw_buffer_load_b16(resource(ww), (int)ow[i][h], step.words, 0);
     };
 
     v16f acc[E][F];

@@ -580,3 +580,11 @@ def test_a_given_stream_holds_the_call_and_its_results():
         assert np.array_equal(a, _bytes(b.contiguous()) if b.element_size() == 1 else _np(b))
     for a, b in zip(plain, step(stream=0)):                             # the default stream
         assert np.array_equal(a, _bytes(b.contiguous()) if b.element_size() == 1 else _np(b))
+
+
+# tiles of one row and of one column at the end, K ending inside the last step: 256 x 192 (128 x 128 with 6 bits), 256 x 256, 128 x 128 of y a workgroup
+@pytest.mark.parametrize("n", [1, 3, 4, 5, 6])
+@pytest.mark.parametrize("K, g", [(72, 8), (136, 8), (80, 16), (96, 32), (192, 64)])
+@pytest.mark.parametrize("M, N", [(2049, 3841), (1025, 11009), (4097, 3841)])
+def test_packed_product_with_one_row_left(M, N, K, g, n):
+    test_packed_product((M, N, K, g, n, (0, 4, 3, 8), True, 0))
