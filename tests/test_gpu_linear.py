@@ -588,3 +588,47 @@ def test_a_given_stream_holds_the_call_and_its_results():
 @pytest.mark.parametrize("M, N", [(2049, 3841), (1025, 11009), (4097, 3841)])
 def test_packed_product_with_one_row_left(M, N, K, g, n):
     test_packed_product((M, N, K, g, n, (0, 4, 3, 8), True, 0))
+
+
+# Scales from 2^-127 to 2^127 whose product is moderate: whole numbers, exact in either type of result.  A size for each way of sharing y out:
+# up to four rows, tiles of 32 x 32, 32 x 64, 64 x 64, 64 x 128, 128 x 128 and (bf16 results alone) 256 x 256.
+@pytest.mark.parametrize("fmt", ["E4M3", "E5M2"])
+@pytest.mark.parametrize("a, b", [(252, 0), (0, 252), (60, 190), (1, 251), (9, 243), (245, 9), (15, 237), (238, 14)])
+@pytest.mark.parametrize("M, N, K", [(3, 130, 300), (40, 150, 300), (301, 1531, 300), (513, 1025, 300), (1001, 4090, 150), (2049, 2050, 150), (2300, 4700, 150)])
+def test_product_under_scales_of_any_size(M, N, K, a, b, fmt):
+    import torch
+    rng = np.random.default_rng(15)
+    (xc, xs), (wc, ws) = _integers(rng, M, K, 1, fmt), _integers(rng, N, K, 128)
+    xs, ws = (xs - 127 + a).astype(np.uint8), (ws - 127 + b).astype(np.uint8)
+    x, w = OL.values(xc, xs, 1, fmt), OL.values(wc, ws, 128, "E4M3")
+    ref = (torch.from_numpy(x).cuda() @ torch.from_numpy(w).cuda().t()).cpu().numpy()
+    x, w = _f8(xc, xs, 1, fmt), _f8(wc, ws, 128, "E4M3")
+    assert np.array_equal(_np(ctx().fp8_matmul(x, w, dtype=torch.float32)), ref)
+    assert np.array_equal(_np(ctx().fp8_matmul(x, w)), _bf16(ref))
+
+
+def test_product_of_the_smallest_numbers():
+    """Results among binary32's subnormal numbers, whole multiples of the least one."""
+    import torch
+    rng = np.random.default_rng(16)
+    for (M, N, K), a in ((d, a) for d in ((3, 130, 300), (40, 150, 300), (513, 1025, 300), (1001, 4090, 150), (2049, 2050, 150)) for a in (1, 50, 80)):
+        (xc, xs), (wc, ws) = _integers(rng, M, K, 1), _integers(rng, N, K, 128)
+        xs, ws = (xs - 127 + a).astype(np.uint8), (ws - 127 + 105 - a).astype(np.uint8)   # 2^-149 and up, with one small scale or two moderate ones
+        x, w = OL.values(xc, xs, 1, "E4M3"), OL.values(wc, ws, 128, "E4M3")
+        ref = (torch.from_numpy(x).cuda() @ torch.from_numpy(w).cuda().t()).cpu().numpy()
+        y = ctx().fp8_matmul(_f8(xc, xs, 1, "E4M3"), _f8(wc, ws, 128, "E4M3"), dtype=torch.float32)
+        assert np.array_equal(y.cpu().numpy().astype(np.float64), ref)
+
+
+def test_product_in_32_bits_drops_nothing_beside_a_large_product():
+    """Two products of 448 x 448 in every 128, of both signs, among products of 1 or 0: sums are whole and below 2^24 in any order, so exact in
+    binary32; on a grid of 2^-16 of the largest of eight (2 here) they would not be."""
+    import torch
+    rng = np.random.default_rng(17)
+    for M, N, K in ((3, 130, 4096), (40, 150, 4096), (301, 1531, 4096), (513, 1025, 4096), (1001, 4090, 1024), (2049, 2050, 1024)):
+        x, w = np.ones((M, K)), np.ones((N, K))
+        x[:, :] = rng.integers(-1, 2, (M, K))
+        x[:, ::128], x[:, 8::128], w[:, ::128], w[:, 8::128] = 448, -448, 448, 448
+        one = lambda r: np.full((r, K // 128), 127, np.uint8)  # noqa: E731
+        y = ctx().fp8_matmul(_f8(OL.encode(x, "E4M3"), one(M), 1, "E4M3"), _f8(OL.encode(w, "E4M3"), one(-(-N // 128)), 128, "E4M3"), dtype=torch.float32)
+        assert np.array_equal(_np(y), (torch.from_numpy(x).cuda() @ torch.from_numpy(w).cuda().t()).cpu().numpy())
