@@ -208,14 +208,31 @@ __global__ __launch_bounds__(256) void f8_square_kernel(const F8QuantParams p, i
 
 // ---- gated unit: s = 1 / (1 + exp(-g)), h = g s u
 // exp(-g) = 2^t (1 + r ln 2) with t the binary32 product of -g and log2(e), r what the product left: as exact as the hardware's 2^t.
-// Where 2^t is 0 or infinite (g beyond about 100 in magnitude), s is 1 or 0 to 32 bits and r says nothing.
+// Where 2^t is 0 (g beyond about 87), s is 1 to 32 bits; g is not below FAR_BELOW here, so that 2^t is finite and s a normal number.
+#define SOPK_L2E 1.44269504f                                            // log2(e) = L2E + L2E_LO
+#define SOPK_L2E_LO 1.9259630e-08f
+#define SOPK_FAR_BELOW (-64.0f)
 __device__ __forceinline__ float logistic(float g)
 {
-    const float L2E = 1.44269504f, L2E_LO = 1.9259630e-08f;             // log2(e) = L2E + L2E_LO
-    const float t = -g * L2E, r = __builtin_fmaf(-g, L2E, -t) - g * L2E_LO;
+    const float t = -g * SOPK_L2E, r = __builtin_fmaf(-g, SOPK_L2E, -t) - g * SOPK_L2E_LO;
     const float p = __builtin_amdgcn_exp2f(t);
-    const float q = p > 0.0f && p < 3.0e38f ? __builtin_fmaf(p, r * 0.693147181f, p) : p;
+    const float q = p > 0.0f ? __builtin_fmaf(p, r * 0.693147181f, p) : p;
     return __builtin_amdgcn_rcpf(1.0f + q);
+}
+// s for g below that, where it is exp(g) to 32 bits.  It leaves binary32's normal numbers at g = -87 and binary32 at -104, and a large factor
+// brings the product back into both: it is formed in binary64, whose smallest number lies at g = -745.
+__device__ __forceinline__ double logistic_far_below(float g)
+{
+    const float c = fmaxf(g, -1200.0f), t = c * SOPK_L2E, r = __builtin_fmaf(c, SOPK_L2E, -t) + c * SOPK_L2E_LO, i = rintf(t);
+    const float p = __builtin_amdgcn_exp2f(t - i);
+    return ldexp((double)__builtin_fmaf(p, r * 0.693147181f, p), (int)i);
+}
+__device__ __forceinline__ bool any_far_below(const float (&g)[8])
+{
+    float least = g[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) least = fminf(least, g[i]);             // (of NaN and a number, the number)
+    return least < SOPK_FAR_BELOW;
 }
 
 template <bool BF16, bool E5M2, bool VEC>
@@ -231,6 +248,10 @@ __global__ __launch_bounds__(256) void f8_gated_kernel(const F8GatedParams p, lo
         load8<BF16, VEC>(p.up, m * p.ldu + k, left, u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] = g[i] * logistic(g[i]) * u[i];
+        if (any_far_below(g)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (g[i] < SOPK_FAR_BELOW) h[i] = (float)((double)g[i] * logistic_far_below(g[i]) * (double)u[i]);
+        }
         quantize_row_block<E5M2>(h, p.h, m, k, left);
         quantize_row_block<E5M2>(g, p.g8, m, k, left);
         quantize_row_block<E5M2>(u, p.u8, m, k, left);
@@ -275,6 +296,16 @@ __global__ __launch_bounds__(256) void f8_gated_grad_kernel(const F8GatedGradPar
             const float s = logistic(g[i]), ds = d[i] * s;
             du[i] = ds * g[i];
             dg[i] = ds * u[i] * __builtin_fmaf(g[i], 1.0f - s, 1.0f);
+        }
+        if (any_far_below(g)) {                                         // (1 - s is 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (g[i] < SOPK_FAR_BELOW) {
+                    const double ds = (double)d[i] * logistic_far_below(g[i]);
+                    du[i] = (float)(ds * (double)g[i]);
+                    dg[i] = (float)(ds * (double)u[i] * (1.0 + (double)g[i]));
+                }
+            }
         }
         if (left > 0) {
             store8<BF16, VEC>(p.dgate, m * p.lddg + k, left, dg);

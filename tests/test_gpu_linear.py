@@ -632,3 +632,24 @@ def test_product_in_32_bits_drops_nothing_beside_a_large_product():
         one = lambda r: np.full((r, K // 128), 127, np.uint8)  # noqa: E731
         y = ctx().fp8_matmul(_f8(OL.encode(x, "E4M3"), one(M), 1, "E4M3"), _f8(OL.encode(w, "E4M3"), one(-(-N // 128)), 128, "E4M3"), dtype=torch.float32)
         assert np.array_equal(_np(y), (torch.from_numpy(x).cuda() @ torch.from_numpy(w).cuda().t()).cpu().numpy())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt", ["E4M3", "E5M2"])
+def test_gated_unit_far_below_zero(dtype, fmt):
+    """Gates from -60 to -130, where the logistic function leaves binary32, beside factors that bring the product back: a row's block has one gate."""
+    rng = np.random.default_rng(18)
+    M, F = 101, 136
+    g = np.repeat(np.linspace(-60, -130, M)[:, None], F, 1)
+    u, dh = (rng.uniform(0.5, 2, (M, F)) * rng.choice([-1, 1], (M, F)) * s for s in (1e37, 1e20))
+    g, u, dh = (_bf16(t) if dtype == "bf16" else t.astype(np.float32) for t in (g, u, dh))
+    for pad, shift in ((0, 0), (3, 1)):
+        h, g8, u8 = ctx().fp8_gated(_t(g, dtype, pad, shift), _t(u, dtype, pad, shift), fmt=FMT[fmt])
+        _near_codes(h, OL.silu_mul(g.astype(np.float64), u.astype(np.float64)), fmt, 2.0 ** -20)
+        gv, uv = (OL.values(_bytes(q.codes), _bytes(q.scales), 1, fmt) for q in (g8, u8))
+        dg, du, dg8, du8 = ctx().fp8_gated_grad(g8, u8, _t(dh, dtype, pad, shift), fmt=FMT[fmt])
+        wg, wu = OL.silu_mul_grad(gv, uv, dh.astype(np.float64))
+        tol = 2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 0)
+        assert np.all(np.abs(_np(dg) - wg) <= tol * np.abs(wg)) and np.all(np.abs(_np(du) - wu) <= tol * np.abs(wu))
+        _near_codes(dg8, wg, fmt, 2.0 ** -20)
+        _near_codes(du8, wu, fmt, 2.0 ** -20)
