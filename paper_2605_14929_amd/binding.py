@@ -810,15 +810,18 @@ class Context:
             raise SopError(2, f"{what} must have contiguous rows")
         return dt, (ld if R > 1 else -(-Cc // 8) * 8)                # (of one row the stride says nothing)
 
-    def _result(self, out, M, N, dtype, x):
-        """(matrix to write to, its sop_dtype, row stride): `out` if it fits, else a new one beside x."""
+    def _result(self, out, M, N, dtype, usual, x):
+        """(matrix to write to, its sop_dtype, row stride): `out` if it fits, else a new one beside x, of the type asked for or the usual one."""
         if out is None:
+            dtype = dtype or usual
             dt = self._dtypes.get(dtype)
             if dt is None:
                 raise SopError(1, "results are float32 or bfloat16")
             return x.new_empty((M, N), dtype=dtype), dt, N
         if tuple(out.shape) != (M, N):
             raise SopError(2, f"out must be {M} x {N}")
+        if dtype is not None and out.dtype != dtype:
+            raise SopError(1, f"out is {out.dtype}, the result asked for {dtype}")
         return (out, *self._numbers(out, "out"))
 
     def fp8_quantize(self, x, rows: int = 1, fmt=E4M3, transposed: bool = False, stream=None) -> Fp8Blocks:
@@ -849,7 +852,7 @@ class Context:
         Kw, N = w.shape if transposed else w.shape[::-1]
         if K != Kw:
             raise SopError(2, f"x has rows of {K} elements, the weight wants {Kw}")
-        out, dt, ldy = self._result(out, M, N, dtype or self._bf16, x.codes)
+        out, dt, ldy = self._result(out, M, N, dtype, self._bf16, x.codes)
         s = self._lib.sop_fp8_matmul(self._h, x._m, w._t if transposed else w._m, transposed, M, N, K, out.data_ptr(), dt, ldy,
                                      self._raw_stream(self.device))
         if s:
@@ -868,7 +871,7 @@ class Context:
             raise SopError(2, f"dy has {M} rows, the checkpoint {x.shape[0]}")
         if accumulate and out is None:
             raise SopError(1, "accumulate needs out")
-        out, dt, ldw = self._result(out, N, K, dtype or self._f32, dy)
+        out, dt, ldw = self._result(out, N, K, dtype, self._f32, dy)
         s = self._lib.sop_fp8_weight_grad(self._h, dy.data_ptr(), lddy, x._m, M, N, K, out.data_ptr(), dt, ldw, accumulate,
                                           self._raw_stream(self.device))
         if s:
@@ -919,9 +922,7 @@ class Context:
         (M, K), (N, Kw) = x.shape, w.shape
         if K != Kw:
             raise SopError(2, f"x has rows of {K} elements, the layer wants {Kw}")
-        out, dt, ldy = self._result(out, M, N, self._bf16, x)
-        if dt != BF16:
-            raise SopError(1, "out must be bfloat16")
+        out, dt, ldy = self._result(out, M, N, self._bf16, self._bf16, x)
         s = self._lib.sop_packed_matmul(self._h, x.data_ptr(), ldx, w._w, M, out.data_ptr(), ldy, self._raw_stream(self.device))
         if s:
             _check(s, self._h)

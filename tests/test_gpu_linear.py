@@ -653,3 +653,17 @@ def test_gated_unit_far_below_zero(dtype, fmt):
         assert np.all(np.abs(_np(dg) - wg) <= tol * np.abs(wg)) and np.all(np.abs(_np(du) - wu) <= tol * np.abs(wu))
         _near_codes(dg8, wg, fmt, 2.0 ** -20)
         _near_codes(du8, wu, fmt, 2.0 ** -20)
+
+
+def test_a_result_of_another_type_than_asked_for_is_refused():
+    import torch
+    cx = ctx()
+    x = torch.ones((4, 256), device="cuda")
+    q, w = cx.fp8_quantize(x), cx.fp8_quantize(torch.ones((140, 256), device="cuda"), rows=128)
+    for f, a, shape in ((cx.fp8_matmul, (q, w), (4, 140)), (cx.fp8_weight_grad, (x.bfloat16(), q), (256, 256))):
+        for has, asked in ((torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)):
+            with pytest.raises(sop.SopError) as e:
+                f(*a, dtype=asked, out=torch.empty(shape, dtype=has, device="cuda"))
+            assert e.value.status == 1
+            out = torch.empty(shape, dtype=has, device="cuda")
+            assert f(*a, dtype=has, out=out) is out and f(*a, out=out) is out
