@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "sop_linear.h"
+#include "sop_linear_rules.h"
 
 namespace sopk {
 
@@ -517,39 +518,26 @@ template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t ro
     hipLaunchKernelGGL((f8mm_rows_kernel<FM, FN, U, W, XF, EXACT>), dim3((unsigned)(tm * tn)), dim3(W * 64), 0, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-// The kernel that is expected to take least, from how many workgroups a compute unit gets.  Microseconds at K = 4096 on 256 compute units,
-// bf16 results: by c workgroups each, the narrow tiles take 4 c + 2 (32 x 32), 6.5 c + 1.5 (32 x 64), 9.3 c + 1 (64 x 64); tiles of 64 x 128 23 for
-// one and 13.5 c for more, of 128 x 128 29 for one and 38.5 for every two, of 256 x 256 60 c.  Where the choice falls wrong it costs little: measured,
-// the best and the next at 300 x 4096 x 4096: 19.0 and 20.1 us; 1024 x 4096 x 4096: 27.9 (64 x 128) and 30.5 (128 x 128); 777 x 5000 x 3000: 31
-// (128 x 128) and 37; 1024 x 11008 x 4096: 60 (256 x 256) and 70 (64 x 128).  Up to four rows operands go straight to
-// registers, two steps in flight: one row through 28672 x 8192 takes 41 us, 45 by 32 x 32 tiles, through 4096 x 11008 9.8 and 10.1; eight rows
-// through 11008 x 4096 12.7 and 9.7.
-template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int n_cu, hipStream_t st)
+template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int choice, hipStream_t st)
 {
-    if (p.M <= 4) return rows_go<1, 1, 2, 8, XF, EXACT>(p, st);
-    auto each = [&](int bm, int bn) { return (float)(((long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) + n_cu - 1) / n_cu); };
-    const float c11 = each(32, 32), c12 = each(32, 64), c22 = each(64, 64), c24 = each(64, 128), c44 = each(128, 128), c88 = each(256, 256);
-    const float cost[6] = {4.0f * c11 + 2.0f, 6.5f * c12 + 1.5f, 9.3f * c22 + 1.0f, c24 <= 1.0f ? 23.0f : 13.5f * c24, c44 <= 1.0f ? 29.0f : 19.25f * (c44 + (float)((long long)c44 & 1)),
-                           EXACT ? 3.4e38f : 60.0f * c88};
-    int best = 0;
-    for (int i = 1; i < 6; ++i) best = cost[i] < cost[best] ? i : best;
-    switch (best) {
-    case 0: return split_go<1, 1, XF, EXACT>(p, st);
-    case 1: return split_go<1, 2, XF, EXACT>(p, st);
-    case 2: return split_go<2, 2, XF, EXACT>(p, st);
-    case 3: return tile_go<64, 128, 2, 2, XF, EXACT>(p, st);
-    case 4: return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
-    default:
-        if constexpr (EXACT) return hipErrorInvalidValue;
-        else return tile_go<256, 256, 2, 4, XF, EXACT>(p, st);
+    switch (choice) {
+    case sopr::F8MM_ROWS: return rows_go<1, 1, 2, 8, XF, EXACT>(p, st);
+    case sopr::F8MM_32x32: return split_go<1, 1, XF, EXACT>(p, st);
+    case sopr::F8MM_32x64: return split_go<1, 2, XF, EXACT>(p, st);
+    case sopr::F8MM_64x64: return split_go<2, 2, XF, EXACT>(p, st);
+    case sopr::F8MM_64x128: return tile_go<64, 128, 2, 2, XF, EXACT>(p, st);
+    case sopr::F8MM_128x128: return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
+    case sopr::F8MM_256x256:
+        if constexpr (!EXACT) return tile_go<256, 256, 2, 4, XF, EXACT>(p, st);
     }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace sopk
 
-extern "C" hipError_t sopk_f8mm_launch(const F8MmParams* p, int x_e5m2, int n_cu, void* stream)
+extern "C" hipError_t sopk_f8mm_launch(const F8MmParams* p, int x_e5m2, int choice, void* stream)
 {
     hipStream_t st = (hipStream_t)stream;
-    if (p->out_bf16) return x_e5m2 ? sopk::go<1, false>(*p, n_cu, st) : sopk::go<0, false>(*p, n_cu, st);
-    return x_e5m2 ? sopk::go<1, true>(*p, n_cu, st) : sopk::go<0, true>(*p, n_cu, st);
+    if (p->out_bf16) return x_e5m2 ? sopk::go<1, false>(*p, choice, st) : sopk::go<0, false>(*p, choice, st);
+    return x_e5m2 ? sopk::go<1, true>(*p, choice, st) : sopk::go<0, true>(*p, choice, st);
 }

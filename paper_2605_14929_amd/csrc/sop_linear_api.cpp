@@ -9,13 +9,14 @@
 
 #include "sop_ctx.h"
 #include "sop_linear.h"
+#include "sop_linear_rules.h"
 
 extern "C" hipError_t sopk_f8_quant_launch(const F8QuantParams* p, int bf16, int e5m2, int vec, int square, void* stream);
 extern "C" hipError_t sopk_f8_gated_launch(const F8GatedParams* p, int bf16, int e5m2, int vec, void* stream);
 extern "C" hipError_t sopk_f8_gated_grad_launch(const F8GatedGradParams* p, int bf16, int ckpt_e5m2, int e5m2, int vec, void* stream);
-extern "C" hipError_t sopk_f8mm_launch(const F8MmParams* p, int x_e5m2, int n_cu, void* stream);
-extern "C" hipError_t sopk_wgrad_launch(const WgradParams* p, int x_e5m2, int n_cu, void* stream);
-extern "C" hipError_t sopk_packed_launch(const PackedMmParams* p, int n_cu, void* stream);
+extern "C" hipError_t sopk_f8mm_launch(const F8MmParams* p, int x_e5m2, int choice, void* stream);
+extern "C" hipError_t sopk_wgrad_launch(const WgradParams* p, int x_e5m2, int choice, void* stream);
+extern "C" hipError_t sopk_packed_launch(const PackedMmParams* p, int choice, void* stream);
 
 namespace {
 
@@ -72,6 +73,23 @@ F8Out out_of(const sop_f8_matrix* q) { return F8Out{q->codes, q->ld_codes, q->sc
 F8In in_of(const sop_f8_matrix* q) { return F8In{q->codes, q->ld_codes, q->scales, q->ld_scales}; }
 bool rows16(const void* p, int64_t ld, int64_t size) { return !off(p, 16) && (ld * size) % 16 == 0; }
 
+// One launch, or, where none can be large enough (fewer than 64 elements along K, and some 2^35 numbers of y), halves of its longer side
+hipError_t packed_parts(const PackedMmParams& p, int n_cu, void* stream)
+{
+    const int choice = sopr::packed_choice(p.M, p.N, p.K, p.n_bits, n_cu);
+    if (choice >= 0) return sopk_packed_launch(&p, choice, stream);
+    PackedMmParams a = p, b = p;
+    if (p.M >= p.N) {
+        a.M = p.M / 2; b.M = p.M - a.M;
+        b.x += a.M * p.ldx; b.y += a.M * p.ldy;
+    } else {
+        a.N = p.N / 2; b.N = p.N - a.N;
+        b.words += (int64_t)a.N * (p.K / p.g); b.payload += (int64_t)a.N * (p.K / 8) * p.n_bits; b.y += a.N;
+    }
+    const hipError_t e = packed_parts(a, n_cu, stream);
+    return e != hipSuccess ? e : packed_parts(b, n_cu, stream);
+}
+
 }  // namespace
 
 extern "C" sop_status sop_fp8_quantize(sop_ctx* c, const void* x, sop_dtype dtype, int64_t M, int64_t K, int64_t ldx, const sop_f8_matrix* q,
@@ -121,10 +139,11 @@ extern "C" sop_status sop_fp8_matmul(sop_ctx* c, const sop_f8_matrix* x, const s
     p.ws_n = w_transposed ? 1 : w->ld_scales; p.ws_k = w_transposed ? w->ld_scales : 1;
     p.M = (int)M; p.N = (int)N; p.K = (int)K;
     p.y = y; p.ldy = ldy; p.out_bf16 = dtype == SOP_BF16;
-    if (((M + 63) / 64) * ((N + 63) / 64) > 0x7FFFFFFF) return bad(c, call, SOP_ESHAPE, "y is too large");
+    const int choice = sopr::f8mm_choice(M, N, dtype == SOP_F32, sopc::compute_units(c));
+    if (choice < 0) return bad(c, call, SOP_ESHAPE, "y is too large for a launch");
     OnDevice on(sopc::device(c));
     if (on.err != hipSuccess) return launched(c, call, on.err);
-    return launched(c, call, sopk_f8mm_launch(&p, x->format == SOP_E5M2, sopc::compute_units(c), stream));
+    return launched(c, call, sopk_f8mm_launch(&p, x->format == SOP_E5M2, choice, stream));
 }
 
 extern "C" sop_status sop_fp8_weight_grad(sop_ctx* c, const void* dy, int64_t lddy, const sop_f8_matrix* x, int64_t M, int64_t N, int64_t K,
@@ -147,9 +166,10 @@ extern "C" sop_status sop_fp8_weight_grad(sop_ctx* c, const void* dy, int64_t ld
     p.M = (int)M; p.N = (int)N; p.K = (int)K;
     p.dw = dw; p.lddw = lddw; p.out_bf16 = dtype == SOP_BF16; p.accumulate = accumulate != 0;
     if (((N + 63) / 64) * ((K + 127) / 128) > 0x7FFFFFFF) return bad(c, call, SOP_ESHAPE, "dw is too large");
+    const bool on16 = rows16(dy, lddy, 2) && lddy <= (int64_t)1 << 22;
     OnDevice on(sopc::device(c));
     if (on.err != hipSuccess) return launched(c, call, on.err);
-    return launched(c, call, sopk_wgrad_launch(&p, M > 0 && x->format == SOP_E5M2, sopc::compute_units(c), stream));
+    return launched(c, call, sopk_wgrad_launch(&p, M > 0 && x->format == SOP_E5M2, sopr::wgrad_choice(M, N, K, on16, sopc::compute_units(c)), stream));
 }
 
 extern "C" sop_status sop_fp8_gated(sop_ctx* c, const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, sop_dtype dtype, int64_t M, int64_t F,
@@ -238,8 +258,7 @@ extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, 
         p.tab[0][i] = w->table_a[i < w->entries_a ? i : w->entries_a - 1];
         if (w->table_b) p.tab[1][i] = w->table_b[i < w->entries_b ? i : w->entries_b - 1];
     }
-    if (((M + 63) / 64) * ((w->N + 63) / 64) > 0x7FFFFFFF) return bad(c, call, SOP_ESHAPE, "y is too large");
     OnDevice on(sopc::device(c));
     if (on.err != hipSuccess) return launched(c, call, on.err);
-    return launched(c, call, sopk_packed_launch(&p, sopc::compute_units(c), stream));
+    return launched(c, call, packed_parts(p, sopc::compute_units(c), stream));
 }

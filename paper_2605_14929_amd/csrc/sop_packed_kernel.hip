@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "sop_linear.h"
+#include "sop_linear_rules.h"
 
 namespace sopk {
 
@@ -601,46 +602,36 @@ template <int NB, int E, int F> static hipError_t wide_go(const PackedMmParams& 
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(256), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-// The kernel that is expected to take least, from how many workgroups a compute unit gets.  Microseconds at K = 4096 on 256 compute units, 4-bit
-// codes, by c workgroups each: the narrow tiles 8 c + 2 (32 x 32), 11 c + 2 (64 x 32), 20.5 c (64 x 64), 19.5 c (128 x 32); the wide ones 64 for one
-// and 51 c for more (128 x 128), 110 c (256 x 192), 128 c (256 x 256; 146 when every unit has one).  Measured, the best and the next: 32 x 11008 x
-// 4096 17.8 (32 x 32) and 19.6; 64 x 11008 x 4096 20.9 (64 x 64) and 23.0; 128 x 4096 x 4096 14.5 (64 x 32) and 18.7; 512 x 4096 x 4096 39 (128 x 32)
-// and 42; 1024 x 4096 x 4096 71 (128 x 128) and 77; 2048 x 11008 x 4096 212 (256 x 192) and 244; 4096 x 4096 x 4096 146 (256 x 256) and 199.  Codes
-// of 3 and 5 bits take up to a quarter more, in the same order.  Up to 16 rows a workgroup takes 16 columns and reads x
-// itself: one row through 4096 x 11008 11.5 us, 20.9 by tiles of 32 x 32.  Tables of pairs of 6-bit codes fit beside 128 x 128 tiles only.
-template <int NB> static hipError_t packed_pick(const PackedMmParams& p, int n_cu, hipStream_t st)
+template <int NB> static hipError_t go(const PackedMmParams& p, int choice, hipStream_t st)
 {
-    if (p.M <= 16) return rows_go<NB, 1, 2, 8>(p, st);
-    auto each = [&](int bm, int bn) { return (float)(((long long)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) + n_cu - 1) / n_cu); };
-    const float c22 = each(128, 128), never = 3.4e38f;
-    const float cost[7] = {8.0f * each(32, 32) + 1.7f, 11.0f * each(64, 32) + 2.0f, 20.5f * each(64, 64), 19.5f * each(128, 32),
-                           p.K < 64 ? never : c22 <= 1.0f ? 64.0f : 51.0f * c22, p.K < 64 || NB > 5 ? never : 110.0f * each(256, 192), p.K < 64 || NB > 5 ? never : 128.0f * each(256, 256)};
-    int best = 0;
-    for (int i = 1; i < 7; ++i) best = cost[i] < cost[best] ? i : best;
-    switch (best) {
-    case 0: return split_go<NB, 1, 1, 1>(p, st);
-    case 1: return split_go<NB, 2, 1, 1>(p, st);
-    case 2: return split_go<NB, 2, 2, 1>(p, st);
-    case 3: return split_go<NB, 4, 1, 1>(p, st);
-    case 4: return wide_go<NB, 2, 2>(p, st);
-    default:
-        if constexpr (NB > 5) return hipErrorInvalidValue;
-        else return best == 5 ? wide_go<NB, 4, 3>(p, st) : wide_go<NB, 4, 4>(p, st);
+    switch (choice) {
+    case sopr::PACKED_ROWS: return rows_go<NB, 1, 2, 8>(p, st);
+    case sopr::PACKED_32x32: return split_go<NB, 1, 1, 1>(p, st);
+    case sopr::PACKED_64x32: return split_go<NB, 2, 1, 1>(p, st);
+    case sopr::PACKED_64x64: return split_go<NB, 2, 2, 1>(p, st);
+    case sopr::PACKED_128x32: return split_go<NB, 4, 1, 1>(p, st);
+    case sopr::PACKED_128x128: return wide_go<NB, 2, 2>(p, st);
+    case sopr::PACKED_256x192:
+        if constexpr (NB <= 5) return wide_go<NB, 4, 3>(p, st);
+        break;
+    case sopr::PACKED_256x256:
+        if constexpr (NB <= 5) return wide_go<NB, 4, 4>(p, st);
     }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace sopk
 
-extern "C" hipError_t sopk_packed_launch(const PackedMmParams* p, int n_cu, void* stream)
+extern "C" hipError_t sopk_packed_launch(const PackedMmParams* p, int choice, void* stream)
 {
     hipStream_t st = (hipStream_t)stream;
     switch (p->n_bits) {
-    case 1: return sopk::packed_pick<1>(*p, n_cu, st);
-    case 2: return sopk::packed_pick<2>(*p, n_cu, st);
-    case 3: return sopk::packed_pick<3>(*p, n_cu, st);
-    case 4: return sopk::packed_pick<4>(*p, n_cu, st);
-    case 5: return sopk::packed_pick<5>(*p, n_cu, st);
-    case 6: return sopk::packed_pick<6>(*p, n_cu, st);
-    default: return hipErrorInvalidValue;
+    case 1: return sopk::go<1>(*p, choice, st);
+    case 2: return sopk::go<2>(*p, choice, st);
+    case 3: return sopk::go<3>(*p, choice, st);
+    case 4: return sopk::go<4>(*p, choice, st);
+    case 5: return sopk::go<5>(*p, choice, st);
+    case 6: return sopk::go<6>(*p, choice, st);
     }
+    return hipErrorInvalidValue;
 }

@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "sop_linear.h"
+#include "sop_linear_rules.h"
 
 namespace sopk {
 
@@ -637,31 +638,23 @@ template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_go(co
     hipLaunchKernelGGL((wgrad_kernel<BN, BK, WR, WC, X5>), dim3((unsigned)(tn * tk)), dim3(WR * WC * 64), bytes, st, p, tn, tk, 8);
     return hipGetLastError();
 }
-// The kernel that is expected to take least, from how many workgroups c a compute unit gets and how many times 64 rows there are (t).
-// Microseconds on 256 compute units, 32-bit results: the rows dealt out 1.4 + c (1.2 + 0.16 t) (32 x 64) and 1.2 + c (2.9 + 0.21 t) (64 x 64);
-// 128 x 128 4.4 + 0.82 t for one and c (4 + 0.6 t) for more; 256 x 256 c (19 + 1.65 t).  Measured (rows x N x K), the best and the next:
-// 8192 x 512 x 512 24 (32 x 64) and 33, by 128 x 128 107; 8192 x 1024 x 1024 32 (64 x 64) and 49; 777 x 1531 x 5024 23 (128 x 128) and 30;
-// 2048 x 4096 x 4096 72 (256 x 256) and 92; 500 x 8192 x 4096 67 (256 x 256) and 71.
-template <bool X5> static hipError_t wgrad_pick(const WgradParams& p, int n_cu, hipStream_t st)
+template <bool X5> static hipError_t go(const WgradParams& p, int choice, hipStream_t st)
 {
-    auto tiles = [&](int a, int b) { return (long long)((p.N + a - 1) / a) * ((p.K + b - 1) / b); };
-    const bool on16 = (reinterpret_cast<uintptr_t>(p.dy) & 15) == 0 && (p.lddy & 7) == 0 && p.lddy <= 1 << 22;
-    if (p.M > 0 && on16) {
-        auto each = [&](int a, int b) { return (float)((tiles(a, b) + n_cu - 1) / n_cu); };
-        const float t = (float)((p.M + 63) / 64), c44 = each(128, 128);
-        const float cost[4] = {1.4f + each(32, 64) * (1.2f + 0.16f * t), 1.2f + each(64, 64) * (2.9f + 0.21f * t), c44 <= 1.0f ? 4.4f + 0.82f * t : c44 * (4.0f + 0.6f * t), each(256, 256) * (19.0f + 1.65f * t)};
-        int best = 0;
-        for (int i = 1; i < 4; ++i) best = cost[i] < cost[best] ? i : best;
-        return best == 0 ? wgrad_split_go<1, X5>(p, st) : best == 1 ? wgrad_split_go<2, X5>(p, st) : best == 2 ? wgrad_turn_go<128, 128, 2, 2, X5>(p, st) : wgrad_large_go<X5>(p, st);
+    switch (choice) {
+    case sopr::WGRAD_32x64: return wgrad_split_go<1, X5>(p, st);
+    case sopr::WGRAD_64x64: return wgrad_split_go<2, X5>(p, st);
+    case sopr::WGRAD_128x128: return wgrad_turn_go<128, 128, 2, 2, X5>(p, st);
+    case sopr::WGRAD_256x256: return wgrad_large_go<X5>(p, st);
+    case sopr::WGRAD_ANY_64x128: return wgrad_go<64, 128, 2, 2, X5>(p, st);
+    case sopr::WGRAD_ANY_128x128: return wgrad_go<128, 128, 2, 2, X5>(p, st);
+    case sopr::WGRAD_ANY_256x256: return wgrad_go<256, 256, 2, 4, X5>(p, st);
     }
-    if (tiles(256, 256) >= n_cu) return wgrad_go<256, 256, 2, 4, X5>(p, st);
-    if (tiles(128, 128) >= n_cu) return wgrad_go<128, 128, 2, 2, X5>(p, st);
-    return wgrad_go<64, 128, 2, 2, X5>(p, st);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace sopk
 
-extern "C" hipError_t sopk_wgrad_launch(const WgradParams* p, int x_e5m2, int n_cu, void* stream)
+extern "C" hipError_t sopk_wgrad_launch(const WgradParams* p, int x_e5m2, int choice, void* stream)
 {
-    return x_e5m2 ? sopk::wgrad_pick<true>(*p, n_cu, (hipStream_t)stream) : sopk::wgrad_pick<false>(*p, n_cu, (hipStream_t)stream);
+    return x_e5m2 ? sopk::go<true>(*p, choice, (hipStream_t)stream) : sopk::go<false>(*p, choice, (hipStream_t)stream);
 }

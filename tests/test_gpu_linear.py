@@ -590,11 +590,14 @@ def test_packed_product_with_one_row_left(M, N, K, g, n):
     test_packed_product((M, N, K, g, n, (0, 4, 3, 8), True, 0))
 
 
-# Scales from 2^-127 to 2^127 whose product is moderate: whole numbers, exact in either type of result.  A size for each way of sharing y out:
-# up to four rows, tiles of 32 x 32, 32 x 64, 64 x 64, 64 x 128, 128 x 128 and (bf16 results alone) 256 x 256.
+# A size for each way of sharing y out: up to four rows, tiles of 32 x 32, 32 x 64, 64 x 64, 64 x 128, 128 x 128 and (bf16 results alone) 256 x 256.
+F8_KERNELS = [(3, 130, 300), (40, 150, 300), (301, 1531, 300), (513, 1025, 300), (1001, 4090, 150), (2049, 2050, 150), (2300, 4700, 150)]
+
+
+# Scales from 2^-127 to 2^127 whose product is moderate: whole numbers, exact in either type of result.
 @pytest.mark.parametrize("fmt", ["E4M3", "E5M2"])
 @pytest.mark.parametrize("a, b", [(252, 0), (0, 252), (60, 190), (1, 251), (9, 243), (245, 9), (15, 237), (238, 14)])
-@pytest.mark.parametrize("M, N, K", [(3, 130, 300), (40, 150, 300), (301, 1531, 300), (513, 1025, 300), (1001, 4090, 150), (2049, 2050, 150), (2300, 4700, 150)])
+@pytest.mark.parametrize("M, N, K", F8_KERNELS)
 def test_product_under_scales_of_any_size(M, N, K, a, b, fmt):
     import torch
     rng = np.random.default_rng(15)
@@ -667,3 +670,55 @@ def test_a_result_of_another_type_than_asked_for_is_refused():
             assert e.value.status == 1
             out = torch.empty(shape, dtype=has, device="cuda")
             assert f(*a, dtype=has, out=out) is out and f(*a, out=out) is out
+
+
+# tiles of 64 x 32 of y a workgroup
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("M, N, K, g", [(100, 4001, 200, 8), (128, 4096, 584, 8), (90, 4030, 1040, 16), (127, 3999, 192, 64)])
+def test_packed_product_of_a_hundred_rows(M, N, K, g, n):
+    test_packed_product((M, N, K, g, n, (1, 5, 5, 12), True, 0))
+
+
+def test_more_rows_or_columns_than_one_grid_of_small_tiles_holds():
+    """2^28 rows in tiles of 32, 2^27 columns by 16: 2^32 threads and more, so larger tiles take them."""
+    import torch
+    cx = ctx()
+    M, K = (1 << 28) + 5, 16
+    x = sop.Fp8Blocks.empty(M, K, sop.E4M3, torch.device("cuda", 0))
+    x.codes.view(torch.uint8).fill_(0x38)                             # 1.0
+    x.scales.view(torch.uint8).fill_(127)
+    x.codes.view(torch.uint8)[M - 1, 3] = 0x40                        # 2.0
+    w = cx.fp8_quantize(torch.ones((1, K), device="cuda"), rows=128)
+    for dtype in (torch.float32, torch.bfloat16):
+        y = cx.fp8_matmul(x, w, dtype=dtype)
+        assert float(y[M - 1, 0]) == K + 1 and float(y[:M - 1].min()) == float(y[:M - 1].max()) == K
+    del x, y
+    w = sop.Fp8Blocks.empty(M, K, sop.E4M3, torch.device("cuda", 0), rows=128)
+    w.codes.view(torch.uint8).fill_(0x38)
+    w.scales.view(torch.uint8).fill_(127)
+    w.codes.view(torch.uint8)[M - 1, 3] = 0x40
+    y = cx.fp8_matmul(cx.fp8_quantize(torch.ones((2, K), device="cuda")), w, dtype=torch.float32)
+    assert float(y[:, M - 1].min()) == float(y[:, M - 1].max()) == K + 1 and float(y[:, :M - 1].min()) == float(y[:, :M - 1].max()) == K
+    del w, y
+    N, K, g, n = (1 << 27) + 5, 8, 8, 1
+    fmt = sop.ScaleFmt(0, 4, 4, 8, -1, -1)                            # 7 << 4: the scale 1
+    words, payload = torch.full((N,), 7 << 4, dtype=torch.int16, device="cuda"), torch.zeros(N, dtype=torch.uint8, device="cuda")
+    payload[N - 1] = 1
+    layer = sop.PackedWeights(words, payload, N, K, g, n, fmt, [np.array([1.0, 3.0], np.float32)])
+    y = cx.packed_matmul(torch.ones((2, K), dtype=torch.bfloat16, device="cuda"), layer)
+    assert float(y[:, N - 1].min()) == float(y[:, N - 1].max()) == K + 2 and float(y[:, :N - 1].min()) == float(y[:, :N - 1].max()) == K
+
+
+def test_packed_products_too_large_for_a_launch():
+    """2^29 columns, or rows, of fewer than 64 elements: no tile is large enough, so two launches share them."""
+    import torch
+    cx = ctx()
+    fmt, K = sop.ScaleFmt(0, 4, 4, 8, -1, -1), 8
+    for M, N in ((1, (1 << 29) + 5), ((1 << 29) + 5, 1)):
+        words, payload = torch.full((N,), 7 << 4, dtype=torch.int16, device="cuda"), torch.zeros(N, dtype=torch.uint8, device="cuda")
+        x = torch.ones((M, K), dtype=torch.bfloat16, device="cuda")
+        x[M - 1, 0] = 2
+        payload[N - 1] = 1
+        y = cx.packed_matmul(x, sop.PackedWeights(words, payload, N, K, 8, 1, fmt, [np.array([1.0, 3.0], np.float32)])).view(-1)
+        assert float(y[-1]) == 13 and float(y[:-1].min()) == float(y[:-1].max()) == (9 if M == 1 else 10)
+        del x, y, words, payload
