@@ -722,3 +722,85 @@ def test_packed_products_too_large_for_a_launch():
         y = cx.packed_matmul(x, sop.PackedWeights(words, payload, N, K, 8, 1, fmt, [np.array([1.0, 3.0], np.float32)])).view(-1)
         assert float(y[-1]) == 13 and float(y[:-1].min()) == float(y[:-1].max()) == (9 if M == 1 else 10)
         del x, y, words, payload
+
+
+# the product over the other index, by every kernel, in both formats and both types of result; K ends inside a step
+@pytest.mark.parametrize("fmt", ["E4M3", "E5M2"])
+@pytest.mark.parametrize("M, N, K", F8_KERNELS + [(2300, 4700, 1001), (1001, 4090, 700)])
+def test_transposed_product_of_whole_numbers_is_exact(M, N, K, fmt):
+    import torch
+    rng = np.random.default_rng(19)
+    (xc, xs), (vc, vs) = _integers(rng, M, K, 1, fmt), _integers(rng, K, N, 128)
+    ref = (torch.from_numpy(OL.values(xc, xs, 1, fmt)).cuda() @ torch.from_numpy(OL.values(vc, vs, 128, "E4M3")).cuda()).cpu().numpy()
+    x, v = _f8(xc, xs, 1, fmt), _f8(vc, vs, 128, "E4M3", codes_t=True)
+    assert np.array_equal(_np(ctx().fp8_matmul(x, v, transposed=True, dtype=torch.float32)), ref)
+    assert np.array_equal(_np(ctx().fp8_matmul(x, v, transposed=True)), _bf16(ref))
+
+
+# results of 32 bits in whole lines of 128 bytes, which go past the caches, alone and added to what is there
+@pytest.mark.parametrize("M, N, K", [(3, 128, 300), (40, 160, 300), (301, 1536, 300), (513, 1024, 300), (1001, 4096, 150), (2049, 2048, 150), (1025, 4096, 4000)])
+def test_product_in_whole_lines(M, N, K):
+    import torch
+    rng = np.random.default_rng(20)
+    (xc, xs), (wc, ws) = _integers(rng, M, K, 1), _integers(rng, N, K, 128)
+    ref = (torch.from_numpy(OL.values(xc, xs, 1, "E4M3")).cuda() @ torch.from_numpy(OL.values(wc, ws, 128, "E4M3")).cuda().t()).cpu().numpy()
+    buf = torch.full((M, N + 32), 7.0, device="cuda")
+    assert buf.data_ptr() % 128 == 0
+    ctx().fp8_matmul(_f8(xc, xs, 1, "E4M3"), _f8(wc, ws, 128, "E4M3"), out=buf[:, :N])
+    assert np.array_equal(_np(buf[:, :N]), ref) and np.all(_np(buf[:, N:]) == 7)
+
+
+@pytest.mark.parametrize("spaced", [True, False])
+@pytest.mark.parametrize("M, N, K", [(65, 101, 160), (1100, 300, 512), (2100, 1001, 1024), (65, 1531, 2112), (130, 1027, 4096), (1025, 4090, 4000), (130, 2050, 4096)])
+def test_weight_gradient_in_whole_lines(M, N, K, spaced):
+    import torch
+    rng = np.random.default_rng(21)
+    xc, xs = _integers(rng, M, K, 1)
+    dy, had = rng.integers(-8, 9, (M, N)).astype(np.float32), rng.integers(-9, 10, (N, K + 32)).astype(np.float32)
+    ref = (torch.from_numpy(dy).cuda().double().t() @ torch.from_numpy(OL.values(xc, xs, 1, "E4M3")).cuda()).cpu().numpy()
+    x, d, out = _f8(xc, xs, 1, "E4M3"), _t(dy, "bf16", 8 + -N % 8 if spaced else 0, 0 if spaced else 1), _t(had)
+    assert out.data_ptr() % 128 == 0
+    ctx().fp8_weight_grad(d, x, out=out[:, :K], accumulate=True)
+    assert np.array_equal(_np(out[:, :K]), ref + had[:, :K]) and np.array_equal(_np(out[:, K:]), had[:, K:])
+    ctx().fp8_weight_grad(d, x, out=out[:, :K])
+    assert np.array_equal(_np(out[:, :K]), ref) and np.array_equal(_np(out[:, K:]), had[:, K:])
+
+
+def _near_codes_within(q, value, fmt, err):
+    """As _near_codes, `value` being known to `err` element by element."""
+    codes, scales = _bytes(q.codes), _bytes(q.scales)
+    M, K = value.shape
+    got = scales.astype(np.int64) - 127
+    lo, hi = OL.block_exponents(np.maximum(np.abs(value) - err, 0), 1, fmt), OL.block_exponents(np.abs(value) + err, 1, fmt)
+    assert np.all((got >= lo) & (got <= hi))
+    step = 2.0 ** OL.spread(got, 1, M, K)
+    unit = 2.0 ** np.maximum(np.floor(np.log2(np.maximum((np.abs(value) + err) / step, 1e-300))), OL.LEAST[fmt]) * 2.0 ** -OL.MANT[fmt] * step
+    assert np.all(np.abs(OL.values(codes, scales, 1, fmt) - value) <= unit / 2 + err)
+
+
+# rows on 16 bytes and off them, rows that end inside eight elements and on them, more rows than the wavefronts of a launch (the last ones are compared)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt", ["E4M3", "E5M2"])
+@pytest.mark.parametrize("M, F", [(1, 8), (33, 1001), (130, 512), (70, 1000), (9000, 520)])
+def test_gated_unit_and_gradient_on_any_alignment(M, F, dtype, fmt):
+    rng = np.random.default_rng(22)
+    g, u, dh = rng.standard_normal((M, F)) * 4, rng.standard_normal((M, F)), rng.standard_normal((M, F)) * 1e-3
+    g, u, dh = (_bf16(t) if dtype == "bf16" else t.astype(np.float32) for t in (g, u, dh))
+    end = slice(max(0, M - 150), M)
+    for pad, shift in ((0, 0), (-F % 8 + 8, 0), (5, 1)):
+        h, g8, u8 = ctx().fp8_gated(_t(g, dtype, pad, shift), _t(u, dtype, pad, shift), fmt=FMT[fmt])
+        dg, du, dg8, du8 = ctx().fp8_gated_grad(g8, u8, _t(dh, dtype, pad, shift), fmt=FMT[fmt])
+        h, g8, u8, dg8, du8 = (sop.Fp8Blocks(q.codes[end], q.scales[end]) for q in (h, g8, u8, dg8, du8))
+        for q, x in ((g8, g), (u8, u)):
+            codes, scales = OL.quantize(x[end], 1, fmt)
+            assert np.array_equal(_bytes(q.codes), codes) and np.array_equal(_bytes(q.scales), scales)
+        _near_codes(h, OL.silu_mul(g[end].astype(np.float64), u[end].astype(np.float64)), fmt, 2.0 ** -20)
+        gv, uv = (OL.values(_bytes(q.codes), _bytes(q.scales), 1, fmt) for q in (g8, u8))
+        wg, wu = OL.silu_mul_grad(gv, uv, dh[end].astype(np.float64))
+        # dgate's last factor, 1 + g (1 - s), may cancel: its error is one of the two terms
+        part = np.abs(dh[end] * uv) * (1 + np.abs(gv)) * (1 / (1 + np.exp(-gv)))
+        tol = 2.0 ** -8 if dtype == "bf16" else 0
+        assert np.all(np.abs(_np(dg[end]) - wg) <= tol * np.abs(wg) + 2.0 ** -20 * part)
+        assert np.all(np.abs(_np(du[end]) - wu) <= (tol + 2.0 ** -20) * np.abs(wu))
+        _near_codes_within(dg8, wg, fmt, 2.0 ** -20 * part)
+        _near_codes(du8, wu, fmt, 2.0 ** -20)
