@@ -181,15 +181,15 @@ template <bool E5M2, bool HIGH> __device__ __forceinline__ int two_rows(int c, f
 }
 
 // ---- rows of dy on 16 bytes.  64 rows a step, three steps in LDS: one being multiplied, one on its way or there, one being asked for.
-// In LDS a row is chunks of 16 bytes; chunk c of row m stands at position c ^ 4 (m & 3) (dy), c ^ 2 (m & 7) (x, rows of 256 bytes) or
-// c ^ 2 (m / 2 & 3) (x, rows of 128), so that the rows that 32 lanes read together fall on different banks.  777 x 1531 x 5024 takes 20.5 us: thirteen
+// In LDS a row is chunks of 16 bytes; chunk c of row m stands at position c ^ 4 (m & 3) (dy, rows of 256 bytes) or c ^ 2 (m / 2 & 3) (x, rows of
+// 128), so that the rows that 32 lanes read together fall on different banks.  777 x 1531 x 5024 takes 20.5 us: thirteen
 // steps of two workgroups a compute unit (12 us), 31 MB of results (6 us), and the first loads.
 template <int BN, int BK, int WR, int WC, bool X5>
 __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
 {
-    constexpr int NT = WR * WC * 64, FA = BN / WR / 32, FB = BK / WC / 32, NKB = BK / 128;
-    constexpr int CD = BN / 8, CX = BK / 16, LD = 64 * CD / NT, LX = 64 * CX / NT, XAT = 64 * BN * 2, SAT = XAT + 64 * BK, STAGE = SAT + NKB * 256;
-    static_assert(LD * NT == 64 * CD && LX * NT == 64 * CX && LD == 4 && LX == 2 && NT / CD % 4 == 0 && NT / CX % 8 == 0 && BK / WC <= 128, "shares of a step");
+    constexpr int NT = WR * WC * 64, FA = BN / WR / 32, FB = BK / WC / 32;
+    constexpr int CD = BN / 8, CX = BK / 16, LD = 64 * CD / NT, LX = 64 * CX / NT, XAT = 64 * BN * 2, SAT = XAT + 64 * BK, STAGE = SAT + 256;
+    static_assert(LD * NT == 64 * CD && LX * NT == 64 * CX && LD == 4 && LX == 2 && NT / CD % 4 == 0 && NT / CX % 8 == 0 && BK == 128, "shares of a step, one scale a row");
     extern __shared__ __align__(16) unsigned char lds[];
     int tn, tk;
     tile_of(blockIdx.x, tiles_n * tiles_k, tiles_n, tiles_k, group, tn, tk);
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
     const int wn = wave / WC * (BN / WR), wk = wave % WC * (BK / WC), i16 = lane & 15, g16 = lane >> 4 & 1, h = lane >> 5;
     const int steps = (p.M + 63) >> 6;
 
-    auto turn_x = [](int m) { return BK == 256 ? (m & 7) << 1 : (m >> 1 & 3) << 1; };
+    auto turn_x = [](int m) { return (m >> 1 & 3) << 1; };
     // where this thread's chunks come from, within 64 rows; chunks beyond the last column read the last one, and their sums go nowhere.
     // (An aligned chunk with one element inside the matrix lies on its page.)
     unsigned int od[LD], ox[LX];
@@ -232,9 +232,9 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
                          lds_address(words) + t % 3 * 256);
     };
     auto put_scales = [&](int t, unsigned char* to) {
-        if (tid < 64 * NKB) {
-            const unsigned int w = *reinterpret_cast<const unsigned int*>(words + t % 3 * 256 + (tid & 63) * 4);
-            *reinterpret_cast<float*>(to + SAT + tid * 4) = e8m0_value(w >> (8 * (((k0 >> 7) + (tid >> 6)) & 3)) & 255u);
+        if (tid < 64) {
+            const unsigned int w = *reinterpret_cast<const unsigned int*>(words + t % 3 * 256 + tid * 4);
+            *reinterpret_cast<float*>(to + SAT + tid * 4) = e8m0_value(w >> (8 * ((k0 >> 7) & 3)) & 255u);
         }
     };
 
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradPar
         const int c = (wk >> 4) + 2 * b + g16, m = 8 * h + (i16 >> 1);
         ax[b] = (unsigned int)(XAT + m * BK + ((c ^ turn_x(m)) << 4) + (i16 & 1) * 8);
     }
-    const unsigned int as = (unsigned int)(SAT + (wk >> 7) * 256 + h * 32);
+    const unsigned int as = (unsigned int)(SAT + h * 32);
 
     v16f acc[FA][FB];
 #pragma unroll
@@ -620,7 +620,7 @@ template <int FN, bool X5> static hipError_t wgrad_split_go(const WgradParams& p
 }
 template <int BN, int BK, int WR, int WC, bool X5> static hipError_t wgrad_turn_go(const WgradParams& p, hipStream_t st)
 {
-    const int tn = (p.N + BN - 1) / BN, tk = (p.K + BK - 1) / BK, bytes = 3 * (64 * BN * 2 + 64 * BK + BK / 128 * 256) + 3 * 256;
+    const int tn = (p.N + BN - 1) / BN, tk = (p.K + BK - 1) / BK, bytes = 3 * (64 * BN * 2 + 64 * BK + 256) + 3 * 256;
     if (bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&wgrad_turn_kernel<BN, BK, WR, WC, X5>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
