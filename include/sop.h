@@ -585,7 +585,8 @@ typedef struct {
     const float* table_b; int entries_b;
 } sop_packed_weights;
 
-/* y[m, n] = sum_k x[m, k] w[n, k] with such weights, w = s * L[code] in binary32, rounded to bf16 for the matrix instructions; x [M, K]
+/* y[m, n] = sum_k x[m, k] w[n, k] with such weights, w = s * L[code] in binary32, rounded to bf16 for the matrix instructions (which takes the
+ * error of y, 1.7e-3 from its own rounding, to 2.2e-3); x [M, K]
  * DEVICE, bf16, 16-byte aligned, row stride ldx a multiple of 8 elements, K and ldx at most 2^22; y [M, N] DEVICE, bf16, row stride ldy; sums are binary32. */
 sop_status sop_packed_matmul(sop_ctx* ctx, const void* x_dev, int64_t ldx, const sop_packed_weights* w, int64_t M, void* y_dev, int64_t ldy, void* hip_stream);
 

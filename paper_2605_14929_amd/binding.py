@@ -782,7 +782,8 @@ class Context:
                                      C.c_void_p(st)), self._h)
         return out
 
-    # ---- products of a linear layer with narrow operands (calls of a few microseconds: their Python side is kept short)
+    # ---- products of a linear layer with narrow operands (calls of a few microseconds: their Python side is kept short).  They take tensors' data and
+    # know nothing of autograd: results require no gradients, the backward operators are called by who wants them.
 
     def _on(self, stream, call, *args, **kw):
         """The call with `stream` (a handle) as torch's current stream: what it allocates is then that stream's too."""

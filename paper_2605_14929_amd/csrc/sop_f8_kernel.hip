@@ -8,8 +8,9 @@
 //
 // All passes read their inputs once and write their outputs once and are bound by HBM.  A lane takes eight neighbouring elements
 // (one 16-byte load of bf16, one 8-byte store of codes), sixteen lanes a block of 128, which find its maximum by rotations inside
-// a row of the wavefront: no LDS.  Measured (a large copy moves 5.04 TB/s here): rows of 4096 x 11008 bf16, 25 us, 5.4 TB/s; squares of 28672 x 8192
-// bf16 with their transposed copy, 192 us, 4.9 TB/s; the gated unit of 8192 x 11008 bf16, 134 us, 4.7 TB/s; its gradient at 1531 x 5024, 16.3 us, 4.7 TB/s.
+// a row of the wavefront: no LDS.  Measured, kernel times (a large copy moves 5.14 TB/s here): rows of 4096 x 11008 bf16, 26 us, 5.2 TB/s; squares of
+// 28672 x 8192 bf16 with their transposed copy, 192 us, 4.9 TB/s; the gated unit of 8192 x 11008 bf16, 135 us, 4.7 TB/s; its gradient at 1531 x 5024,
+// 17.5 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "sop_linear.h"

@@ -8,8 +8,8 @@
 //   fp32  An 8-bit float times a power of two is a bf16 number while it stays within bf16's range: the operands become bf16 exactly and go through
 //         the bf16 instruction, whose sums are binary32 throughout (1e-7 off), at half the rate.  Under scales so large or small that it does not, a
 //         part of a block's scale goes into its operands and the rest onto the block's sum.  Done throughout, that costs: 4096 x 4096 x 4096 takes 147 us
-//         so, 124 with all of it in the operands; so who has met such scales walks its steps a second time.  (Up to four rows, bound by
-//         the read of w, they go onto the sums always.)
+//         so, 124 with all of it in the operands; so who has met such scales walks its steps a second time (230 us against 114, all
+//         workgroups doing so).  Up to four rows, bound by the read of w, they go onto the sums always.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -93,7 +93,8 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
             for (int i = 0; i < 4; ++i) if (n + i < p.N) y[i] = (uint16_t)bf16_bits(v[i]);
         }
     } else {
-        // whole lines are written past the caches: 4096 x 11008 x 512 takes 65 us so, 79 otherwise; 1460 x 5296 x 288 14.9 and 14.6
+        // Whole lines are written past the caches.  4096 x 11008 x 512 takes 63 us so and 64 otherwise where each call has a y of its own, 62 and 56 where
+        // all write to one, 151 and 155 with a pass that reads y; 1024 x 4096 x 4096 38.0 and 38.5; 1460 x 5296 x 288 13.2 both ways.
         const bool lines = ((reinterpret_cast<uintptr_t>(p.y) | (unsigned long long)p.ldy * 4) & 127) == 0;
         float* y = reinterpret_cast<float*>(p.y) + at;
         if (n + 3 < p.N && lines) __builtin_nontemporal_store(v, reinterpret_cast<v4f*>(y));
@@ -122,7 +123,7 @@ __device__ __forceinline__ void clear_beyond(unsigned char* tile, int rows, int 
 // ---- tiles: BM x BN of y by WR x WC wavefronts, 128 elements along K a step, two steps in LDS.  A wavefront's part is made of 32 x 32
 // squares.  In LDS a row is eight chunks of 16 bytes, chunk c at position c ^ (row / 2 & 7): LDS serves a 16-byte read sixteen lanes at
 // a time (0-3, 12-15, 20-23 and 24-27, then the others of the first 32, ...), whose rows so fall on different banks.  256 x 256 by eight
-// wavefronts: 8192 x 28672 x 8192 takes 1600 us (2410 TFLOP/s), 4096 x 4096 x 11008 157 us (2350).  With 128 of 256 compute units at work and power to
+// wavefronts: 8192 x 28672 x 8192 takes 1584 us (2430 TFLOP/s), 4096 x 4096 x 11008 144 us (2560).  With 128 of 256 compute units at work and power to
 // spare, a step takes 1.65 us: its loads alone 1.1 (64 KB a compute unit, with two steps in flight or one), its operands' reads and matrix instructions alone
 // 1.5, of which the instructions are 0.95.  Operands read two matrix instructions ahead, half of the workgroup a half-step behind the other, four
 // wavefronts of 128 x 128, and lines asked for into L2 ahead of the loads all took as long or longer.
@@ -279,8 +280,8 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
 }
 
 // ---- few tiles: FM x 16 rows of x by FN x 16 columns a workgroup, K dealt out to its W wavefronts, U steps at a time.  Operands go from
-// memory to registers as the matrix instruction wants them; the wavefronts' sums meet in LDS in a fixed order.  One row through 4096 x 11008 takes
-// 9.8 us, 4.6 TB/s, bound by the read of w.
+// memory to registers as the matrix instruction wants them; the wavefronts' sums meet in LDS in a fixed order.  One row through 28672 x 8192 whose
+// weights lie in HBM takes 39.1 us, 6.0 TB/s, bound by the read of w; through 4096 x 11008 a call takes 12.8 us so, 10.6 with the weights in the last-level cache.
 template <int FM, int FN, int U, int W, int XF, bool EXACT>
 __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
@@ -381,7 +382,7 @@ __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, i
 // ---- few tiles: 32 FM x 32 FN of y a workgroup, K dealt out to its W wavefronts step by step.  Every wavefront has its own place in LDS for
 // a step's operands and waits for its own loads alone: rows come in whole lines that way, which operands loaded straight into registers
 // (32 bytes of a row a lane) do not.  While a step is multiplied the wavefront's next one is on its way.  The wavefronts' sums meet in LDS in
-// a fixed order.  301 x 1531 x 5024 with fp32 results takes 12.7 us by it, 34 by tiles of 64 x 128: five steps a wavefront, each as long as its
+// a fixed order.  301 x 1531 x 5024 with fp32 results takes 12.5 us by it, 34 by tiles of 64 x 128: five steps a wavefront, each as long as its
 // loads take to come.
 template <int FM, int FN, int XF, bool EXACT>
 __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)

@@ -85,7 +85,6 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
-typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 
@@ -106,7 +105,7 @@ __device__ __forceinline__ unsigned int bf16_pair(float lo, float hi)
     v[0] = (__bf16)lo; v[1] = (__bf16)hi;
     return __builtin_bit_cast(unsigned int, v);
 }
-// eight 8-bit floats times a scale, as bf16: exact
+// eight 8-bit floats times a scale, as bf16: exact within its normal numbers
 template <bool E5M2> __device__ __forceinline__ v4i eight_bf16(unsigned int lo, unsigned int hi, float s)
 {
     v4i r;

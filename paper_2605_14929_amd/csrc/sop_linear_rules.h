@@ -1,5 +1,6 @@
 // Which kernel takes a product of a linear layer with narrow operands: the one that is expected to take least, among those whose launch is
-// possible.  Plain C++, so that the rules can be evaluated on a host.
+// possible.  Plain C++, so that the rules can be evaluated on a host.  The times beside the rules are those that the costs were taken from; they compare kernels
+// of one run.
 #ifndef SOP_LINEAR_RULES_H
 #define SOP_LINEAR_RULES_H
 
@@ -21,8 +22,9 @@ inline int least(const float* cost, int n)
 // ---- product of two 8-bit matrices.  The cost is counted from how many workgroups a compute unit gets.  Microseconds at K = 4096 on 256 compute units,
 // bf16 results: by c workgroups each, the narrow tiles take 4 c + 2 (32 x 32), 6.5 c + 1.5 (32 x 64), 9.3 c + 1 (64 x 64); tiles of 64 x 128 23 for
 // one and 13.5 c for more, of 128 x 128 29 for one and 38.5 for every two, of 256 x 256 60 c (bf16 results alone).  Where the choice falls wrong it costs
-// little: measured, the best and the next at 300 x 4096 x 4096: 19.0 and 20.1 us; 1024 x 4096 x 4096: 27.9 (64 x 128) and 30.5 (128 x 128); 777 x 5000 x
-// 3000: 31 (128 x 128) and 37; 1024 x 11008 x 4096: 60 (256 x 256) and 70 (64 x 128).  Up to four rows operands go straight to
+// little: measured, the best and the next at 300 x 4096 x 4096: 19.0 and 20.1 us; 1024 x 4096 x 4096: 27.9 (64 x 128) and 30.5 (128 x
+// 128); 777 x 5000 x 3000: 31 (128 x 128) and 37; 1024 x 11008 x 4096: 60 (256 x 256) and 70 (64 x 128).  32-bit results go by the same costs, which
+// were not measured for them, and K is not in them.  Up to four rows operands go straight to
 // registers, two steps in flight: one row through 28672 x 8192 takes 41 us, 45 by 32 x 32 tiles, through 4096 x 11008 9.8 and 10.1; eight rows
 // through 11008 x 4096 12.7 and 9.7.
 enum F8mm { F8MM_32x32, F8MM_32x64, F8MM_64x64, F8MM_64x128, F8MM_128x128, F8MM_256x256, F8MM_ROWS };

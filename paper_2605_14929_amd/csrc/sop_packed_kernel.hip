@@ -90,8 +90,9 @@ __device__ __forceinline__ void store_y(const PackedMmParams& p, int m, int n, v
 
 // ---- few rows of x: FM x 16 of them by 16 columns a workgroup, K dealt out to its W wavefronts, 128 elements a step, U steps of a
 // wavefront in flight: a lane takes 32 neighbouring codes of its row, eight for each of four matrix instructions, and the same elements of x.
-// One row through 4096 x 11008 (28 MB of codes and scale words) takes 11.5 us, through 28672 x 8192 (147 MB) 48; more steps in flight or more
-// wavefronts take as long (12.2 for four steps): a weight's four to five instructions and its look-up in LDS bound it, sixteen rows (18.3) their loads too.
+// One row through 4096 x 11008 (28 MB of codes and scale words) takes 10.6 us, 11.6 where they lie in HBM, through 28672 x 8192 (147 MB) 41 and 44; sixteen
+// rows 17.4.  More steps in flight or more wavefronts take as long; nothing is busy most of the time (vector ALUs 31 % of the cycles, LDS 13 %), and what
+// would shorten a wavefront's way from a code to its weight - codes looked up in pairs, as below - has not been built here.
 // WPL: scale words of 32 codes (4, 2 or 1 for g = 8, 16 and more).
 template <int NB, int FM, int U, int W, int WPL>
 __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParams p)
@@ -190,8 +191,8 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
 // ---- narrow tiles, K dealt out: 32 FM x 32 FN of y a workgroup, its eight wavefronts taking steps of 64 S elements in turn.  A wavefront has its
 // step of x in a place of its own in LDS (no barrier before the sums are joined), and forms the weights in the registers that the matrix
 // instructions read: a lane takes 32 neighbouring codes of its row, eight for each of four instructions, and the same elements of x.  The next
-// step is asked for when this one's operands have been read.  128 x 4096 x 4096 of 4-bit codes takes 14.5 us (wide tiles of 128 x 128: 60), 32 x 11008
-// x 4096 17.8: forming the weights once for 32 to 128 rows bounds it.
+// step is asked for when this one's operands have been read.  128 x 4096 x 4096 of 4-bit codes takes 11.7 us (wide tiles of 128 x 128: 60), 32 x 11008
+// x 4096 16.1: forming the weights, code by code, once for 32 to 128 rows bounds it.
 template <int NB, int FM, int FN, int S, int WPL>
 __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
@@ -331,8 +332,9 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
 // instruction stand a part of the look-ups and of the scale word of an eight, and a part of the products of the eight before.  A matrix
 // instruction (32 cycles) hides seven others of its wavefront, so what a weight costs in instructions is what counts: two codes
 // are looked up at once, in a table of the 4^NB pairs of either codebook.  Before a step's last sixteen elements comes its barrier: the
-// next step is there, this one's place is free.  2048 x 11008 x 4096 of 4-bit codes takes 203 us, 910 TFLOP/s: matrix instructions are busy 40 % of the
-// cycles, the look-ups and products of the weights, once a tile, fill the others.
+// next step is there, this one's place is free.  2048 x 11008 x 4096 of 4-bit codes takes 194 us, 950 TFLOP/s: matrix instructions are busy 41 % of the
+// cycles; the others go to the look-ups and products of the weights, formed anew by every row of tiles, and 44 % of the cycles in which LDS is at work to
+// bank conflicts of the pairs' look-ups.
 template <int NB, int E, int F, bool G8>
 __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {

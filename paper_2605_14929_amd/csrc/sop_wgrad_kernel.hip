@@ -8,8 +8,8 @@
 // Both operands arrive with the summed index outermost, the matrix instruction wants it innermost.  Where dy's rows lie on 16 bytes,
 // both go to LDS as they are, straight from memory, and are turned by LDS's transposing reads (a sixteen-lane group reads four rows of
 // sixteen 16-bit, or eight rows of sixteen 8-bit elements and receives the columns); the checkpoint stays in 8 bits until then.
-// Otherwise a thread loads eight rows of two (dy) or four (x) columns, turns them in registers, and writes columns (8192 x 11008 x 4096 in the simple
-// form of that 1388 us, by the transposing reads 632).
+// Otherwise a thread loads eight rows of two (dy) or four (x) columns, turns them in registers, and writes columns (8192 x 11007 x 4096 takes 1339 us
+// so, 8192 x 11008 x 4096 by the transposing reads 611).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -41,8 +41,9 @@ __device__ __forceinline__ void store_dw(const WgradParams& p, int n, int k, v4f
         }
     } else {
         float* w = reinterpret_cast<float*>(p.dw) + at;
-        // whole lines are written past the caches: 64 x 11008 x 4096 takes 38 us so, 41.5 otherwise, 777 x 1531 x 5024 20.8 and 22.9 (lines in parts, 26 x
-        // 1920 x 4793, 26 and 14)
+        // Whole lines are written past the caches.  Two results in turn: 64 x 11008 x 4096 takes 36.6 us so and 39.5 otherwise, with an update that reads
+        // them 114 and 125; 777 x 1531 x 5024 21.3 and 23.1, 36 and 36; but 2048 x 4096 x 4096 67 and 64, 98 and 93, and 64 x 4096 x 4096 17.0 and
+        // 16.4, 47 and 45.  (Lines in parts, 26 x 1920 x 4793: 26 and 14.)
         const bool lines = ((reinterpret_cast<uintptr_t>(p.dw) | (unsigned long long)p.lddw * 4) & 127) == 0;
         if (four) {
             if (p.accumulate) v += reinterpret_cast<const FourWords*>(w)->v;
@@ -182,7 +183,7 @@ template <bool E5M2, bool HIGH> __device__ __forceinline__ int two_rows(int c, f
 
 // ---- rows of dy on 16 bytes.  64 rows a step, three steps in LDS: one being multiplied, one on its way or there, one being asked for.
 // In LDS a row is chunks of 16 bytes; chunk c of row m stands at position c ^ 4 (m & 3) (dy, rows of 256 bytes) or c ^ 2 (m / 2 & 3) (x, rows of
-// 128), so that the rows that 32 lanes read together fall on different banks.  777 x 1531 x 5024 takes 20.5 us: thirteen
+// 128), so that the rows that 32 lanes read together fall on different banks.  777 x 1531 x 5024 takes 19.7 us: thirteen
 // steps of two workgroups a compute unit (12 us), 31 MB of results (6 us), and the first loads.
 template <int BN, int BK, int WR, int WC, bool X5>
 __global__ __launch_bounds__(WR * WC * 64) void wgrad_turn_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
@@ -446,8 +447,8 @@ __global__ __launch_bounds__(512) void wgrad_split_kernel(const WgradParams p, i
 // work.  While sixteen rows are multiplied (sixteen matrix instructions), behind each of them stands a sixteenth of: the reads of the next
 // sixteen rows of dy, the reads of the codes after the next, the conversion of the next codes, the loads of the step after the next.  A
 // wavefront issues an instruction in four cycles, so a matrix instruction (32 cycles) hides seven others: they are dealt out evenly.
-// Halfway through a step comes its barrier: the next step has arrived, the place of the step before is free.  8192 x 11008 x 4096 takes 632 us,
-// 1170 TFLOP/s (a large library product in bf16 1450); the matrix instructions are busy 57 % of the cycles at a clock that they lower.
+// Halfway through a step comes its barrier: the next step has arrived, the place of the step before is free.  8192 x 11008 x 4096 takes 611 us,
+// 1210 TFLOP/s (a large library product in bf16 1619); the matrix instructions are busy 57 % of the cycles at a clock that they lower.
 template <bool X5>
 __global__ __launch_bounds__(256) void wgrad_large_kernel(const WgradParams p, int tiles_n, int tiles_k, int group)
 {
