@@ -590,6 +590,101 @@ typedef struct {
  * DEVICE, bf16, 16-byte aligned, row stride ldx a multiple of 8 elements, K and ldx at most 2^22; y [M, N] DEVICE, bf16, row stride ldy; sums are binary32. */
 sop_status sop_packed_matmul(sop_ctx* ctx, const void* x_dev, int64_t ldx, const sop_packed_weights* w, int64_t M, void* y_dev, int64_t ldy, void* hip_stream);
 
+/* ---- what stands around such a layer in a block of a model: products with an epilogue, norms with the residual stream, gradients clipped together.
+ * Under the same rules as the calls above: nothing is kept in the context, calls may overlap, all are asynchronous on hip_stream, allocate nothing, may be
+ * captured into a graph, and take workspace from the caller where they need any.  All arithmetic is binary32 (sums over rows and tensors: see there);
+ * results are rounded once.  Infinities and NaN go the way of the formulas.  Matrices of numbers are fp32 or bf16 on any alignment of an element, row strides in elements. */
+
+/* Epilogue of a product with sums v: z = v + bias, y = residual + scale act(z).
+ *   SOP_ACT_RELU       max(z, 0)                SOP_ACT_SILU       z / (1 + exp(-z))
+ *   SOP_ACT_GELU       z Phi(z), Phi the normal distribution
+ *   SOP_ACT_GELU_TANH  z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
+ * An activation of -infinity is its limit, 0.
+ *   bias      DEVICE, N floats, or NULL
+ *   residual  DEVICE, [M, N] of y's type, row stride ldr, or NULL; it may be y itself (then with y's row stride)
+ *   z         DEVICE, [M, N] of y's type, row stride ldz, or NULL: z is kept for sop_fp8_linear_grad */
+typedef enum { SOP_ACT_NONE = 0, SOP_ACT_RELU = 1, SOP_ACT_SILU = 2, SOP_ACT_GELU = 3, SOP_ACT_GELU_TANH = 4 } sop_act;
+typedef struct {
+    const float* bias;
+    const void* residual; int64_t ldr;
+    void* z; int64_t ldz;
+    sop_act act;
+    float scale;
+} sop_epilogue;
+
+/* sop_fp8_matmul (w_transposed = 0 or 1) with an epilogue. */
+sop_status sop_fp8_linear(sop_ctx* ctx, const sop_f8_matrix* x, const sop_f8_matrix* w, int w_transposed, int64_t M, int64_t N, int64_t K,
+                          const sop_epilogue* epilogue, void* y, sop_dtype dtype, int64_t ldy, void* hip_stream);
+
+/* sop_packed_matmul with an epilogue; y, residual and z are bf16. */
+sop_status sop_packed_linear(sop_ctx* ctx, const void* x_dev, int64_t ldx, const sop_packed_weights* w, int64_t M, const sop_epilogue* epilogue,
+                             void* y_dev, int64_t ldy, void* hip_stream);
+
+/* Gradient of an epilogue, from the z that it kept: dz = scale dy act'(z) (relu: 0 at 0), as numbers of dy's type (for sop_fp8_weight_grad), in 8 bits (for
+ * the input gradient; formed from the binary32 values), and dbias = sum of dz over the rows.  The residual's gradient is dy.
+ *   dy [M, N], z [M, N] of dy's type (NULL without an activation), dz [M, N] of dy's type or NULL; dz8 of block_rows 1
+ *   dbias: DEVICE, N floats, or NULL; sums over rows are binary32 within some hundred rows and binary64 above them, in an order fixed by the sizes and the GPU
+ *   workspace: DEVICE, 16-byte aligned, sop_fp8_linear_grad_workspace() bytes; NULL where dbias is */
+sop_status sop_fp8_linear_grad_workspace(sop_ctx* ctx, int64_t M, int64_t N, size_t* bytes);
+sop_status sop_fp8_linear_grad(sop_ctx* ctx, const void* dy_dev, int64_t lddy, const void* z_dev, int64_t ldz, sop_dtype dtype, int64_t M, int64_t N,
+                               sop_act act, float scale, void* dz_dev, int64_t lddz, const sop_f8_matrix* dz8, float* dbias_dev,
+                               void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Norms before and after a block, with its gate and residual scale: y is what the block computed, r the residual stream,
+ *   x = y / sqrt(mean of y^2 over the row + eps) after    (without `after`: x = y)
+ *   s = r + scale gate x                                  n = s / sqrt(mean of s^2 over the row + eps) before
+ * n is formed from the binary32 sum, not from the rounded one.
+ *   y [M, D], r [M, D], s [M, D] of r's type; y NULL: s is r, and is not written (s NULL).  s may be r itself (with its row stride).
+ *   after, before: DEVICE, D floats, or NULL: no such norm.  gate: DEVICE or NULL, [groups, D], row j for rows j M / groups up; groups divides M
+ *   n: DEVICE or NULL, numbers of n_dtype;  n8: NULL, or 8 bits (block_rows 1).  At least one of them with `before`, neither without.
+ * eps is at least 2^-64; D at most 2^20. */
+typedef struct {
+    const float* after; const float* before;
+    const void* gate; int64_t ld_gate; sop_dtype gate_dtype; int64_t groups;
+    float scale, eps;
+} sop_residual_norm_opts;
+sop_status sop_residual_norm(sop_ctx* ctx, const sop_residual_norm_opts* opts, int64_t M, int64_t D,
+                             const void* y_dev, int64_t ld_y, sop_dtype y_dtype, const void* r_dev, int64_t ld_r, sop_dtype r_dtype,
+                             void* s_dev, int64_t ld_s, void* n_dev, int64_t ld_n, sop_dtype n_dtype, const sop_f8_matrix* n8, void* hip_stream);
+
+/* Its gradients at the stored s, from ds (the gradient that s gets elsewhere; NULL: none) and dn:
+ *   dr = ds + (p - h mean(p h)) / sqrt(mean s^2 + eps), h = s / sqrt(mean s^2 + eps), p = before dn      (without `before`: dr = ds)
+ *   dy = (q - u mean(q u)) / sqrt(mean y^2 + eps), u = y / sqrt(mean y^2 + eps), q = scale gate after dr  (without `after`: dy = scale gate dr, u = y)
+ *   dbefore = sum of dn h, dafter = sum of scale gate dr u, over all rows; dgate[j] = sum of scale after dr u over the rows of gate row j
+ * formed from the binary32 dr.  Types: s, ds and dr of r_dtype; y, dn and dy of y_dtype; dgate of gate_dtype, row stride ld_dgate; dbefore, dafter: D floats.
+ * s and dn are not looked at without `before`; y NULL: nothing of y is.  dy8 (NULL or block_rows 1): dy in 8 bits, formed from the binary32 values.  dbefore, dafter and
+ * dgate are NULL where they are not wanted (dafter without `after`, dgate without a gate).  Sums over rows as in sop_fp8_linear_grad.
+ *   workspace: DEVICE, 16-byte aligned, sop_residual_norm_grad_workspace() bytes */
+typedef struct {
+    const void* ds; int64_t ld_ds;
+    const void* dn; int64_t ld_dn;
+    const void* s; int64_t ld_s;
+    const void* y; int64_t ld_y;
+    void* dr; int64_t ld_dr;
+    void* dy; int64_t ld_dy;
+    const sop_f8_matrix* dy8;
+    float* dbefore; float* dafter;
+    void* dgate; int64_t ld_dgate;
+    sop_dtype r_dtype, y_dtype;
+} sop_residual_norm_grads;
+sop_status sop_residual_norm_grad_workspace(sop_ctx* ctx, int64_t M, int64_t D, int64_t groups, size_t* bytes);
+sop_status sop_residual_norm_grad(sop_ctx* ctx, const sop_residual_norm_opts* opts, int64_t M, int64_t D, const sop_residual_norm_grads* grads,
+                                  void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* The norm of all gradients of a model, norm = sqrt(sum of x^2 over all elements of all tensors) (squares and sums in binary64, in an order fixed by the
+ * sizes and the GPU), and the gradients times min(1, most / norm): a factor rounded to binary32, products rounded to out's type.
+ *   tensors  HOST, count of them, read before the call returns: x DEVICE, n >= 0 elements of x_dtype one after the other; out DEVICE, n elements of out_dtype:
+ *            x itself (in place, with its type; not touched where the factor is 1) or memory that overlaps no x, and no other out; n at most 2^36
+ *   norm     DEVICE, one float
+ *   workspace: DEVICE, 8-byte aligned, sop_clip_grads_workspace() bytes
+ * The factor is formed from the norm in binary64, norm is that rounded to binary32 (infinity beyond its range).  A NaN among the gradients makes all outputs NaN; an
+ * infinity makes the finite ones 0.  sop_grad_norm looks at no out and writes the norm alone. */
+typedef struct { const void* x; void* out; int64_t n; sop_dtype x_dtype, out_dtype; } sop_grad;
+sop_status sop_clip_grads_workspace(sop_ctx* ctx, int64_t count, size_t* bytes);
+sop_status sop_grad_norm(sop_ctx* ctx, const sop_grad* tensors, int64_t count, float* norm_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+sop_status sop_clip_grads(sop_ctx* ctx, const sop_grad* tensors, int64_t count, float most, float* norm_dev, void* workspace_dev, size_t workspace_bytes,
+                          void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

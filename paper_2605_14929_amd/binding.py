@@ -3,7 +3,9 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import numpy as np
 
@@ -153,6 +155,19 @@ def lib():
         L.sop_fp8_gated_grad.argtypes = [C.c_void_p, C.POINTER(_F8Matrix), C.POINTER(_F8Matrix), C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64,
                                          C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(_F8Matrix), C.POINTER(_F8Matrix), C.c_void_p]
         L.sop_packed_matmul.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_Packed), C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        epilogue = [C.POINTER(_Epilogue)]
+        L.sop_fp8_linear.argtypes = L.sop_fp8_matmul.argtypes[:7] + epilogue + L.sop_fp8_matmul.argtypes[7:]
+        L.sop_packed_linear.argtypes = L.sop_packed_matmul.argtypes[:5] + epilogue + L.sop_packed_matmul.argtypes[5:]
+        L.sop_fp8_linear_grad_workspace.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]
+        L.sop_fp8_linear_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int, C.c_float, C.c_void_p,
+                                          C.c_int64, C.POINTER(_F8Matrix), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sop_residual_norm.argtypes = [C.c_void_p, C.POINTER(_NormOpts), C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_int,
+                                        C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.POINTER(_F8Matrix), C.c_void_p]
+        L.sop_residual_norm_grad_workspace.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]
+        L.sop_residual_norm_grad.argtypes = [C.c_void_p, C.POINTER(_NormOpts), C.c_int64, C.c_int64, C.POINTER(_NormGrads), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sop_clip_grads_workspace.argtypes = [C.c_void_p, C.c_int64, C.POINTER(C.c_size_t)]
+        L.sop_grad_norm.argtypes = [C.c_void_p, C.c_char_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]   # (sop_grad, packed)
+        L.sop_clip_grads.argtypes = [C.c_void_p, C.c_char_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.sop_layer_shift.argtypes = [C.POINTER(C.c_int64), C.c_int64, ScaleFmt, C.POINTER(C.c_int), C.POINTER(C.c_double)]
         _lib = L
     return _lib
@@ -302,6 +317,38 @@ class Outputs:
 
 
 E4M3, E5M2 = 0, 1
+RELU, SILU, GELU, GELU_TANH = 1, 2, 3, 4
+
+
+class _Epilogue(C.Structure):
+    """sop_epilogue"""
+    _fields_ = [("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64), ("z", C.c_void_p), ("ldz", C.c_int64), ("act", C.c_int), ("scale", C.c_float)]
+
+
+class _NormOpts(C.Structure):
+    """sop_residual_norm_opts"""
+    _fields_ = [("after", C.c_void_p), ("before", C.c_void_p), ("gate", C.c_void_p), ("ld_gate", C.c_int64), ("gate_dtype", C.c_int), ("groups", C.c_int64),
+                ("scale", C.c_float), ("eps", C.c_float)]
+
+
+class _NormGrads(C.Structure):
+    """sop_residual_norm_grads"""
+    _fields_ = [("ds", C.c_void_p), ("ld_ds", C.c_int64), ("dn", C.c_void_p), ("ld_dn", C.c_int64), ("s", C.c_void_p), ("ld_s", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("dr", C.c_void_p), ("ld_dr", C.c_int64), ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("dy8", C.POINTER(_F8Matrix)), ("dbefore", C.c_void_p), ("dafter", C.c_void_p),
+                ("dgate", C.c_void_p), ("ld_dgate", C.c_int64), ("r_dtype", C.c_int), ("y_dtype", C.c_int)]
+
+
+_GRAD = struct.Struct("@QQqii")                                       # sop_grad
+
+
+class ResidualNormGrads(NamedTuple):
+    """What Context.residual_norm_grad returns; None where there is nothing of it."""
+    dr: object
+    dy: object
+    dy8: object
+    dbefore: object
+    dafter: object
+    dgate: object
 
 
 def _up(n, unit):
@@ -331,6 +378,17 @@ def _room(torch, R, Cc, unit, dtype, device):
     """An uninitialised [R, Cc] of bytes laid out so, and the distance of its rows."""
     ld = -(-Cc // unit) * unit
     return torch.empty_strided((R, Cc), (ld, 1), dtype=dtype, device=device), ld
+
+
+def _dense(t):
+    """Whether a tensor's elements fill a range of memory, in whatever order of its dimensions."""
+    n = 1
+    for size, step in sorted(zip(t.shape, t.stride()), key=lambda d: (d[1], d[0])):
+        if size != 1:
+            if step != n:
+                return False
+            n *= size
+    return True
 
 
 class Fp8Blocks:
@@ -928,3 +986,233 @@ class Context:
         if s:
             _check(s, self._h)
         return out
+
+    # ---- what stands around such a layer in a block of a model
+
+    def _vector(self, v, n, what):
+        """The address of n float32 on the context's GPU, one after the other; None of None."""
+        if v is None:
+            return None
+        if v.get_device() != self.device:
+            raise SopError(1, f"{what} must be on the context's GPU (no CPU fallback)")
+        if v.dtype is not self._f32 or not v.is_contiguous():
+            raise SopError(1, f"{what} must be contiguous float32")
+        if v.numel() != n or v.dim() != 1:
+            raise SopError(2, f"{what} must have {n} elements")
+        return v.data_ptr()
+
+    def _matrix(self, x, shape, dt, what):
+        """(address, row stride) of a matrix of numbers of one shape and sop_dtype."""
+        xt, ld = self._numbers(x, what)
+        if x.shape != shape:
+            raise SopError(2, f"{what} must be {shape[0]} x {shape[1]}")
+        if xt != dt:
+            raise SopError(1, f"{what} is {x.dtype}, which does not go with the other operands")
+        return x.data_ptr(), ld
+
+    def _epilogue(self, M, N, out, dt, ldy, bias, act, residual, scale, keep):
+        """(sop_epilogue, z or None)"""
+        r, ldr = (None, 0) if residual is None else self._matrix(residual, (M, N), dt, "residual")
+        z = out.new_empty((M, N)) if keep else None
+        return _Epilogue(self._vector(bias, N, "bias"), r, ldr, None if z is None else z.data_ptr(), N, act or 0, scale), z
+
+    def fp8_linear(self, x: Fp8Blocks, w: Fp8Blocks, bias=None, act=None, residual=None, scale: float = 1.0, keep: bool = False, transposed: bool = False, dtype=None,
+                   out=None, stream=None):
+        """sop_fp8_linear: y = residual + scale act(z), z = x w^T + bias, of x [M, K] (rows = 1) and w [N, K] (rows = 128; transposed as in fp8_matmul).  bias [N]
+        float32; act: None, RELU, SILU, GELU (the exact one) or GELU_TANH; residual [M, N] of y's type, which may be `out`; dtype / out as in fp8_matmul.  keep: returns
+        (y, z), z of y's type, for fp8_linear_grad."""
+        if stream is not None:
+            return self._on(stream, self.fp8_linear, x, w, bias, act, residual, scale, keep, transposed, dtype, out)
+        self._here(x, w)
+        if transposed and w._t is None:
+            raise SopError(1, "the transposed product needs the weight's codes_t (fp8_quantize(..., transposed=True))")
+        M, K = x.shape
+        Kw, N = w.shape if transposed else w.shape[::-1]
+        if K != Kw:
+            raise SopError(2, f"x has rows of {K} elements, the weight wants {Kw}")
+        out, dt, ldy = self._result(out, M, N, dtype, self._bf16, x.codes)
+        e, z = self._epilogue(M, N, out, dt, ldy, bias, act, residual, scale, keep)
+        s = self._lib.sop_fp8_linear(self._h, x._m, w._t if transposed else w._m, transposed, M, N, K, e, out.data_ptr(), dt, ldy, self._raw_stream(self.device))
+        if s:
+            _check(s, self._h)
+        return (out, z) if keep else out
+
+    def packed_linear(self, x, w: PackedWeights, bias=None, act=None, residual=None, scale: float = 1.0, keep: bool = False, out=None, stream=None):
+        """sop_packed_linear: fp8_linear with x [M, K] bfloat16 and a packed layer; y, residual and z are bfloat16."""
+        if stream is not None:
+            return self._on(stream, self.packed_linear, x, w, bias, act, residual, scale, keep, out)
+        self._here(w)
+        _, ldx = self._numbers(x, "x", True)
+        (M, K), (N, Kw) = x.shape, w.shape
+        if K != Kw:
+            raise SopError(2, f"x has rows of {K} elements, the layer wants {Kw}")
+        out, dt, ldy = self._result(out, M, N, self._bf16, self._bf16, x)
+        e, z = self._epilogue(M, N, out, dt, ldy, bias, act, residual, scale, keep)
+        s = self._lib.sop_packed_linear(self._h, x.data_ptr(), ldx, w._w, M, e, out.data_ptr(), ldy, self._raw_stream(self.device))
+        if s:
+            _check(s, self._h)
+        return (out, z) if keep else out
+
+    def _workspace(self, size, like, *sizes):
+        """(address, bytes, what keeps it) of what a call named by its _workspace entry point needs."""
+        import torch
+        n = C.c_size_t()
+        _check(size(self._h, *sizes, C.byref(n)), self._h)
+        ws = torch.empty(max(n.value, 16), dtype=torch.uint8, device=like.device)
+        return ws.data_ptr(), ws.numel(), ws
+
+    def fp8_linear_grad(self, dy, z=None, act=None, scale: float = 1.0, bias: bool = True, fmt=E5M2, stream=None):
+        """sop_fp8_linear_grad: (dz, dz8, dbias) of the epilogue act / scale from dy [M, N] and the z that fp8_linear kept: numbers of dy's type (for fp8_weight_grad; dy
+        itself where there is neither activation nor scale), 8 bits (for the input gradient), float32 sums over the rows (bias = False: None)."""
+        if stream is not None:
+            return self._on(stream, self.fp8_linear_grad, dy, z, act, scale, bias, fmt)
+        dt, ldd = self._numbers(dy, "dy")
+        M, N = dy.shape
+        if act and z is None:
+            raise SopError(1, "the gradient of an activation needs z")
+        zp, ldz = self._matrix(z, (M, N), dt, "z") if act else (None, 0)
+        dz = dy if not act and scale == 1.0 else dy.new_empty((M, N))
+        dz8 = Fp8Blocks.empty(M, N, fmt, dy.device)
+        db, at, size = None, None, 0
+        if bias:
+            db = dy.new_empty(N, dtype=self._f32)
+            at, size, ws = self._workspace(self._lib.sop_fp8_linear_grad_workspace, dy, M, N)
+        s = self._lib.sop_fp8_linear_grad(self._h, dy.data_ptr(), ldd, zp, ldz, dt, M, N, act or 0, scale, None if dz is dy else dz.data_ptr(), N, dz8._m,
+                                          None if db is None else db.data_ptr(), at, size, self._raw_stream(self.device))
+        if s:
+            _check(s, self._h)
+        return dz, dz8, db
+
+    def _norm_opts(self, M, D, after, gate, scale, before, eps):
+        o = _NormOpts(self._vector(after, D, "after"), self._vector(before, D, "before"), None, 0, F32, 0, scale, eps)
+        if gate is not None:
+            g = gate.view(1, D) if gate.dim() == 1 and gate.shape[0] == D else gate
+            o.gate_dtype, o.ld_gate = self._numbers(g, "gate")
+            if g.shape[1] != D or g.shape[0] < 1 or M % g.shape[0]:
+                raise SopError(2, f"gate must have rows of {D} elements, and a number of them that divides {M}")
+            o.gate, o.groups = g.data_ptr(), g.shape[0]
+        return o
+
+    def residual_norm(self, r, y=None, after=None, gate=None, scale: float = 1.0, before=None, eps: float = 1e-6, dtype=None, fmt=None, out=None, stream=None):
+        """sop_residual_norm: (s, n, n8) of the residual stream r [M, D] and a block's output y [M, D]: s = r + scale gate y after / rms(y), of r's type (r itself without
+        y), and s before / rms(s) as numbers of `dtype` (n) and in 8 bits of `fmt` (n8), each None where it is not asked for.  after, before: [D] float32, or None: no
+        such norm.  gate: [D], or [G, D] with G a divisor of M: each row for M / G rows.  out: where s goes; it may be r."""
+        if stream is not None:
+            return self._on(stream, self.residual_norm, r, y, after, gate, scale, before, eps, dtype, fmt, out)
+        dr, ldr = self._numbers(r, "r")
+        M, D = r.shape
+        o = self._norm_opts(M, D, after, gate, scale, before, eps)
+        yp, ldy, dty, sp, lds, s = None, 0, dr, None, 0, r
+        if y is not None:
+            dty, ldy = self._numbers(y, "y")
+            if y.shape != r.shape:
+                raise SopError(2, "r and y must have one shape")
+            s, _, lds = self._result(out, M, D, r.dtype, r.dtype, r)
+            yp, sp = y.data_ptr(), s.data_ptr()
+        elif out is not None:
+            raise SopError(1, "without y there is no sum to write")
+        n, dn = None, F32
+        if dtype is not None:
+            n, dn, _ = self._result(None, M, D, dtype, None, r)
+        n8 = None if fmt is None else Fp8Blocks.empty(M, D, fmt, r.device)
+        st = self._lib.sop_residual_norm(self._h, o, M, D, yp, ldy, dty, r.data_ptr(), ldr, dr, sp, lds, None if n is None else n.data_ptr(), D, dn,
+                                         None if n8 is None else n8._m, self._raw_stream(self.device))
+        if st:
+            _check(st, self._h)
+        return s, n, n8
+
+    def residual_norm_grad(self, ds, dn=None, s=None, before=None, y=None, after=None, gate=None, scale: float = 1.0, eps: float = 1e-6, fmt=None, stream=None):
+        """sop_residual_norm_grad: ResidualNormGrads(dr, dy, dy8, dbefore, dafter, dgate) of residual_norm with these operands, from the gradient ds that s gets elsewhere
+        (None: none) and dn.  s: the sum that was returned (with `before`).  Types: s, ds and dr alike, y, dn and dy alike (without y, dn of either type); dy8 is dy in
+        8 bits of `fmt` (None: not made); dbefore and dafter are float32, dgate of gate's type and shape."""
+        if stream is not None:
+            return self._on(stream, self.residual_norm_grad, ds, dn, s, before, y, after, gate, scale, eps, fmt)
+        if (before is None) != (dn is None) or (before is None) != (s is None):
+            raise SopError(1, "before, dn and s are given together")
+        like = ds if ds is not None else s
+        if like is None:
+            raise SopError(1, "no gradient to go from: neither ds nor dn")
+        dt, _ = self._numbers(like, "ds" if ds is not None else "s")
+        shape = M, D = like.shape
+        o = self._norm_opts(M, D, after, gate, scale, before, eps)
+        of_y = y if y is not None else dn
+        dty = dt if of_y is None else self._numbers(of_y, "y or dn")[0]
+        t = _NormGrads(r_dtype=dt, y_dtype=dty)
+        if ds is not None:
+            t.ds, t.ld_ds = self._matrix(ds, shape, dt, "ds")
+        if before is not None:
+            t.s, t.ld_s = self._matrix(s, shape, dt, "s")
+            t.dn, t.ld_dn = self._matrix(dn, shape, dty, "dn")
+        dr, dy, dy8 = like.new_empty(shape), None, None
+        t.dr, t.ld_dr = dr.data_ptr(), D
+        if y is not None:
+            t.y, t.ld_y = self._matrix(y, shape, dty, "y")
+            dy = y.new_empty(shape)
+            t.dy, t.ld_dy = dy.data_ptr(), D
+            if fmt is not None:
+                dy8 = Fp8Blocks.empty(M, D, fmt, like.device)
+                t.dy8 = C.pointer(dy8._m)
+        elif fmt is not None:
+            raise SopError(1, "without y there is no dy8")
+        db = None if before is None else before.new_empty(D)
+        da = None if after is None else after.new_empty(D)
+        dg = None if gate is None else gate.new_empty(gate.shape)
+        t.dbefore, t.dafter = None if db is None else db.data_ptr(), None if da is None else da.data_ptr()
+        if dg is not None:
+            t.dgate, t.ld_dgate = dg.data_ptr(), D
+        at, size, ws = self._workspace(self._lib.sop_residual_norm_grad_workspace, like, M, D, o.groups)
+        st = self._lib.sop_residual_norm_grad(self._h, o, M, D, t, at, size, self._raw_stream(self.device))
+        if st:
+            _check(st, self._h)
+        return ResidualNormGrads(dr, dy, dy8, db, da, dg)
+
+    def _grads(self, tensors, outs):
+        """The tensors as sop_grad, packed, and how many."""
+        import torch
+        parts, dev, dts = [], self.device, self._dtypes
+        if outs is not None and len(outs) != len(tensors):
+            raise SopError(2, "as many outs as tensors")
+        for i, x in enumerate(tensors):
+            o = x if outs is None else outs[i]
+            if x is None and o is None:
+                continue                                                    # (a weight without a gradient)
+            if not isinstance(x, torch.Tensor) or not isinstance(o, torch.Tensor):
+                raise SopError(1, "gradients are tensors")
+            dx, do = dts.get(x.dtype), dts.get(o.dtype)
+            if dx is None or do is None:
+                raise SopError(1, "gradients are float32 or bfloat16")
+            if x.get_device() != dev or o.get_device() != dev:
+                raise SopError(1, "gradients must be on the context's GPU (no CPU fallback)")
+            if x.shape != o.shape:
+                raise SopError(2, "a gradient and its out have one shape")
+            if not x.is_contiguous() or (o is not x and not o.is_contiguous()):
+                if not _dense(x) or (o is not x and o.stride() != x.stride()):
+                    raise SopError(2, "a gradient's elements lie one after the other, and its out's in the same order")
+            parts.append(_GRAD.pack(x.data_ptr(), o.data_ptr(), x.numel(), dx, do))
+        return b"".join(parts), len(parts)
+
+    def grad_norm(self, tensors, stream=None):
+        """sop_grad_norm: the norm of all elements of all tensors (float32 or bfloat16; None is passed over), a [1] float32 tensor."""
+        if stream is not None:
+            return self._on(stream, self.grad_norm, tensors)
+        return self._norm_of(tensors, None, None)
+
+    def clip_grads(self, tensors, most: float, out=None, stream=None):
+        """sop_clip_grads: the tensors times min(1, most / their norm), in place or into `out` (a tensor for each, float32 or bfloat16, none of them memory of
+        another gradient); returns the norm, a [1] float32 tensor."""
+        if stream is not None:
+            return self._on(stream, self.clip_grads, tensors, most, out)
+        return self._norm_of(tensors, float(most), out)
+
+    def _norm_of(self, tensors, most, out):
+        import torch
+        tensors = list(tensors)
+        packed, n = self._grads(tensors, out)
+        norm = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", self.device))
+        at, size, ws = self._workspace(self._lib.sop_clip_grads_workspace, norm, n)
+        st = self._raw_stream(self.device)
+        s = (self._lib.sop_grad_norm(self._h, packed, n, norm.data_ptr(), at, size, st) if most is None
+             else self._lib.sop_clip_grads(self._h, packed, n, most, norm.data_ptr(), at, size, st))
+        if s:
+            _check(s, self._h)
+        return norm

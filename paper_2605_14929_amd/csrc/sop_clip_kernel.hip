@@ -1,0 +1,151 @@
+// The norm of many tensors together, norm = sqrt(sum of x^2), and the tensors times min(1, most / norm).
+//
+// Two passes, bound by HBM: the factor is known only when everything has been read.  A launch takes the addresses of up to 96 tensors in its
+// arguments, and the tensors in chunks of 8192 elements, which workgroups take in turn.  Squares are formed and added in binary64: exact squares, and nothing
+// overflows.  Each workgroup leaves one partial sum, and every workgroup of the second pass adds them all up for itself, in one order, so that no third
+// launch stands between.  The second pass goes through the tensors from their end, what the first has read last being in the last-level cache.
+#include <hip/hip_runtime.h>
+
+#include "sop_block.h"
+
+namespace sopk {
+
+struct __attribute__((packed, aligned(4))) Four32 { v4i v; };
+struct __attribute__((packed, aligned(2))) Eight16 { v4i v; };
+
+// chunk c of the list: which tensor, and where in it
+struct Piece { int e; long long from, left; };
+__device__ __forceinline__ Piece piece_of(const ClipParams& p, int c)
+{
+    int lo = 0, hi = p.count - 1;
+    while (lo < hi) { const int mid = (lo + hi) >> 1; if (c < p.e[mid].end) hi = mid; else lo = mid + 1; }
+    const long long from = (long long)(c - (lo ? p.e[lo - 1].end : 0)) * SOP_K_CLIP_CHUNK;
+    return Piece{lo, from, p.e[lo].n - from};
+}
+// eight elements a thread; zeros beyond the end
+__device__ __forceinline__ void eight(const void* x, bool bf16, long long at, long long left, float (&v)[8])
+{
+    if (left >= 8) {
+        if (bf16) {
+            const v4i r = reinterpret_cast<const Eight16*>(reinterpret_cast<const uint16_t*>(x) + at)->v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __int_as_float((i & 1) ? r[i >> 1] & (int)0xFFFF0000 : r[i >> 1] << 16);
+        } else {
+            const Four32* q = reinterpret_cast<const Four32*>(reinterpret_cast<const float*>(x) + at);
+            const v4i a = q[0].v, b = q[1].v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = __int_as_float(a[i]); v[4 + i] = __int_as_float(b[i]); }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = i >= left ? 0.0f : bf16 ? __uint_as_float((unsigned int)reinterpret_cast<const uint16_t*>(x)[at + i] << 16) : reinterpret_cast<const float*>(x)[at + i];
+}
+__device__ __forceinline__ void put_eight(void* y, bool bf16, long long at, long long left, const float (&v)[8])
+{
+    if (left >= 8) {
+        if (bf16) {
+            reinterpret_cast<Eight16*>(reinterpret_cast<uint16_t*>(y) + at)->v = v4i{(int)bf16_pair(v[0], v[1]), (int)bf16_pair(v[2], v[3]), (int)bf16_pair(v[4], v[5]), (int)bf16_pair(v[6], v[7])};
+        } else {
+            Four32* q = reinterpret_cast<Four32*>(reinterpret_cast<float*>(y) + at);
+            q[0].v = __builtin_bit_cast(v4i, v4f{v[0], v[1], v[2], v[3]});
+            q[1].v = __builtin_bit_cast(v4i, v4f{v[4], v[5], v[6], v[7]});
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= left) continue;
+        if (bf16) reinterpret_cast<uint16_t*>(y)[at + i] = (uint16_t)bf16_bits(v[i]);
+        else reinterpret_cast<float*>(y)[at + i] = v[i];
+    }
+}
+// the sum over a workgroup of 256 threads, for all of them
+__device__ __forceinline__ double block_sum(double s, double* four)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) four[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return (four[0] + four[1]) + (four[2] + four[3]);
+}
+
+__global__ __launch_bounds__(256) void square_sum_kernel(const ClipParams p)
+{
+    __shared__ double four[4];
+    double sum[2] = {0.0, 0.0};
+    for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
+        const Piece z = piece_of(p, c);
+        const void* x = p.e[z.e].x;
+        const bool bf16 = p.e[z.e].types & 1;
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = (i * 256 + threadIdx.x) * 8;
+            eight(x, bf16, z.from + k, z.left - k, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { const double d = (double)v[i][j]; sum[j & 1] = __builtin_fma(d, d, sum[j & 1]); }
+    }
+    const double s = block_sum(sum[0] + sum[1], four);
+    if (threadIdx.x == 0) p.part[p.first + blockIdx.x] = s;
+}
+
+__device__ __forceinline__ double all_parts(const ClipParams& p, double* four)
+{
+    double s = 0.0;
+    for (int i = threadIdx.x; i < p.parts; i += 256) s += p.part[i];
+    return sqrt(block_sum(s, four));
+}
+__global__ __launch_bounds__(256) void norm_of_parts_kernel(const ClipParams p)
+{
+    __shared__ double four[4];
+    const double norm = all_parts(p, four);
+    if (threadIdx.x == 0) *p.norm = (float)norm;
+}
+__global__ __launch_bounds__(256) void clip_kernel(const ClipParams p)
+{
+    __shared__ double four[4];
+    const double norm = all_parts(p, four);
+    if (p.first == 0 && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
+    const float factor = norm <= p.most ? 1.0f : (float)(p.most / norm);        // (NaN where the norm is)
+    for (int c = p.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+        const Piece z = piece_of(p, c);
+        const ClipEntry& e = p.e[z.e];
+        if (e.x == e.out && factor == 1.0f) continue;                           // (in place, and nothing to do)
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = (i * 256 + threadIdx.x) * 8;
+            eight(e.x, e.types & 1, z.from + k, z.left - k, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = (i * 256 + threadIdx.x) * 8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] *= factor;
+            put_eight(e.out, e.types & 2, z.from + k, z.left - k, v[i]);
+        }
+    }
+}
+
+}  // namespace sopk
+
+extern "C" hipError_t sopk_square_sum_launch(const ClipParams* p, int words, void* stream)
+{
+    hipLaunchKernelGGL(sopk::square_sum_kernel, dim3((unsigned)words), dim3(256), 0, (hipStream_t)stream, *p);
+    return hipGetLastError();
+}
+extern "C" hipError_t sopk_norm_of_parts_launch(const ClipParams* p, void* stream)
+{
+    hipLaunchKernelGGL(sopk::norm_of_parts_kernel, dim3(1), dim3(256), 0, (hipStream_t)stream, *p);
+    return hipGetLastError();
+}
+extern "C" hipError_t sopk_clip_launch(const ClipParams* p, int words, void* stream)
+{
+    hipLaunchKernelGGL(sopk::clip_kernel, dim3((unsigned)words), dim3(256), 0, (hipStream_t)stream, *p);
+    return hipGetLastError();
+}

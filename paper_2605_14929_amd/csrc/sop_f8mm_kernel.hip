@@ -14,6 +14,7 @@
 
 #include <type_traits>
 
+#include "sop_epilogue.h"
 #include "sop_linear.h"
 #include "sop_linear_rules.h"
 
@@ -106,6 +107,13 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
     }
 }
 
+// ... as they are, or through the epilogue (BF16: the type of y)
+template <bool EPI, bool BF16> __device__ __forceinline__ void leave(const F8MmParams& p, int m, int n, v4f v)
+{
+    if constexpr (EPI) finish_four<BF16>(p, m, n, v, epilogue_operands<BF16>(p, m, n));
+    else store_y(p, m, n, v);
+}
+
 // The last step of a K that is no multiple of 128: a row is read up to a multiple of 16, and what lies beyond K becomes zeros in LDS, `rows` rows
 // that thread `me` of `n` shares.
 __device__ __forceinline__ void clear_beyond(unsigned char* tile, int rows, int left, int me, int n)
@@ -127,7 +135,7 @@ __device__ __forceinline__ void clear_beyond(unsigned char* tile, int rows, int 
 // spare, a step takes 1.65 us: its loads alone 1.1 (64 KB a compute unit, with two steps in flight or one), its operands' reads and matrix instructions alone
 // 1.5, of which the instructions are 0.95.  Operands read two matrix instructions ahead, half of the workgroup a half-step behind the other, four
 // wavefronts of 128 x 128, and lines asked for into L2 ahead of the loads all took as long or longer.
-template <int BM, int BN, int WR, int WC, int XF, bool EXACT>
+template <int BM, int BN, int WR, int WC, int XF, bool EXACT, bool EPI>
 __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
     constexpr int NT = WR * WC * 64, FM = BM / WR / 32, FN = BN / WC / 32, CX = BM * 8 / NT, CW = BN * 8 / NT;
@@ -268,21 +276,33 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
         }
     }
     __syncthreads();                                                    // (LDS is free for the results)
-    v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
+    if constexpr (EPI) {
+        // as many of the wavefront's squares at once as find room, so that the epilogue's code stands there once or twice, in a loop over quarters of them
+        constexpr int SQUARES = FM * FN, ROOM = 2 * STAGE / (WR * WC) / 4096, PART = ROOM < SQUARES ? ROOM : SQUARES;
+        v4f* place = reinterpret_cast<v4f*>(lds + wave * (PART * 4096));
 #pragma unroll
-    for (int a = 0; a < FM; ++a)
+        for (int first = 0; first < SQUARES; first += PART) {
 #pragma unroll
-        for (int b = 0; b < FN; ++b) {
-            put_square(place, lane, acc[a][b]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) store_y(p, m0 + wm + a * 32 + 8 * i + (lane >> 3), n0 + wn + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+            for (int s = first; s < first + PART && s < SQUARES; ++s) put_square(place + (s - first) * 256, lane, acc[s / FN][s % FN]);
+            finish_squares<!EXACT, FN>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
         }
+    } else {
+        v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
+#pragma unroll
+        for (int a = 0; a < FM; ++a)
+#pragma unroll
+            for (int b = 0; b < FN; ++b) {
+                put_square(place, lane, acc[a][b]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) store_y(p, m0 + wm + a * 32 + 8 * i + (lane >> 3), n0 + wn + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+            }
+    }
 }
 
 // ---- few tiles: FM x 16 rows of x by FN x 16 columns a workgroup, K dealt out to its W wavefronts, U steps at a time.  Operands go from
 // memory to registers as the matrix instruction wants them; the wavefronts' sums meet in LDS in a fixed order.  One row through 28672 x 8192 whose
 // weights lie in HBM takes 39.1 us, 6.0 TB/s, bound by the read of w; through 4096 x 11008 a call takes 12.8 us so, 10.6 with the weights in the last-level cache.
-template <int FM, int FN, int U, int W, int XF, bool EXACT>
+template <int FM, int FN, int U, int W, int XF, bool EXACT, bool EPI>
 __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
     __shared__ v4f part[W][FM][FN][64];
@@ -375,7 +395,7 @@ __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, i
         v4f s = part[0][a][b][lane];
 #pragma unroll
         for (int i = 1; i < W; ++i) s += part[i][a][b][lane];
-        store_y(p, m0 + a * 16 + r16, n0 + b * 16 + 4 * q, s);
+        leave<EPI, !EXACT>(p, m0 + a * 16 + r16, n0 + b * 16 + 4 * q, s);
     }
 }
 
@@ -384,7 +404,7 @@ __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, i
 // (32 bytes of a row a lane) do not.  While a step is multiplied the wavefront's next one is on its way.  The wavefronts' sums meet in LDS in
 // a fixed order.  301 x 1531 x 5024 with fp32 results takes 12.5 us by it, 34 by tiles of 64 x 128: five steps a wavefront, each as long as its
 // loads take to come.
-template <int FM, int FN, int XF, bool EXACT>
+template <int FM, int FN, int XF, bool EXACT, bool EPI>
 __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int tiles_m, int tiles_n, int group)
 {
     constexpr int W = 8, ROWS = 32 * (FM + FN), OWN = ROWS * 128, LOADS = ROWS / 8;
@@ -487,14 +507,14 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
         v4f s = reinterpret_cast<const v4f*>(lds)[at];
 #pragma unroll
         for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[at];
-        store_y(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
+        leave<EPI, !EXACT>(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
     }
 }
 
-template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t tile_go(const F8MmParams& p, hipStream_t st)
+template <int BM, int BN, int WR, int WC, int XF, bool EXACT, bool EPI> static hipError_t tile_go(const F8MmParams& p, hipStream_t st)
 {
     const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128;
-    auto fn = &f8mm_tile_kernel<BM, BN, WR, WC, XF, EXACT>;
+    auto fn = &f8mm_tile_kernel<BM, BN, WR, WC, XF, EXACT, EPI>;
     if (bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
@@ -502,10 +522,10 @@ template <int BM, int BN, int WR, int WC, int XF, bool EXACT> static hipError_t 
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(WR * WC * 64), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int FM, int FN, int XF, bool EXACT> static hipError_t split_go(const F8MmParams& p, hipStream_t st)
+template <int FM, int FN, int XF, bool EXACT, bool EPI> static hipError_t split_go(const F8MmParams& p, hipStream_t st)
 {
     const int tm = (p.M + 32 * FM - 1) / (32 * FM), tn = (p.N + 32 * FN - 1) / (32 * FN), bytes = 8 * 32 * (FM + FN) * 128;
-    auto fn = &f8mm_split_kernel<FM, FN, XF, EXACT>;
+    auto fn = &f8mm_split_kernel<FM, FN, XF, EXACT, EPI>;
     if (bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
@@ -513,32 +533,41 @@ template <int FM, int FN, int XF, bool EXACT> static hipError_t split_go(const F
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(512), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int FM, int FN, int U, int W, int XF, bool EXACT> static hipError_t rows_go(const F8MmParams& p, hipStream_t st)
+template <int FM, int FN, int U, int W, int XF, bool EXACT, bool EPI> static hipError_t rows_go(const F8MmParams& p, hipStream_t st)
 {
     const int tm = (p.M + FM * 16 - 1) / (FM * 16), tn = (p.N + FN * 16 - 1) / (FN * 16);
-    hipLaunchKernelGGL((f8mm_rows_kernel<FM, FN, U, W, XF, EXACT>), dim3((unsigned)(tm * tn)), dim3(W * 64), 0, st, p, tm, tn, 8);
+    hipLaunchKernelGGL((f8mm_rows_kernel<FM, FN, U, W, XF, EXACT, EPI>), dim3((unsigned)(tm * tn)), dim3(W * 64), 0, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int XF, bool EXACT> static hipError_t go(const F8MmParams& p, int choice, hipStream_t st)
+template <int XF, bool EXACT, bool EPI> static hipError_t go(const F8MmParams& p, int choice, hipStream_t st)
 {
     switch (choice) {
-    case sopr::F8MM_ROWS: return rows_go<1, 1, 2, 8, XF, EXACT>(p, st);
-    case sopr::F8MM_32x32: return split_go<1, 1, XF, EXACT>(p, st);
-    case sopr::F8MM_32x64: return split_go<1, 2, XF, EXACT>(p, st);
-    case sopr::F8MM_64x64: return split_go<2, 2, XF, EXACT>(p, st);
-    case sopr::F8MM_64x128: return tile_go<64, 128, 2, 2, XF, EXACT>(p, st);
-    case sopr::F8MM_128x128: return tile_go<128, 128, 2, 2, XF, EXACT>(p, st);
+    case sopr::F8MM_ROWS: return rows_go<1, 1, 2, 8, XF, EXACT, EPI>(p, st);
+    case sopr::F8MM_32x32: return split_go<1, 1, XF, EXACT, EPI>(p, st);
+    case sopr::F8MM_32x64: return split_go<1, 2, XF, EXACT, EPI>(p, st);
+    case sopr::F8MM_64x64: return split_go<2, 2, XF, EXACT, EPI>(p, st);
+    case sopr::F8MM_64x128: return tile_go<64, 128, 2, 2, XF, EXACT, EPI>(p, st);
+    case sopr::F8MM_128x128: return tile_go<128, 128, 2, 2, XF, EXACT, EPI>(p, st);
     case sopr::F8MM_256x256:
-        if constexpr (!EXACT) return tile_go<256, 256, 2, 4, XF, EXACT>(p, st);
+        if constexpr (!EXACT) return tile_go<256, 256, 2, 4, XF, EXACT, EPI>(p, st);
     }
     return hipErrorInvalidValue;
 }
 
 }  // namespace sopk
 
+#ifdef SOPK_EPILOGUE
+extern "C" hipError_t sopk_f8mm_epilogue_launch(const F8MmParams* p, int x_e5m2, int choice, void* stream)
+#else
 extern "C" hipError_t sopk_f8mm_launch(const F8MmParams* p, int x_e5m2, int choice, void* stream)
+#endif
 {
+#ifdef SOPK_EPILOGUE
+    constexpr bool epi = true;
+#else
+    constexpr bool epi = false;
+#endif
     hipStream_t st = (hipStream_t)stream;
-    if (p->out_bf16) return x_e5m2 ? sopk::go<1, false>(*p, choice, st) : sopk::go<0, false>(*p, choice, st);
-    return x_e5m2 ? sopk::go<1, true>(*p, choice, st) : sopk::go<0, true>(*p, choice, st);
+    if (p->out_bf16) return x_e5m2 ? sopk::go<1, false, epi>(*p, choice, st) : sopk::go<0, false, epi>(*p, choice, st);
+    return x_e5m2 ? sopk::go<1, true, epi>(*p, choice, st) : sopk::go<0, true, epi>(*p, choice, st);
 }

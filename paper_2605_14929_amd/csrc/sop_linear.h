@@ -32,12 +32,21 @@ struct F8GatedGradParams {
     F8Out dg8, du8;
 };
 
+/* What becomes of a product's sums v: z = v + bias, y = residual + scale act(z) */
+struct Epilogue {
+    const float* bias;                       // null: none
+    const void* residual; long long ldr;     // of y's type, null: none
+    void* z; long long ldz;                  // of y's type, null: not kept
+    float scale; int act;
+};
+
 /* y[m, n] = sum over blocks b of 2^(xs[m, b] + ws[n / 128, b] - 254) sum_{k in b} x[m, k] w[n, k] */
 struct F8MmParams {
     const unsigned char* x; long long ldx; const unsigned char* xs; long long ldxs;
     const unsigned char* w; long long ldw; const unsigned char* ws; long long ws_n, ws_k;   // scale of block (n / 128, k / 128) at n * ws_n + k * ws_k
     int M, N, K;
     void* y; long long ldy; int out_bf16;
+    Epilogue e;                              // looked at by the kernels with an epilogue alone
 };
 
 /* dw[n, k] = sum_m dy[m, n] x[m, k] 2^(xs[m, k / 128] - 127) (+ dw) */
@@ -58,6 +67,7 @@ struct PackedMmParams {
     int sign_up, sel_pos, sel_mask;          // word << sign_up has the sign in bit 31 (0: none); selector = word >> sel_pos & sel_mask
     uint16_t* y; long long ldy;              // bf16
     float tab[2][SOP_K_PACKED_TAB];
+    Epilogue e;                              // looked at by the kernels with an epilogue alone
 };
 
 #if defined(__HIPCC__)

@@ -1,94 +1,60 @@
 // Entry points of the products of a linear layer with narrow operands: every argument is checked here, before a launch; the kernels'
 // own bounds rest on what these checks let through.
-#include "../../include/sop.h"
-
-#include <hip/hip_runtime.h>
-
-#include <cstdio>
 #include <cstring>
 
-#include "sop_ctx.h"
-#include "sop_linear.h"
+#include "sop_checks.h"
 #include "sop_linear_rules.h"
 
 extern "C" hipError_t sopk_f8_quant_launch(const F8QuantParams* p, int bf16, int e5m2, int vec, int square, void* stream);
 extern "C" hipError_t sopk_f8_gated_launch(const F8GatedParams* p, int bf16, int e5m2, int vec, void* stream);
 extern "C" hipError_t sopk_f8_gated_grad_launch(const F8GatedGradParams* p, int bf16, int ckpt_e5m2, int e5m2, int vec, void* stream);
 extern "C" hipError_t sopk_f8mm_launch(const F8MmParams* p, int x_e5m2, int choice, void* stream);
+extern "C" hipError_t sopk_f8mm_epilogue_launch(const F8MmParams* p, int x_e5m2, int choice, void* stream);
 extern "C" hipError_t sopk_wgrad_launch(const WgradParams* p, int x_e5m2, int choice, void* stream);
 extern "C" hipError_t sopk_packed_launch(const PackedMmParams* p, int choice, void* stream);
+extern "C" hipError_t sopk_packed_epilogue_launch(const PackedMmParams* p, int choice, void* stream);
 
 namespace {
 
-constexpr int64_t kMaxDim = (int64_t)1 << 30, kMaxStride = (int64_t)1 << 23;
-
-struct OnDevice {
-    int prev = 0;
-    bool switched = false;
-    hipError_t err = hipSuccess;
-    explicit OnDevice(int dev) { (void)hipGetDevice(&prev); if (prev != dev) { err = hipSetDevice(dev); switched = err == hipSuccess; } }
-    ~OnDevice() { if (switched) (void)hipSetDevice(prev); }
-};
-
-bool off(const void* p, uintptr_t unit) { return (reinterpret_cast<uintptr_t>(p) & (unit - 1)) != 0; }
-bool dtype_ok(sop_dtype d) { return d == SOP_F32 || d == SOP_BF16; }
-int64_t size_of(sop_dtype d) { return d == SOP_F32 ? 4 : 2; }
-
-// a matrix of numbers: null if it is one
-const char* plain_fault(const void* p, int64_t cols, int64_t ld, int64_t size)
-{
-    if (!p) return "a matrix is NULL";
-    if (off(p, (uintptr_t)size)) return "a matrix is not aligned to its elements";
-    if (ld < cols) return "a row stride is smaller than the row";
-    return nullptr;
-}
-// a matrix in 8 bits: null if it is one
-const char* f8_fault(const sop_f8_matrix* q, int64_t cols, int64_t scale_cols, int block_rows)
-{
-    if (!q || !q->codes || !q->scales) return "an 8-bit matrix is NULL";
-    if (q->format != SOP_E4M3 && q->format != SOP_E5M2) return "an 8-bit matrix is of no known format";
-    if (q->block_rows != block_rows) return block_rows == 1 ? "activations and gradients have blocks of one row" : "weights have blocks of 128 rows";
-    if (off(q->codes, 16) || (q->ld_codes & 15) || off(q->scales, 4) || (q->ld_scales & 3)) return "codes are on 16 bytes with a row stride of a multiple of 16, scales on 4 with one of 4";
-    if (q->ld_codes < cols || q->ld_scales < scale_cols) return "a row stride is smaller than the row";
-    if (q->ld_codes > kMaxStride || q->ld_scales > kMaxStride) return "a row stride is larger than 2^23";
-    return nullptr;
-}
-sop_status bad(sop_ctx* c, const char* call, sop_status s, const char* why)
-{
-    char text[256];
-    std::snprintf(text, sizeof(text), "%s: %s", call, why);
-    return sopc::fail(c, s, text);
-}
-sop_status launched(sop_ctx* c, const char* call, hipError_t e)
-{
-    if (e == hipSuccess) return SOP_OK;
-    char text[256];
-    std::snprintf(text, sizeof(text), "%s: kernel launch: %s", call, hipGetErrorString(e));
-    return sopc::fail(c, SOP_EHIP, text);
-}
-bool dims_ok(int64_t M, int64_t N, int64_t K) { return M >= 0 && N >= 1 && K >= 1 && M <= kMaxDim && N <= kMaxDim && K <= kMaxDim; }
-const char* const kDims = "M >= 0 and N, K >= 1, at most 2^30 each";
-int64_t blocks(int64_t n) { return (n + 127) / 128; }
-F8Out out_of(const sop_f8_matrix* q) { return F8Out{q->codes, q->ld_codes, q->scales, q->ld_scales}; }
-F8In in_of(const sop_f8_matrix* q) { return F8In{q->codes, q->ld_codes, q->scales, q->ld_scales}; }
-bool rows16(const void* p, int64_t ld, int64_t size) { return !off(p, 16) && (ld * size) % 16 == 0; }
-
 // One launch, or, where none can be large enough (fewer than 64 elements along K, and some 2^35 numbers of y), halves of its longer side
-hipError_t packed_parts(const PackedMmParams& p, int n_cu, void* stream)
+hipError_t packed_parts(const PackedMmParams& p, bool epilogue, int n_cu, void* stream)
 {
     const int choice = sopr::packed_choice(p.M, p.N, p.K, p.n_bits, n_cu);
-    if (choice >= 0) return sopk_packed_launch(&p, choice, stream);
+    if (choice >= 0) return epilogue ? sopk_packed_epilogue_launch(&p, choice, stream) : sopk_packed_launch(&p, choice, stream);
     PackedMmParams a = p, b = p;
     if (p.M >= p.N) {
         a.M = p.M / 2; b.M = p.M - a.M;
         b.x += a.M * p.ldx; b.y += a.M * p.ldy;
+        if (p.e.residual) b.e.residual = static_cast<const uint16_t*>(p.e.residual) + a.M * p.e.ldr;
+        if (p.e.z) b.e.z = static_cast<uint16_t*>(p.e.z) + a.M * p.e.ldz;
     } else {
         a.N = p.N / 2; b.N = p.N - a.N;
         b.words += (int64_t)a.N * (p.K / p.g); b.payload += (int64_t)a.N * (p.K / 8) * p.n_bits; b.y += a.N;
+        if (p.e.bias) b.e.bias += a.N;
+        if (p.e.residual) b.e.residual = static_cast<const uint16_t*>(p.e.residual) + a.N;
+        if (p.e.z) b.e.z = static_cast<uint16_t*>(p.e.z) + a.N;
     }
-    const hipError_t e = packed_parts(a, n_cu, stream);
-    return e != hipSuccess ? e : packed_parts(b, n_cu, stream);
+    const hipError_t e = packed_parts(a, epilogue, n_cu, stream);
+    return e != hipSuccess ? e : packed_parts(b, epilogue, n_cu, stream);
 }
+
+// an epilogue of [M, N] results of `size` bytes: null if it is one
+const char* epilogue_fault(const sop_epilogue* e, int64_t N, int64_t size, const void* y, int64_t ldy)
+{
+    if (!e) return "the epilogue is NULL";
+    if (e->act < SOP_ACT_NONE || e->act > SOP_ACT_GELU_TANH) return "no known activation";
+    if (off(e->bias, 4)) return "the bias is not aligned to its elements";
+    if (e->residual) {
+        if (const char* why = plain_fault(e->residual, N, e->ldr, size)) return why;
+        if (e->residual == y && e->ldr != ldy) return "a residual that is y has its row stride";
+    }
+    if (e->z) {
+        if (const char* why = plain_fault(e->z, N, e->ldz, size)) return why;
+        if (e->z == y || e->z == e->residual) return "z has memory of its own";
+    }
+    return nullptr;
+}
+Epilogue epilogue_of(const sop_epilogue* e) { return Epilogue{e->bias, e->residual, e->ldr, e->z, e->ldz, e->scale, (int)e->act}; }
 
 }  // namespace
 
@@ -120,10 +86,9 @@ extern "C" sop_status sop_fp8_quantize(sop_ctx* c, const void* x, sop_dtype dtyp
     return launched(c, call, sopk_f8_quant_launch(&p, dtype == SOP_BF16, q->format == SOP_E5M2, rows16(x, ldx, size_of(dtype)), rows == 128, stream));
 }
 
-extern "C" sop_status sop_fp8_matmul(sop_ctx* c, const sop_f8_matrix* x, const sop_f8_matrix* w, int w_transposed, int64_t M, int64_t N, int64_t K,
-                                     void* y, sop_dtype dtype, int64_t ldy, void* stream)
+static sop_status fp8_product(const char* call, sop_ctx* c, const sop_f8_matrix* x, const sop_f8_matrix* w, int w_transposed, int64_t M, int64_t N, int64_t K,
+                              const sop_epilogue* e, bool epilogue, void* y, sop_dtype dtype, int64_t ldy, void* stream)
 {
-    const char* call = "sop_fp8_matmul";
     if (!c) return SOP_EINVAL;
     if (!dims_ok(M, N, K)) return bad(c, call, SOP_ESHAPE, kDims);
     if (!dtype_ok(dtype)) return bad(c, call, SOP_EINVAL, "y is fp32 or bf16");
@@ -132,6 +97,7 @@ extern "C" sop_status sop_fp8_matmul(sop_ctx* c, const sop_f8_matrix* x, const s
     if (M == 0) return SOP_OK;
     if (const char* why = f8_fault(x, K, blocks(K), 1)) return bad(c, call, SOP_EINVAL, why);
     if (const char* why = plain_fault(y, N, ldy, size_of(dtype))) return bad(c, call, SOP_EINVAL, why);
+    if (epilogue) if (const char* why = epilogue_fault(e, N, size_of(dtype), y, ldy)) return bad(c, call, SOP_EINVAL, why);
     F8MmParams p;
     std::memset(&p, 0, sizeof(p));
     p.x = x->codes; p.ldx = x->ld_codes; p.xs = x->scales; p.ldxs = x->ld_scales;
@@ -139,11 +105,24 @@ extern "C" sop_status sop_fp8_matmul(sop_ctx* c, const sop_f8_matrix* x, const s
     p.ws_n = w_transposed ? 1 : w->ld_scales; p.ws_k = w_transposed ? w->ld_scales : 1;
     p.M = (int)M; p.N = (int)N; p.K = (int)K;
     p.y = y; p.ldy = ldy; p.out_bf16 = dtype == SOP_BF16;
+    if (epilogue) p.e = epilogue_of(e);
     const int choice = sopr::f8mm_choice(M, N, dtype == SOP_F32, sopc::compute_units(c));
     if (choice < 0) return bad(c, call, SOP_ESHAPE, "y is too large for a launch");
     OnDevice on(sopc::device(c));
     if (on.err != hipSuccess) return launched(c, call, on.err);
-    return launched(c, call, sopk_f8mm_launch(&p, x->format == SOP_E5M2, choice, stream));
+    return launched(c, call, epilogue ? sopk_f8mm_epilogue_launch(&p, x->format == SOP_E5M2, choice, stream) : sopk_f8mm_launch(&p, x->format == SOP_E5M2, choice, stream));
+}
+
+extern "C" sop_status sop_fp8_matmul(sop_ctx* c, const sop_f8_matrix* x, const sop_f8_matrix* w, int w_transposed, int64_t M, int64_t N, int64_t K,
+                                     void* y, sop_dtype dtype, int64_t ldy, void* stream)
+{
+    return fp8_product("sop_fp8_matmul", c, x, w, w_transposed, M, N, K, nullptr, false, y, dtype, ldy, stream);
+}
+
+extern "C" sop_status sop_fp8_linear(sop_ctx* c, const sop_f8_matrix* x, const sop_f8_matrix* w, int w_transposed, int64_t M, int64_t N, int64_t K,
+                                     const sop_epilogue* e, void* y, sop_dtype dtype, int64_t ldy, void* stream)
+{
+    return fp8_product("sop_fp8_linear", c, x, w, w_transposed, M, N, K, e, true, y, dtype, ldy, stream);
 }
 
 extern "C" sop_status sop_fp8_weight_grad(sop_ctx* c, const void* dy, int64_t lddy, const sop_f8_matrix* x, int64_t M, int64_t N, int64_t K,
@@ -220,9 +199,9 @@ extern "C" sop_status sop_fp8_gated_grad(sop_ctx* c, const sop_f8_matrix* gate8,
     return launched(c, call, sopk_f8_gated_grad_launch(&p, dtype == SOP_BF16, gate8->format == SOP_E5M2, dgate8->format == SOP_E5M2, vec, stream));
 }
 
-extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, const sop_packed_weights* w, int64_t M, void* y, int64_t ldy, void* stream)
+static sop_status packed_product(const char* call, sop_ctx* c, const void* x, int64_t ldx, const sop_packed_weights* w, int64_t M, const sop_epilogue* e, bool epilogue,
+                                 void* y, int64_t ldy, void* stream)
 {
-    const char* call = "sop_packed_matmul";
     if (!c) return SOP_EINVAL;
     if (!w) return bad(c, call, SOP_EINVAL, "the weights are NULL");
     if (!dims_ok(M, w->N, w->K)) return bad(c, call, SOP_ESHAPE, kDims);
@@ -243,6 +222,7 @@ extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, 
     if (!rows16(x, ldx, 2)) return bad(c, call, SOP_EINVAL, "x is on 16 bytes, its row stride a multiple of 8 elements");
     if (w->K > kMaxStride / 2 || (ldx > kMaxStride / 2 && M > 1)) return bad(c, call, SOP_ESHAPE, "rows of x are at most 2^22 elements apart");
     if (const char* why = plain_fault(y, w->N, ldy, 2)) return bad(c, call, SOP_EINVAL, why);
+    if (epilogue) if (const char* why = epilogue_fault(e, w->N, 2, y, ldy)) return bad(c, call, SOP_EINVAL, why);
     PackedMmParams p;
     std::memset(&p, 0, sizeof(p));
     p.x = static_cast<const uint16_t*>(x); p.ldx = M > 1 ? ldx : w->K; p.words = w->words_dev; p.payload = w->payload_dev;
@@ -258,7 +238,18 @@ extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, 
         p.tab[0][i] = w->table_a[i < w->entries_a ? i : w->entries_a - 1];
         if (w->table_b) p.tab[1][i] = w->table_b[i < w->entries_b ? i : w->entries_b - 1];
     }
+    if (epilogue) p.e = epilogue_of(e);
     OnDevice on(sopc::device(c));
     if (on.err != hipSuccess) return launched(c, call, on.err);
-    return launched(c, call, packed_parts(p, sopc::compute_units(c), stream));
+    return launched(c, call, packed_parts(p, epilogue, sopc::compute_units(c), stream));
+}
+
+extern "C" sop_status sop_packed_matmul(sop_ctx* c, const void* x, int64_t ldx, const sop_packed_weights* w, int64_t M, void* y, int64_t ldy, void* stream)
+{
+    return packed_product("sop_packed_matmul", c, x, ldx, w, M, nullptr, false, y, ldy, stream);
+}
+
+extern "C" sop_status sop_packed_linear(sop_ctx* c, const void* x, int64_t ldx, const sop_packed_weights* w, int64_t M, const sop_epilogue* e, void* y, int64_t ldy, void* stream)
+{
+    return packed_product("sop_packed_linear", c, x, ldx, w, M, e, true, y, ldy, stream);
 }

@@ -1,0 +1,657 @@
+// Norms before and after a block with its gate and residual scale, forward and backward.  With rows m and columns k:
+//   x = y s1, s1 = 1 / sqrt(mean_k y^2 + eps)  (no norm after the block: x = y)      s = r + f x, f = scale gate after
+//   h = s s2, s2 = 1 / sqrt(mean_k s^2 + eps)                                        n = before h, as numbers, in 8 bits, or both
+// and backward, s being the stored sum, p = before dn:
+//   dr = ds + s2 (p - h mean_k(p h))             dbefore = sum_m dn h
+//   dy = s1 (q - x mean_k(q x)), q = f dr        t = sum_m dr x over the rows of a gate: dgate = scale after t, dafter = sum scale gate t
+//   (no norm after the block: dy = q)
+//
+// Every pass is bound by HBM.  A row stays in the registers of the threads that share it (T threads, C times eight neighbouring elements each), so that it is
+// read once; its sums go over a wavefront by rotations and over a workgroup through LDS.  Threads keep their columns from row to row, so weights, and the
+// backward pass's sums over rows, stay in registers too: a workgroup leaves one row of partial sums, and a second kernel adds those up in a fixed order.
+// Longer rows (more than 16384 elements, backward 8192) are read several times over instead.
+//
+// Sums of squares are binary32; where one leaves its range (elements beyond 2^63 or so) the row's are formed once more from elements 2^-70 as large.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "sop_block.h"
+#include "sop_block_rules.h"
+#include "sop_rows.h"
+
+namespace sopk {
+
+// The sum over a wavefront, for all lanes
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));   // row_ror:8, 4, 2, 1: sums of sixteen
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xF, 0xF, false));
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xF, 0xF, false));
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xF, 0xF, false));
+    const int b = __float_as_int(x);
+    return (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
+           (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
+}
+// Sums over the T threads of a row.  Two places in LDS by turns: whoever writes one has passed the barrier behind the other's reads.
+template <int T> struct RowSums {
+    static constexpr int W = T / 64;
+    float (*slot)[16][4];                                               // [2][wavefronts][sums]
+    int turn = 0;
+    template <int N> __device__ __forceinline__ void operator()(float (&v)[N])
+    {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = wave_sum(v[j]);
+        if constexpr (W > 1) {
+            const int wave = threadIdx.x >> 6;
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) slot[turn][wave][j] = v[j];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float s = slot[turn][0][j];
+#pragma unroll
+                for (int w = 1; w < W; ++w) s += slot[turn][w][j];
+                v[j] = s;
+            }
+            turn ^= 1;
+        }
+    }
+};
+// 1 / sqrt(mean + eps) of a row whose sum of squares is `sum`; where that is beyond SOPK_MUCH, what `again` says: the sum of squares of elements times FEWER
+#define SOPK_MUCH 1e37f
+#define SOPK_FEWER 8.470329473e-22f                                     // 2^-70
+__device__ __forceinline__ bool too_much(float sum) { return !(sum <= SOPK_MUCH); }
+__device__ __forceinline__ float unit_of(float sum, float inv_d, float eps) { return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_d, eps)); }
+__device__ __forceinline__ float unit_of_fewer(float sum, float inv_d) { return __builtin_amdgcn_rsqf(sum * inv_d) * SOPK_FEWER; }
+
+// ---- forward, a row in registers
+template <int T, int C, bool YB, bool RB>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormParams p, long long each)
+{
+    constexpr int RW = T < 256 ? 256 / T : 1;
+    __shared__ float slot[2][16][4];
+    RowSums<T> sums{slot};
+    const int t = threadIdx.x & (T - 1), who = RW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / T) : 0;
+    const float inv_d = 1.0f / (float)p.D;
+    int k[C], left[C];
+    float f[C][8], b[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        k[c] = (c * T + t) * 8;
+        left[c] = p.D - k[c];
+        vector8(p.before, k[c], left[c], 0.0f, b[c]);
+    }
+    const long long m0 = ((long long)blockIdx.x * RW + who) * each, m1 = m0 + each < p.M ? m0 + each : p.M;
+    if (m0 >= m1) return;                                               // (wavefronts of a row each meet nowhere; a workgroup of one row leaves together)
+    long long g = m0 / p.per_group, turn = m0;
+    for (long long m = m0; m < m1; ++m) {
+        if (p.y && m == turn) {                                         // the rows of a gate's row begin here
+            if (m != m0) ++g;
+            turn = (g + 1) * p.per_group;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float after[8];
+                gate8(p.gate, p.ldg, p.gate_bf16, g, k[c], left[c], f[c]);
+                vector8(p.after, k[c], left[c], 1.0f, after);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[c][i] = p.scale * f[c][i] * after[i];
+            }
+        }
+        const char* row = reinterpret_cast<const char*>(p.r) + m * p.ldr * (RB ? 2 : 4);
+        const char* rowy = reinterpret_cast<const char*>(p.y) + m * p.ldy * (YB ? 2 : 4);
+        Raw<RB> r[C];
+        Raw<YB> y[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            r[c] = ask<RB>(row, k[c], left[c]);
+            y[c] = p.y ? ask<YB>(rowy, k[c], left[c]) : nothing<YB>();
+        }
+        float s[C][8];
+        if (p.y) {
+            float s1 = 1.0f;
+            if (p.after) {
+                float sum[1] = {0.0f};
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(at(y[c], i), at(y[c], i), sum[0]);
+                sums(sum);
+                s1 = unit_of(sum[0], inv_d, p.eps);
+                if (too_much(sum[0])) {
+                    sum[0] = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) { const float z = at(y[c], i) * SOPK_FEWER; sum[0] = __builtin_fmaf(z, z, sum[0]); }
+                    sums(sum);
+                    s1 = unit_of_fewer(sum[0], inv_d);
+                }
+            }
+            char* out = reinterpret_cast<char*>(p.out) + m * p.ldo * (RB ? 2 : 4);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[c][i] = __builtin_fmaf(at(y[c], i) * s1, f[c][i], at(r[c], i));
+                put<RB>(out, k[c], left[c], s[c]);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[c][i] = at(r[c], i);
+        }
+        if (!p.before) continue;
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(s[c][i], s[c][i], sum[0]);   // (zero beyond the row's end)
+        sums(sum);
+        float s2 = unit_of(sum[0], inv_d, p.eps);
+        if (too_much(sum[0])) {
+            sum[0] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { const float z = s[c][i] * SOPK_FEWER; sum[0] = __builtin_fmaf(z, z, sum[0]); }
+            sums(sum);
+            s2 = unit_of_fewer(sum[0], inv_d);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[c][i] = s[c][i] * s2 * b[c][i];
+            if (p.n) put_numbers(p.n, m, p.ldn, p.n_bf16, k[c], left[c], s[c]);
+            if (p.q.codes) put_codes(p.q, p.e5m2, s[c], m, k[c], left[c]);
+        }
+    }
+}
+
+// ---- forward, rows of any length: three walks over a row (the last writes, so the sum may go where r was)
+template <bool YB, bool RB>
+__global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
+{
+    __shared__ float slot[2][16][4];
+    RowSums<1024> sums{slot};
+    const float inv_d = 1.0f / (float)p.D;
+    const int whole = (p.D + 8191) / 8192 * 8192;                       // (all lanes of sixteen take part in a block's maximum)
+    for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
+        const long long g = m / p.per_group;
+        const char* row = reinterpret_cast<const char*>(p.r) + m * p.ldr * (RB ? 2 : 4);
+        const char* rowy = reinterpret_cast<const char*>(p.y) + m * p.ldy * (YB ? 2 : 4);
+        float s1 = 1.0f, s2 = 0.0f;
+        auto total = [&](int k, float (&s)[8]) {
+            const int left = p.D - k;
+            const Raw<RB> r = ask<RB>(row, k, left);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = at(r, i);
+            if (!p.y) return;
+            const Raw<YB> y = ask<YB>(rowy, k, left);
+            float f[8], after[8];
+            gate8(p.gate, p.ldg, p.gate_bf16, g, k, left, f);
+            vector8(p.after, k, left, 1.0f, after);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = __builtin_fmaf(at(y, i) * s1, p.scale * f[i] * after[i], s[i]);
+        };
+        auto squares = [&](bool of_y, float by) {
+            float sum[1] = {0.0f};
+            for (int k = threadIdx.x * 8; k < p.D; k += 8192) {
+                float v[8];
+                if (of_y) {
+                    const Raw<YB> y = ask<YB>(rowy, k, p.D - k);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = at(y, i);
+                } else total(k, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { const float z = v[i] * by; sum[0] = __builtin_fmaf(z, z, sum[0]); }
+            }
+            sums(sum);
+            return sum[0];
+        };
+        auto unit = [&](bool of_y) {
+            const float sum = squares(of_y, 1.0f);
+            return too_much(sum) ? unit_of_fewer(squares(of_y, SOPK_FEWER), inv_d) : unit_of(sum, inv_d, p.eps);
+        };
+        if (p.y && p.after) s1 = unit(true);
+        if (p.before) s2 = unit(false);
+        for (int k = threadIdx.x * 8; k < whole; k += 8192) {
+            const int left = p.D - k;
+            float s[8], b[8];
+            total(k, s);
+            if (p.y) put<RB>(reinterpret_cast<char*>(p.out) + m * p.ldo * (RB ? 2 : 4), k, left, s);
+            if (!p.before) continue;
+            vector8(p.before, k, left, 0.0f, b);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = s[i] * s2 * b[i];
+            if (p.n) put_numbers(p.n, m, p.ldn, p.n_bf16, k, left, s);
+            if (p.q.codes) put_codes(p.q, p.e5m2, s, m, k, left);
+        }
+    }
+}
+
+// ---- backward.  The kernels' arguments once more, where few rows want them: read there, so that they hold no registers while rows go by.
+__device__ __forceinline__ const NormGradParams& seldom()
+{
+    unsigned long long at = (unsigned long long)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const NormGradParams*)(const __attribute__((address_space(4))) NormGradParams*)at;
+}
+// The groups and rows of a workgroup
+struct Share { long long g0, g1; int part, parts; };
+__device__ __forceinline__ Share share_of(const NormGradParams& p, long long w)
+{
+    if (p.parts > 1) return Share{w / p.parts, w / p.parts + 1, (int)(w % p.parts), p.parts};
+    return Share{w * p.groups / p.words, (w + 1) * p.groups / p.words, 0, 1};
+}
+__device__ __forceinline__ long long begin_of(const NormGradParams& p, long long g, int part) { return g * p.per_group + part * p.per_group / p.parts; }
+
+// What sums over rows a thread has when a group ends: t = sum of dr x
+template <int C> __device__ __forceinline__ void end_group(long long w, long long g, const int (&k)[C], const int (&left)[C], float (&t)[C][8], float (&da)[C][8])
+{
+    const NormGradParams& p = seldom();
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        float gate[8];
+        gate8(p.gate, p.ldg, p.gate_bf16, g, k[c], left[c], gate);
+        if (p.dgate && p.parts > 1) put<false>(p.part_t + w * p.D, k[c], left[c], t[c]);
+        else if (p.dgate) {
+            float after[8];
+            vector8(p.after, k[c], left[c], 1.0f, after);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) after[i] = p.scale * after[i] * t[c][i];
+            put_numbers(p.dgate, g, p.lddg, p.gate_bf16, k[c], left[c], after);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { da[c][i] = __builtin_fmaf(p.scale * gate[i], t[c][i], da[c][i]); t[c][i] = 0.0f; }
+    }
+}
+
+// ---- backward, a row in registers
+template <int T, int C, bool YB, bool RB>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_grad_kernel(const NormGradParams p)
+{
+    constexpr int RW = T < 256 ? 256 / T : 1;
+    __shared__ float slot[2][16][4];
+    __shared__ float joined[RW > 1 ? RW : 1][RW > 1 ? C * T * 8 : 1];
+    RowSums<T> sums{slot};
+    const int t = threadIdx.x & (T - 1), who = RW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / T) : 0;
+    const float inv_d = 1.0f / (float)p.D;
+    int k[C], left[C];
+    float f[C][8], b[C][8], st[C][8], sa[C][8], sb[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        k[c] = (c * T + t) * 8;
+        left[c] = p.D - k[c];
+        vector8(seldom().before, k[c], left[c], 0.0f, b[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) st[c][i] = sa[c][i] = sb[c][i] = 0.0f;
+    }
+    // the wavefronts of a workgroup that have a row each put their sums together: the first one has them all
+    auto join = [&](float (&v)[C][8]) {
+        if constexpr (RW > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) joined[who][(c * 8 + i) * T + t] = v[c][i];
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float s = joined[0][(c * 8 + i) * T + t];
+#pragma unroll
+                    for (int w = 1; w < RW; ++w) s += joined[w][(c * 8 + i) * T + t];
+                    v[c][i] = who == 0 ? s : 0.0f;
+                }
+        }
+    };
+    const Share z = share_of(seldom(), blockIdx.x);
+    for (long long g = z.g0; g < z.g1; ++g) {
+        if (p.y) {
+            const NormGradParams& p = seldom();
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float after[8];
+                gate8(p.gate, p.ldg, p.gate_bf16, g, k[c], left[c], f[c]);
+                vector8(p.after, k[c], left[c], 1.0f, after);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[c][i] = p.scale * f[c][i] * after[i];
+            }
+        }
+        const long long end = begin_of(seldom(), g, z.part + 1);
+        for (long long m = begin_of(seldom(), g, z.part) + who; m < end; m += RW) {
+            Raw<RB> rs[C], rd[C];
+            Raw<YB> rn[C], ry[C];
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                rs[c] = p.before ? ask<RB>(reinterpret_cast<const char*>(p.s) + m * p.lds * (RB ? 2 : 4), k[c], left[c]) : nothing<RB>();
+                rn[c] = p.before ? ask<YB>(reinterpret_cast<const char*>(p.dn) + m * p.lddn * (YB ? 2 : 4), k[c], left[c]) : nothing<YB>();
+                ry[c] = p.y ? ask<YB>(reinterpret_cast<const char*>(p.y) + m * p.ldy * (YB ? 2 : 4), k[c], left[c]) : nothing<YB>();
+                rd[c] = p.ds ? ask<RB>(reinterpret_cast<const char*>(p.ds) + m * p.ldds * (RB ? 2 : 4), k[c], left[c]) : nothing<RB>();
+            }
+            float sum[3] = {0.0f, 0.0f, 0.0f};                          // of s^2, p s and y^2
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float s = at(rs[c], i), y = at(ry[c], i);
+                    sum[0] = __builtin_fmaf(s, s, sum[0]);
+                    sum[1] = __builtin_fmaf(b[c][i] * at(rn[c], i), s, sum[1]);
+                    sum[2] = __builtin_fmaf(y, y, sum[2]);
+                }
+            sums(sum);
+            float s2 = unit_of(sum[0], inv_d, p.eps), s1 = p.after ? unit_of(sum[2], inv_d, p.eps) : 1.0f, mean = sum[1] * s2 * inv_d;
+            if (too_much(sum[0]) || too_much(fabsf(sum[1])) || (p.after && too_much(sum[2]))) {
+                float few[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float s = at(rs[c], i) * SOPK_FEWER, y = at(ry[c], i) * SOPK_FEWER;
+                        few[0] = __builtin_fmaf(s, s, few[0]);
+                        few[1] = __builtin_fmaf(y, y, few[1]);
+                    }
+                sums(few);
+                if (too_much(sum[0])) s2 = unit_of_fewer(few[0], inv_d);
+                if (p.after && too_much(sum[2])) s1 = unit_of_fewer(few[1], inv_d);
+                float ph[1] = {0.0f};
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ph[0] = __builtin_fmaf(b[c][i] * at(rn[c], i), at(rs[c], i) * s2, ph[0]);
+                sums(ph);
+                mean = ph[0] * inv_d;
+            }
+            float dr[C][8], qx[1] = {0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float h = at(rs[c], i) * s2, x = at(ry[c], i) * s1, dn = at(rn[c], i);
+                    dr[c][i] = __builtin_fmaf(s2, __builtin_fmaf(-h, mean, b[c][i] * dn), at(rd[c], i));
+                    sb[c][i] = __builtin_fmaf(dn, h, sb[c][i]);
+                    st[c][i] = __builtin_fmaf(dr[c][i], x, st[c][i]);
+                }
+                put<RB>(reinterpret_cast<char*>(p.dr) + m * p.lddr * (RB ? 2 : 4), k[c], left[c], dr[c]);
+            }
+            if (!p.y) continue;
+            if (p.after) {
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) qx[0] = __builtin_fmaf(f[c][i] * dr[c][i], at(ry[c], i) * s1, qx[0]);
+                sums(qx);
+            }
+            const float c1 = qx[0] * inv_d;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float q = f[c][i] * dr[c][i];
+                    dr[c][i] = p.after ? s1 * __builtin_fmaf(-at(ry[c], i) * s1, c1, q) : q;
+                }
+                put<YB>(reinterpret_cast<char*>(p.dy) + m * p.lddy * (YB ? 2 : 4), k[c], left[c], dr[c]);
+                if (p.q.codes) put_codes(p.q, p.e5m2, dr[c], m, k[c], left[c]);
+            }
+        }
+        const NormGradParams& r = seldom();
+        if (r.dafter || r.dgate) {
+            join(st);
+            if (who == 0) end_group<C>(blockIdx.x, g, k, left, st, sa);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) st[c][i] = 0.0f;
+        }
+    }
+    const NormGradParams& r = seldom();
+    if (r.dbefore) join(sb);
+    if (who != 0) return;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (r.dafter) put<false>(r.part_a + (long long)blockIdx.x * r.D, k[c], left[c], sa[c]);
+        if (r.dbefore) put<false>(r.part_b + (long long)blockIdx.x * r.D, k[c], left[c], sb[c]);
+    }
+}
+
+// ---- backward, rows of any length: first the rows (dr, dy, and what the sums need of a row), then strips of 512 columns
+template <bool YB, bool RB> struct LongRow {
+    const NormGradParams& p;
+    long long m, g;
+    __device__ __forceinline__ const char* row(const void* x, long long ld, bool bf16) const { return reinterpret_cast<const char*>(x) + m * ld * (bf16 ? 2 : 4); }
+    // s, p = before dn (or dn), y and f of eight columns; dr from them
+    __device__ __forceinline__ void read(int k, float (&s)[8], float (&dn)[8], float (&y)[8], float (&b)[8]) const
+    {
+        const int left = p.D - k;
+        const Raw<RB> rs = p.before ? ask<RB>(row(p.s, p.lds, RB), k, left) : nothing<RB>();
+        const Raw<YB> rn = p.before ? ask<YB>(row(p.dn, p.lddn, YB), k, left) : nothing<YB>(), ry = p.y ? ask<YB>(row(p.y, p.ldy, YB), k, left) : nothing<YB>();
+        vector8(p.before, k, left, 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { s[i] = at(rs, i); dn[i] = at(rn, i); y[i] = at(ry, i); }
+    }
+    __device__ __forceinline__ void sum_grad(int k, const float (&s)[8], const float (&dn)[8], const float (&b)[8], float s2, float mean, float (&dr)[8]) const
+    {
+        const Raw<RB> rd = p.ds ? ask<RB>(row(p.ds, p.ldds, RB), k, p.D - k) : nothing<RB>();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dr[i] = __builtin_fmaf(s2, __builtin_fmaf(-(s[i] * s2), mean, b[i] * dn[i]), at(rd, i));
+    }
+    __device__ __forceinline__ void factors(int k, float (&f)[8]) const
+    {
+        float after[8];
+        gate8(p.gate, p.ldg, p.gate_bf16, g, k, p.D - k, f);
+        vector8(p.after, k, p.D - k, 1.0f, after);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = p.scale * f[i] * after[i];
+    }
+};
+template <bool YB, bool RB>
+__global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradParams p)
+{
+    __shared__ float slot[2][16][4];
+    RowSums<1024> sums{slot};
+    const float inv_d = 1.0f / (float)p.D;
+    const int whole = (p.D + 8191) / 8192 * 8192;
+    for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
+        const LongRow<YB, RB> w{p, m, m / p.per_group};
+        float s[8], dn[8], y[8], b[8], dr[8], f[8];
+        auto squares = [&](float by) {
+            v2f r = {0.0f, 0.0f};
+            float sum[2] = {0.0f, 0.0f};
+            for (int k = threadIdx.x * 8; k < p.D; k += 8192) {
+                w.read(k, s, dn, y, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { const float u = s[i] * by, v = y[i] * by; sum[0] = __builtin_fmaf(u, u, sum[0]); sum[1] = __builtin_fmaf(v, v, sum[1]); }
+            }
+            sums(sum);
+            r[0] = sum[0]; r[1] = sum[1];
+            return r;
+        };
+        const v2f sq = squares(1.0f);
+        float s2 = unit_of(sq[0], inv_d, p.eps), s1 = p.after ? unit_of(sq[1], inv_d, p.eps) : 1.0f;
+        if (too_much(sq[0]) || (p.after && too_much(sq[1]))) {
+            const v2f few = squares(SOPK_FEWER);
+            if (too_much(sq[0])) s2 = unit_of_fewer(few[0], inv_d);
+            if (p.after && too_much(sq[1])) s1 = unit_of_fewer(few[1], inv_d);
+        }
+        float sum[1] = {0.0f};
+        if (p.before) {
+            for (int k = threadIdx.x * 8; k < p.D; k += 8192) {
+                w.read(k, s, dn, y, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(b[i] * dn[i], s[i] * s2, sum[0]);
+            }
+            sums(sum);
+        }
+        const float mean = sum[0] * inv_d;
+        sum[0] = 0.0f;
+        if (p.y && p.after) {
+            for (int k = threadIdx.x * 8; k < p.D; k += 8192) {
+                w.read(k, s, dn, y, b);
+                w.sum_grad(k, s, dn, b, s2, mean, dr);
+                w.factors(k, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(f[i] * dr[i], y[i] * s1, sum[0]);
+            }
+            sums(sum);
+        }
+        const float c1 = sum[0] * inv_d;
+        for (int k = threadIdx.x * 8; k < whole; k += 8192) {
+            const int left = p.D - k;
+            w.read(k, s, dn, y, b);
+            w.sum_grad(k, s, dn, b, s2, mean, dr);
+            put<RB>(reinterpret_cast<char*>(p.dr) + m * p.lddr * (RB ? 2 : 4), k, left, dr);
+            if (!p.y) continue;
+            w.factors(k, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q = f[i] * dr[i];
+                dr[i] = p.after ? s1 * __builtin_fmaf(-y[i] * s1, c1, q) : q;
+            }
+            put<YB>(reinterpret_cast<char*>(p.dy) + m * p.lddy * (YB ? 2 : 4), k, left, dr);
+            if (p.q.codes) put_codes(p.q, p.e5m2, dr, m, k, left);
+        }
+        if (threadIdx.x == 0) { p.stats[3 * m] = s1; p.stats[3 * m + 1] = s2; p.stats[3 * m + 2] = mean; }
+    }
+}
+template <bool YB, bool RB>
+__global__ __launch_bounds__(256) void norm_grad_columns_kernel(const NormGradParams p)
+{
+    __shared__ float joined[4][8 * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int k[1] = {((int)blockIdx.x * 64 + lane) * 8}, left[1] = {p.D - k[0]};
+    float st[1][8] = {}, sa[1][8] = {}, sb[1][8] = {};
+    auto join = [&](float (&v)[1][8]) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) joined[wave][i * 64 + lane] = v[0][i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[0][i] = (joined[0][i * 64 + lane] + joined[1][i * 64 + lane]) + (joined[2][i * 64 + lane] + joined[3][i * 64 + lane]);
+    };
+    const long long word = blockIdx.y;
+    const Share z = share_of(p, word);
+    for (long long g = z.g0; g < z.g1; ++g) {
+        const long long end = begin_of(p, g, z.part + 1);
+        for (long long m = begin_of(p, g, z.part) + wave; m < end; m += 4) {
+            const LongRow<YB, RB> w{p, m, g};
+            const float s1 = p.stats[3 * m], s2 = p.stats[3 * m + 1], mean = p.stats[3 * m + 2];
+            float s[8], dn[8], y[8], b[8], dr[8];
+            w.read(k[0], s, dn, y, b);
+            w.sum_grad(k[0], s, dn, b, s2, mean, dr);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sb[0][i] = __builtin_fmaf(dn[i], s[i] * s2, sb[0][i]);
+                st[0][i] = __builtin_fmaf(dr[i], y[i] * s1, st[0][i]);
+            }
+        }
+        if (p.dafter || p.dgate) {
+            join(st);
+            if (wave == 0) end_group<1>(word, g, k, left, st, sa);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) st[0][i] = 0.0f;
+        }
+    }
+    if (p.dbefore) join(sb);
+    if (wave != 0) return;
+    if (p.dafter) put<false>(p.part_a + word * p.D, k[0], left[0], sa[0]);
+    if (p.dbefore) put<false>(p.part_b + word * p.D, k[0], left[0], sb[0]);
+}
+
+// ---- the rows of partial sums added up, in binary64, in a fixed order: 32 columns a workgroup, its 32 half-wavefronts share the rows
+__global__ __launch_bounds__(1024) void join_kernel(const JoinParams p)
+{
+    __shared__ double part[32][33];
+    const int col = threadIdx.x & 31, row = threadIdx.x >> 5, d = blockIdx.x * 32 + col;
+    long long set = blockIdx.y;
+    int j = 0;
+    while (j < 2 && set >= p.sets[j]) { set -= p.sets[j]; ++j; }
+    const long long rows = p.rows[j];
+    const float* from = p.part[j] + set * rows * p.D + d;
+    double s = 0.0;
+    if (d < p.D) {
+        long long i = row;
+        for (; i + 96 < rows; i += 128) {
+            const float a = from[i * p.D], b = from[(i + 32) * p.D], c = from[(i + 64) * p.D], e = from[(i + 96) * p.D];
+            s += ((double)a + (double)b) + ((double)c + (double)e);
+        }
+        for (; i < rows; i += 32) s += (double)from[i * p.D];
+    }
+    part[row][col] = s;
+    __syncthreads();
+    if (row != 0 || d >= p.D) return;
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += part[i][col];
+    if (j == 2) s *= (double)p.factor * (p.after ? (double)p.after[d] : 1.0);
+    if (p.out_bf16[j]) reinterpret_cast<uint16_t*>(p.out[j])[set * p.ldo[j] + d] = (uint16_t)bf16_bits((float)s);
+    else reinterpret_cast<float*>(p.out[j])[set * p.ldo[j] + d] = (float)s;
+}
+
+template <int T, int C, bool YB, bool RB> static hipError_t norm_go(const NormParams& p, int n_cu, hipStream_t st)
+{
+    constexpr int RW = T < 256 ? 256 / T : 1, NT = T < 256 ? 256 : T;
+    const long long most = (long long)n_cu * 2048 / NT * RW, each = (p.M + most - 1) / most, units = (p.M + each - 1) / each;
+    hipLaunchKernelGGL((norm_kernel<T, C, YB, RB>), dim3((unsigned)((units + RW - 1) / RW)), dim3(NT), 0, st, p, each);
+    return hipGetLastError();
+}
+template <int T, int C, bool YB, bool RB> static hipError_t norm_grad_go(const NormGradParams& p, hipStream_t st)
+{
+    hipLaunchKernelGGL((norm_grad_kernel<T, C, YB, RB>), dim3((unsigned)p.words), dim3(T < 256 ? 256 : T), 0, st, p);
+    return hipGetLastError();
+}
+static long long grid_of(long long n, long long most) { return n < most ? n : most; }
+
+template <bool YB, bool RB> static hipError_t norm_shape_go(const NormParams& p, int n_cu, hipStream_t st)
+{
+    const sopr::RowShape s = sopr::norm_shape(p.D);
+    switch (s.T * 16 + s.C) {
+    case 64 * 16 + 1: return norm_go<64, 1, YB, RB>(p, n_cu, st);
+    case 64 * 16 + 2: return norm_go<64, 2, YB, RB>(p, n_cu, st);
+    case 256 * 16 + 1: return norm_go<256, 1, YB, RB>(p, n_cu, st);
+    case 256 * 16 + 2: return norm_go<256, 2, YB, RB>(p, n_cu, st);
+    case 512 * 16 + 2: return norm_go<512, 2, YB, RB>(p, n_cu, st);
+    case 512 * 16 + 3: return norm_go<512, 3, YB, RB>(p, n_cu, st);
+    case 512 * 16 + 4: return norm_go<512, 4, YB, RB>(p, n_cu, st);
+    }
+    hipLaunchKernelGGL((norm_long_kernel<YB, RB>), dim3((unsigned)grid_of(p.M, 2 * n_cu)), dim3(1024), 0, st, p);
+    return hipGetLastError();
+}
+template <bool YB, bool RB> static hipError_t norm_grad_shape_go(const NormGradParams& p, int n_cu, hipStream_t st)
+{
+    const sopr::RowShape s = sopr::norm_grad_shape(p.D);
+    switch (s.T * 16 + s.C) {
+    case 64 * 16 + 1: return norm_grad_go<64, 1, YB, RB>(p, st);
+    case 64 * 16 + 2: return norm_grad_go<64, 2, YB, RB>(p, st);
+    case 256 * 16 + 1: return norm_grad_go<256, 1, YB, RB>(p, st);
+    case 256 * 16 + 2: return norm_grad_go<256, 2, YB, RB>(p, st);
+    case 512 * 16 + 2: return norm_grad_go<512, 2, YB, RB>(p, st);
+    }
+    hipLaunchKernelGGL((norm_grad_long_kernel<YB, RB>), dim3((unsigned)grid_of(p.M, 2 * n_cu)), dim3(1024), 0, st, p);
+    if (p.dafter || p.dbefore || p.dgate) hipLaunchKernelGGL((norm_grad_columns_kernel<YB, RB>), dim3((unsigned)((p.D + 511) / 512), (unsigned)p.words), dim3(256), 0, st, p);
+    return hipGetLastError();
+}
+
+}  // namespace sopk
+
+extern "C" hipError_t sopk_norm_launch(const NormParams* p, int y_bf16, int r_bf16, int n_cu, void* stream)
+{
+    hipStream_t st = (hipStream_t)stream;
+    if (y_bf16) return r_bf16 ? sopk::norm_shape_go<true, true>(*p, n_cu, st) : sopk::norm_shape_go<true, false>(*p, n_cu, st);
+    return r_bf16 ? sopk::norm_shape_go<false, true>(*p, n_cu, st) : sopk::norm_shape_go<false, false>(*p, n_cu, st);
+}
+extern "C" hipError_t sopk_norm_grad_launch(const NormGradParams* p, int y_bf16, int r_bf16, int n_cu, void* stream)
+{
+    hipStream_t st = (hipStream_t)stream;
+    if (y_bf16) return r_bf16 ? sopk::norm_grad_shape_go<true, true>(*p, n_cu, st) : sopk::norm_grad_shape_go<true, false>(*p, n_cu, st);
+    return r_bf16 ? sopk::norm_grad_shape_go<false, true>(*p, n_cu, st) : sopk::norm_grad_shape_go<false, false>(*p, n_cu, st);
+}
+extern "C" hipError_t sopk_join_launch(const JoinParams* p, void* stream)
+{
+    const long long sets = p->sets[0] + p->sets[1] + p->sets[2];
+    hipLaunchKernelGGL(sopk::join_kernel, dim3((unsigned)((p->D + 31) / 32), (unsigned)sets), dim3(1024), 0, (hipStream_t)stream, *p);
+    return hipGetLastError();
+}

@@ -7,6 +7,7 @@
 
 #include <type_traits>
 
+#include "sop_epilogue.h"
 #include "sop_linear.h"
 #include "sop_linear_rules.h"
 
@@ -88,13 +89,20 @@ __device__ __forceinline__ void store_y(const PackedMmParams& p, int m, int n, v
     }
 }
 
+// ... as they are, or through the epilogue
+template <bool EPI> __device__ __forceinline__ void leave(const PackedMmParams& p, int m, int n, v4f v)
+{
+    if constexpr (EPI) finish_four<true>(p, m, n, v, epilogue_operands<true>(p, m, n));
+    else store_y(p, m, n, v);
+}
+
 // ---- few rows of x: FM x 16 of them by 16 columns a workgroup, K dealt out to its W wavefronts, 128 elements a step, U steps of a
 // wavefront in flight: a lane takes 32 neighbouring codes of its row, eight for each of four matrix instructions, and the same elements of x.
 // One row through 4096 x 11008 (28 MB of codes and scale words) takes 10.6 us, 11.6 where they lie in HBM, through 28672 x 8192 (147 MB) 41 and 44; sixteen
 // rows 17.4.  More steps in flight or more wavefronts take as long; nothing is busy most of the time (vector ALUs 31 % of the cycles, LDS 13 %), and what
 // would shorten a wavefront's way from a code to its weight - codes looked up in pairs, as below - has not been built here.
 // WPL: scale words of 32 codes (4, 2 or 1 for g = 8, 16 and more).
-template <int NB, int FM, int U, int W, int WPL>
+template <int NB, int FM, int U, int W, int WPL, bool EPI>
 __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParams p)
 {
     __shared__ __align__(16) float tab[2 << NB];
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
         v4f s = part[0][a][lane];
 #pragma unroll
         for (int i = 1; i < W; ++i) s += part[i][a][lane];
-        store_y(p, a * 16 + r16, n0 + 4 * q, s);
+        leave<EPI>(p, a * 16 + r16, n0 + 4 * q, s);
     }
 }
 
@@ -193,7 +201,7 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
 // instructions read: a lane takes 32 neighbouring codes of its row, eight for each of four instructions, and the same elements of x.  The next
 // step is asked for when this one's operands have been read.  128 x 4096 x 4096 of 4-bit codes takes 11.7 us (wide tiles of 128 x 128: 60), 32 x 11008
 // x 4096 16.1: forming the weights, code by code, once for 32 to 128 rows bounds it.
-template <int NB, int FM, int FN, int S, int WPL>
+template <int NB, int FM, int FN, int S, int WPL, bool EPI>
 __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
     constexpr int W = 8, OWN = (S > FN ? S : FN) * FM * 4096;
@@ -322,7 +330,7 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
         v4f s = reinterpret_cast<const v4f*>(lds)[at];
 #pragma unroll
         for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[at];
-        store_y(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
+        leave<EPI>(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
     }
 }
 
@@ -335,7 +343,7 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
 // next step is there, this one's place is free.  2048 x 11008 x 4096 of 4-bit codes takes 194 us, 950 TFLOP/s: matrix instructions are busy 41 % of the
 // cycles; the others go to the look-ups and products of the weights, formed anew by every row of tiles, and 44 % of the cycles in which LDS is at work to
 // bank conflicts of the pairs' look-ups.
-template <int NB, int E, int F, bool G8>
+template <int NB, int E, int F, bool G8, bool EPI>
 __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const PackedMmParams p, int tiles_m, int tiles_n, int group)
 {
     constexpr int BM = 64 * E, BN = 64 * F, SLOTS = E * F, EACH = 4 / E, XL = 2 * E, STAGE = (BM + BN) * 128, BOOK = 8 << 2 * NB, TAB = 2 * BOOK, CW = (NB + 1) / 2, WORDS = G8 ? 2 : 1;
@@ -568,72 +576,93 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
     }
     wait_loads();
     __syncthreads();                                                    // (LDS is free for the results)
-    v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
+    if constexpr (EPI) {
+        // as many of the wavefront's squares at once as find room, so that the epilogue's code stands there twice at most, in a loop over quarters of them
+        constexpr int SQUARES = E * F, ROOM = (TAB + 2 * STAGE) / 4 / 4096, PART = ROOM < SQUARES ? ROOM : SQUARES;
+        v4f* place = reinterpret_cast<v4f*>(lds + wave * (PART * 4096));
 #pragma unroll
-    for (int a = 0; a < E; ++a)
+        for (int first = 0; first < SQUARES; first += PART) {
 #pragma unroll
-        for (int b = 0; b < F; ++b) {
-            put_square(place, lane, acc[a][b]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) store_y(p, m0 + wm + a * 32 + 8 * i + (lane >> 3), n0 + wn + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+            for (int s = first; s < first + PART && s < SQUARES; ++s) put_square(place + (s - first) * 256, lane, acc[s / F][s % F]);
+            finish_squares<true, F>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
         }
+    } else {
+        v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
+#pragma unroll
+        for (int a = 0; a < E; ++a)
+#pragma unroll
+            for (int b = 0; b < F; ++b) {
+                put_square(place, lane, acc[a][b]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) store_y(p, m0 + wm + a * 32 + 8 * i + (lane >> 3), n0 + wn + b * 32 + 4 * (lane & 7), place[quarter_slot(i, lane)]);
+            }
+    }
 }
 
-template <int NB, int FM, int U, int W> static hipError_t rows_go(const PackedMmParams& p, hipStream_t st)
+template <int NB, int FM, int U, int W, bool EPI> static hipError_t rows_go(const PackedMmParams& p, hipStream_t st)
 {
-    auto fn = p.g == 8 ? &packed_rows_kernel<NB, FM, U, W, 4> : p.g == 16 ? &packed_rows_kernel<NB, FM, U, W, 2> : &packed_rows_kernel<NB, FM, U, W, 1>;
+    auto fn = p.g == 8 ? &packed_rows_kernel<NB, FM, U, W, 4, EPI> : p.g == 16 ? &packed_rows_kernel<NB, FM, U, W, 2, EPI> : &packed_rows_kernel<NB, FM, U, W, 1, EPI>;
     hipLaunchKernelGGL(fn, dim3((unsigned)((p.N + 15) / 16)), dim3(W * 64), 0, st, p);
     return hipGetLastError();
 }
-template <int NB, int FM, int FN, int S> static hipError_t split_go(const PackedMmParams& p, hipStream_t st)
+template <int NB, int FM, int FN, int S, bool EPI> static hipError_t split_go(const PackedMmParams& p, hipStream_t st)
 {
     const int tm = (p.M + 32 * FM - 1) / (32 * FM), tn = (p.N + 32 * FN - 1) / (32 * FN), bytes = 8 * (S > FN ? S : FN) * FM * 4096;
-    auto fn = p.g == 8 ? &packed_split_kernel<NB, FM, FN, S, 4> : p.g == 16 ? &packed_split_kernel<NB, FM, FN, S, 2> : &packed_split_kernel<NB, FM, FN, S, 1>;
+    auto fn = p.g == 8 ? &packed_split_kernel<NB, FM, FN, S, 4, EPI> : p.g == 16 ? &packed_split_kernel<NB, FM, FN, S, 2, EPI> : &packed_split_kernel<NB, FM, FN, S, 1, EPI>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(512), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int NB, int E, int F> static hipError_t wide_go(const PackedMmParams& p, hipStream_t st)
+template <int NB, int E, int F, bool EPI> static hipError_t wide_go(const PackedMmParams& p, hipStream_t st)
 {
     const int tm = (p.M + 64 * E - 1) / (64 * E), tn = (p.N + 64 * F - 1) / (64 * F), bytes = (16 << 2 * NB) + 2 * (64 * E + 64 * F) * 128;
     static_assert((16 << 2 * NB) + 2 * (64 * E + 64 * F) * 128 <= 160 * 1024, "the tables and two steps fit into LDS");
-    auto fn = p.g == 8 ? &packed_wide_kernel<NB, E, F, true> : &packed_wide_kernel<NB, E, F, false>;
+    auto fn = p.g == 8 ? &packed_wide_kernel<NB, E, F, true, EPI> : &packed_wide_kernel<NB, E, F, false, EPI>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(fn, dim3((unsigned)(tm * tn)), dim3(256), bytes, st, p, tm, tn, 8);
     return hipGetLastError();
 }
-template <int NB> static hipError_t go(const PackedMmParams& p, int choice, hipStream_t st)
+template <int NB, bool EPI> static hipError_t go(const PackedMmParams& p, int choice, hipStream_t st)
 {
     switch (choice) {
-    case sopr::PACKED_ROWS: return rows_go<NB, 1, 2, 8>(p, st);
-    case sopr::PACKED_32x32: return split_go<NB, 1, 1, 1>(p, st);
-    case sopr::PACKED_64x32: return split_go<NB, 2, 1, 1>(p, st);
-    case sopr::PACKED_64x64: return split_go<NB, 2, 2, 1>(p, st);
-    case sopr::PACKED_128x32: return split_go<NB, 4, 1, 1>(p, st);
-    case sopr::PACKED_128x128: return wide_go<NB, 2, 2>(p, st);
+    case sopr::PACKED_ROWS: return rows_go<NB, 1, 2, 8, EPI>(p, st);
+    case sopr::PACKED_32x32: return split_go<NB, 1, 1, 1, EPI>(p, st);
+    case sopr::PACKED_64x32: return split_go<NB, 2, 1, 1, EPI>(p, st);
+    case sopr::PACKED_64x64: return split_go<NB, 2, 2, 1, EPI>(p, st);
+    case sopr::PACKED_128x32: return split_go<NB, 4, 1, 1, EPI>(p, st);
+    case sopr::PACKED_128x128: return wide_go<NB, 2, 2, EPI>(p, st);
     case sopr::PACKED_256x192:
-        if constexpr (NB <= 5) return wide_go<NB, 4, 3>(p, st);
+        if constexpr (NB <= 5) return wide_go<NB, 4, 3, EPI>(p, st);
         break;
     case sopr::PACKED_256x256:
-        if constexpr (NB <= 5) return wide_go<NB, 4, 4>(p, st);
+        if constexpr (NB <= 5) return wide_go<NB, 4, 4, EPI>(p, st);
     }
     return hipErrorInvalidValue;
 }
 
 }  // namespace sopk
 
+#ifdef SOPK_EPILOGUE
+extern "C" hipError_t sopk_packed_epilogue_launch(const PackedMmParams* p, int choice, void* stream)
+#else
 extern "C" hipError_t sopk_packed_launch(const PackedMmParams* p, int choice, void* stream)
+#endif
 {
+#ifdef SOPK_EPILOGUE
+    constexpr bool epi = true;
+#else
+    constexpr bool epi = false;
+#endif
     hipStream_t st = (hipStream_t)stream;
     switch (p->n_bits) {
-    case 1: return sopk::go<1>(*p, choice, st);
-    case 2: return sopk::go<2>(*p, choice, st);
-    case 3: return sopk::go<3>(*p, choice, st);
-    case 4: return sopk::go<4>(*p, choice, st);
-    case 5: return sopk::go<5>(*p, choice, st);
-    case 6: return sopk::go<6>(*p, choice, st);
+    case 1: return sopk::go<1, epi>(*p, choice, st);
+    case 2: return sopk::go<2, epi>(*p, choice, st);
+    case 3: return sopk::go<3, epi>(*p, choice, st);
+    case 4: return sopk::go<4, epi>(*p, choice, st);
+    case 5: return sopk::go<5, epi>(*p, choice, st);
+    case 6: return sopk::go<6, epi>(*p, choice, st);
     }
     return hipErrorInvalidValue;
 }
