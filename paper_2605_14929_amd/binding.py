@@ -1058,8 +1058,10 @@ class Context:
         import torch
         n = C.c_size_t()
         _check(size(self._h, *sizes, C.byref(n)), self._h)
-        ws = torch.empty(max(n.value, 16), dtype=torch.uint8, device=like.device)
-        return ws.data_ptr(), ws.numel(), ws
+        if n.value == 0:
+            return None, 0, None
+        ws = torch.empty(n.value, dtype=torch.uint8, device=like.device)
+        return ws.data_ptr(), n.value, ws
 
     def fp8_linear_grad(self, dy, z=None, act=None, scale: float = 1.0, bias: bool = True, fmt=E5M2, stream=None):
         """sop_fp8_linear_grad: (dz, dz8, dbias) of the epilogue act / scale from dy [M, N] and the z that fp8_linear kept: numbers of dy's type (for fp8_weight_grad; dy

@@ -2,7 +2,7 @@
 //
 // One pass, bound by HBM.  A wavefront takes a strip of 512 columns, eight a lane, and goes down its share of the rows, so that the sums of a column stay in
 // registers; the four wavefronts of a workgroup take rows by turns and join their sums in LDS, and workgroups leave a row of partial sums each, which a
-// second kernel adds up in a fixed order (none where one workgroup has all rows).
+// second kernel adds up in a fixed order.  Few rows go without it: a workgroup takes 128 columns of all of them, 64 rows at a time.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -13,6 +13,42 @@
 
 namespace sopk {
 
+// eight numbers d = scale dy and z become dz
+template <bool BF16> __device__ __forceinline__ void slopes(int act, const Raw<BF16>& z, float (&d)[8])
+{
+    switch (act) {
+    case 1:
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(1, at(z, i), d[i]);
+        break;
+    case 2:
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(2, at(z, i), d[i]);
+        break;
+    case 3:
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(3, at(z, i), d[i]);
+        break;
+    case 4:
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(4, at(z, i), d[i]);
+    }
+}
+template <bool BF16> struct GradRow { Raw<BF16> d, z; };
+template <bool BF16> __device__ __forceinline__ GradRow<BF16> ask_row(const ActGradParams& p, long long m, int k, int left)
+{
+    return GradRow<BF16>{ask<BF16>(reinterpret_cast<const char*>(p.dy) + m * p.lddy * (BF16 ? 2 : 4), k, left),
+                         p.z ? ask<BF16>(reinterpret_cast<const char*>(p.z) + m * p.ldz * (BF16 ? 2 : 4), k, left) : nothing<BF16>()};
+}
+template <bool BF16, bool E5M2> __device__ __forceinline__ void finish_row(const ActGradParams& p, const GradRow<BF16>& r, long long m, int k, int left, float (&d)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = p.scale * at(r.d, i);
+    slopes<BF16>(p.act, r.z, d);
+    if (p.dz) put<BF16>(reinterpret_cast<char*>(p.dz) + m * p.lddz * (BF16 ? 2 : 4), k, left, d);
+    quantize_row_block<E5M2>(d, p.q, m, k, left);
+}
+
 template <bool BF16, bool E5M2, bool SUMS>
 __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradParams p)
 {
@@ -21,32 +57,9 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradParams p)
     const int strip = (int)(blockIdx.x % (unsigned)p.strips), k = strip * 512 + lane * 8, left = p.N - k;
     const long long word = blockIdx.x / (unsigned)p.strips, m0 = word * p.M / p.words, m1 = (word + 1) * p.M / p.words;
     float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    const F8Out q = p.q;
     for (long long m = m0 + wave; m < m1; m += 4) {
-        const Raw<BF16> rd = ask<BF16>(reinterpret_cast<const char*>(p.dy) + m * p.lddy * (BF16 ? 2 : 4), k, left);
-        const Raw<BF16> rz = p.z ? ask<BF16>(reinterpret_cast<const char*>(p.z) + m * p.ldz * (BF16 ? 2 : 4), k, left) : nothing<BF16>();
         float d[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = p.scale * at(rd, i);
-        switch (p.act) {
-        case 1:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = act_slope(1, at(rz, i), d[i]);
-            break;
-        case 2:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = act_slope(2, at(rz, i), d[i]);
-            break;
-        case 3:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = act_slope(3, at(rz, i), d[i]);
-            break;
-        case 4:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = act_slope(4, at(rz, i), d[i]);
-        }
-        if (p.dz) put<BF16>(reinterpret_cast<char*>(p.dz) + m * p.lddz * (BF16 ? 2 : 4), k, left, d);
-        quantize_row_block<E5M2>(d, q, m, k, left);
+        finish_row<BF16, E5M2>(p, ask_row<BF16>(p, m, k, left), m, k, left, d);
         if constexpr (SUMS) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += d[i];
@@ -59,8 +72,40 @@ __global__ __launch_bounds__(256) void act_grad_kernel(const ActGradParams p)
         if (wave != 0) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] = (joined[0][i * 64 + lane] + joined[1][i * 64 + lane]) + (joined[2][i * 64 + lane] + joined[3][i * 64 + lane]);
-        put<false>(p.part ? p.part + word * p.N : p.dbias, k, left, sum);
+        put<false>(p.part + word * p.N, k, left, sum);
     }
+}
+
+// Few rows, with their sums: sixteen lanes a row of a workgroup's 128 columns.
+template <bool BF16, bool E5M2>
+__global__ __launch_bounds__(1024) void act_grad_few_kernel(const ActGradParams p)
+{
+    __shared__ float joined[16][128];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, column = (lane & 15) * 8, k = (int)blockIdx.x * 128 + column, left = p.N - k;
+    float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    long long m = threadIdx.x >> 4;
+    GradRow<BF16> next = ask_row<BF16>(p, m < p.M ? m : p.M - 1, k, left);
+    for (; m < p.M; m += 64) {
+        const GradRow<BF16> row = next;
+        if (m + 64 < p.M) next = ask_row<BF16>(p, m + 64, k, left);
+        float d[8];
+        finish_row<BF16, E5M2>(p, row, m, k, left, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += d[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16);
+        sum[i] += __shfl_xor(sum[i], 32);
+        if (lane < 16) joined[wave][column + i] = sum[i];
+    }
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c >= 128 || (int)blockIdx.x * 128 + c >= p.N) return;
+    float s = joined[0][c];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += joined[w][c];
+    p.dbias[(int)blockIdx.x * 128 + c] = s;
 }
 
 }  // namespace sopk
@@ -69,10 +114,13 @@ extern "C" hipError_t sopk_act_grad_launch(const ActGradParams* pp, int bf16, in
 {
     const ActGradParams p = *pp;
     using T = std::true_type; using F = std::false_type;
+    auto few = [&](auto B, auto E) {
+        hipLaunchKernelGGL((sopk::act_grad_few_kernel<decltype(B)::value, decltype(E)::value>), dim3((unsigned)((p.N + 127) / 128)), dim3(1024), 0, (hipStream_t)stream, p);
+    };
     auto go = [&](auto B, auto E, auto S) {
         hipLaunchKernelGGL((sopk::act_grad_kernel<decltype(B)::value, decltype(E)::value, decltype(S)::value>), dim3((unsigned)(p.words * p.strips)), dim3(256), 0, (hipStream_t)stream, p);
     };
-    auto go2 = [&](auto B, auto E) { if (p.dbias) go(B, E, T{}); else go(B, E, F{}); };
+    auto go2 = [&](auto B, auto E) { if (!p.dbias) go(B, E, F{}); else if (p.part) go(B, E, T{}); else few(B, E); };
     auto go3 = [&](auto B) { if (e5m2) go2(B, T{}); else go2(B, F{}); };
     if (bf16) go3(T{}); else go3(F{});
     return hipGetLastError();

@@ -29,15 +29,17 @@ struct NormGradParams {
     void* dy; long long lddy;
     F8Out q; int e5m2;
     float* dafter; float* dbefore; void* dgate; long long lddg;   // null: not wanted
-    float* part_a; float* part_b; float* part_t;                  // a row of D for each workgroup
+    float* part_a; float* part_b; float* part_t;                  // a row of D for each workgroup: dafter's (parts = 1) or t (parts > 1), dbefore's
     float* stats;                                                 // rows read several times: 1 / rms(y), 1 / rms(s) and mean(p h) of each
     long long words; int parts;
 };
-/* out[d] = sum over rows i of part[i][d], rows `rows` apart from set to set */
+/* Rows of partial sums added up: out[j] of set s, column d = sum over `rows` rows i of part[j][s rows + i][d] (j = 0: times factor and gate[i / share][d], 2: times factor
+ * and after[d]) */
 struct JoinParams {
-    const float* part[3]; void* out[3]; long long rows[3];        // rows to add up for each of sets[j] outputs
+    const float* part[3]; void* out[3]; long long rows[3];
     long long sets[3]; long long ldo[3]; int out_bf16[3];
-    const float* after; float factor;                             // the third is multiplied by factor * after
+    const float* after; float factor;
+    const void* gate; long long ldg; int gate_bf16, share;             // gate null: weights of 1
     int D;
 };
 
@@ -49,7 +51,7 @@ struct ActGradParams {
     float scale; int act;
     void* dz; long long lddz;                // null: not written
     F8Out q;
-    float* part; float* dbias;               // null: no sums; part null: one workgroup has all rows of its columns
+    float* part; float* dbias;               // null: no sums; part null: a workgroup has all rows of its columns
     long long words; int strips;
 };
 

@@ -30,7 +30,7 @@ hipError_t join(JoinParams p, void* stream)
         while (p.sets[j] > most) {
             JoinParams q;
             std::memset(&q, 0, sizeof(q));
-            q.D = p.D; q.after = p.after; q.factor = p.factor;
+            q.D = p.D; q.after = p.after; q.factor = p.factor; q.gate = p.gate; q.ldg = p.ldg; q.gate_bf16 = p.gate_bf16; q.share = p.share;
             q.part[j] = p.part[j]; q.out[j] = p.out[j]; q.rows[j] = p.rows[j]; q.sets[j] = most; q.ldo[j] = p.ldo[j]; q.out_bf16[j] = p.out_bf16[j];
             const hipError_t e = sopk_join_launch(&q, stream);
             if (e != hipSuccess) return e;
@@ -60,7 +60,7 @@ const char* norm_fault(const sop_residual_norm_opts* o, int64_t M, int64_t D)
     return nullptr;
 }
 
-struct GradPlan { int64_t groups, each; sopr::RowShare share; size_t part_a, part_b, part_t, stats, bytes; };
+struct GradPlan { int64_t groups, each; sopr::RowShare share; size_t part_a, part_b, stats, bytes; };
 GradPlan plan_of(int64_t M, int64_t D, int64_t groups, int n_cu)
 {
     GradPlan g;
@@ -70,8 +70,7 @@ GradPlan plan_of(int64_t M, int64_t D, int64_t groups, int n_cu)
     const size_t row = (size_t)g.share.words * (size_t)D * 4;
     g.part_a = 0;
     g.part_b = row;
-    g.part_t = 2 * row;
-    g.stats = (g.share.parts > 1 ? 3 : 2) * row;
+    g.stats = 2 * row;
     g.bytes = g.stats + (sopr::norm_grad_shape(D).T == 0 ? (size_t)M * 12 : 0);
     return g;
 }
@@ -83,8 +82,7 @@ extern "C" sop_status sop_fp8_linear_grad_workspace(sop_ctx* c, int64_t M, int64
     if (!c) return SOP_EINVAL;
     if (!bytes) return bad(c, "sop_fp8_linear_grad_workspace", SOP_EINVAL, "bytes is NULL");
     if (!dims_ok(M, N, 1)) return bad(c, "sop_fp8_linear_grad_workspace", SOP_ESHAPE, kDims);
-    const int64_t words = sopr::act_grad_words(M, N, sopc::compute_units(c));
-    *bytes = words > 1 ? (size_t)words * (size_t)N * 4 : 0;
+    *bytes = sopr::act_grad_few(M) ? 0 : (size_t)sopr::act_grad_words(M, N, sopc::compute_units(c)) * (size_t)N * 4;
     return SOP_OK;
 }
 
@@ -112,7 +110,7 @@ extern "C" sop_status sop_fp8_linear_grad(sop_ctx* c, const void* dy, int64_t ld
     p.dz = dz; p.lddz = lddz; p.dbias = dbias;
     p.words = sopr::act_grad_words(M, N, sopc::compute_units(c));
     p.strips = (int)((N + 511) / 512);
-    if (dbias && M > 0 && p.words > 1) {
+    if (dbias && M > 0 && !sopr::act_grad_few(M)) {
         if (!workspace || off(workspace, 16) || workspace_bytes < (size_t)p.words * (size_t)N * 4) return bad(c, call, SOP_ENOMEM, "the workspace is NULL, not on 16 bytes, or too small");
         p.part = static_cast<float*>(workspace);
     }
@@ -125,7 +123,7 @@ extern "C" sop_status sop_fp8_linear_grad(sop_ctx* c, const void* dy, int64_t ld
     if (!dbias) return SOP_OK;
     JoinParams j;
     std::memset(&j, 0, sizeof(j));
-    j.D = (int)N;
+    j.D = (int)N; j.factor = 1.0f;
     one_sum(j, 0, p.part, M > 0 ? p.words : 0, 1, dbias, 0, false);
     return launched(c, call, join(j, stream));
 }
@@ -226,7 +224,7 @@ extern "C" sop_status sop_residual_norm_grad(sop_ctx* c, const sop_residual_norm
         p.dr = t->dr; p.lddr = t->ld_dr; p.dy = t->dy; p.lddy = t->ld_dy;
         if (t->dy8) { p.q = out_of(t->dy8); p.e5m2 = t->dy8->format == SOP_E5M2; }
         p.dafter = t->dafter; p.dbefore = t->dbefore; p.dgate = t->dgate; p.lddg = t->ld_dgate;
-        p.part_a = reinterpret_cast<float*>(at + g.part_a); p.part_b = reinterpret_cast<float*>(at + g.part_b); p.part_t = reinterpret_cast<float*>(at + g.part_t);
+        p.part_a = reinterpret_cast<float*>(at + g.part_a); p.part_b = reinterpret_cast<float*>(at + g.part_b); p.part_t = p.part_a;
         p.stats = reinterpret_cast<float*>(at + g.stats);
         p.words = g.share.words; p.parts = g.share.parts;
         const hipError_t e = sopk_norm_grad_launch(&p, (t->y || o->before ? t->y_dtype : t->r_dtype) == SOP_BF16, t->r_dtype == SOP_BF16, sopc::compute_units(c), stream);
@@ -234,11 +232,14 @@ extern "C" sop_status sop_residual_norm_grad(sop_ctx* c, const sop_residual_norm
     }
     JoinParams j;
     std::memset(&j, 0, sizeof(j));
-    j.D = (int)D; j.after = o->after; j.factor = o->scale;
+    j.D = (int)D; j.after = o->after;
     const int64_t words = M > 0 ? g.share.words : 0;
+    const bool shared = g.share.parts > 1;                              // (what the workgroups left is t: dafter = sum of scale gate t, dgate = scale after t)
     if (t->dafter) one_sum(j, 0, p.part_a, words, 1, t->dafter, 0, false);
     if (t->dbefore) one_sum(j, 1, p.part_b, words, 1, t->dbefore, 0, false);
-    if (t->dgate && (M == 0 || g.share.parts > 1)) one_sum(j, 2, p.part_t, M > 0 ? g.share.parts : 0, o->groups, t->dgate, t->ld_dgate, o->gate_dtype == SOP_BF16);
+    if (t->dgate && (M == 0 || shared)) one_sum(j, 2, p.part_t, M > 0 ? g.share.parts : 0, o->groups, t->dgate, t->ld_dgate, o->gate_dtype == SOP_BF16);
+    if (shared && o->gate) { j.gate = o->gate; j.ldg = o->ld_gate; j.gate_bf16 = o->gate_dtype == SOP_BF16; j.share = g.share.parts; }
+    j.factor = shared ? o->scale : 1.0f;                                // (whole groups: workgroups have put scale and gate on their sums)
     return launched(c, call, join(j, stream));
 }
 

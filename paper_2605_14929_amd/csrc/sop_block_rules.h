@@ -4,15 +4,20 @@
 
 namespace sopr {
 
-// A row of D elements by T threads, C times eight elements each, which keep it in registers; D beyond 16384 is read several times instead (T = 0).
+// A row of D elements by T threads, C times eight elements each, which keep it in registers (T = 64: a wavefront, four of them a workgroup); D beyond 16384 is
+// read several times instead (T = 0).
 struct RowShape { int T, C; };
+inline int threads_for(long long D, int C) { return (int)((D + 512 * C - 1) / (512 * C)) * 64; }
 inline RowShape norm_shape(long long D)
 {
-    return D <= 512 ? RowShape{64, 1} : D <= 1024 ? RowShape{64, 2} : D <= 2048 ? RowShape{256, 1} : D <= 4096 ? RowShape{256, 2} : D <= 8192 ? RowShape{512, 2}
-         : D <= 12288 ? RowShape{512, 3} : D <= 16384 ? RowShape{512, 4} : RowShape{0, 0};
+    const int C = D <= 512 ? 1 : D <= 1024 ? 2 : D <= 2048 ? 1 : D <= 8192 ? 2 : 4;
+    return D > 16384 ? RowShape{0, 0} : RowShape{threads_for(D, C), C};
 }
-// Backward, where a thread holds four times as much, from 8192 on.
-inline RowShape norm_grad_shape(long long D) { return D <= 8192 ? norm_shape(D) : RowShape{0, 0}; }
+// Backward, where a thread holds four times as much: eight elements up to 8192 (8192 x 4096 bf16 105 us, sixteen 108; 777 x 5024 fp32 32 and 34).
+inline RowShape norm_grad_shape(long long D)
+{
+    return D <= 1024 ? norm_shape(D) : D <= 8192 ? RowShape{threads_for(D, 1), 1} : RowShape{0, 0};
+}
 
 // Rows in G groups of `each` (a group shares a row of the gate), to `words` workgroups: as many groups as there are workgroups and more are dealt out whole
 // (parts = 1, workgroup i has groups i G / words ..), fewer are cut into `parts` each (workgroup i has part i % parts of group i / parts).
@@ -25,11 +30,14 @@ inline RowShare norm_share(long long G, long long each, long long most)
     return RowShare{G * parts, (int)parts};
 }
 
-// How many workgroups the backward pass has at most: what the compute units hold at once (each leaves a row of partial sums).
+// How many workgroups the backward pass has at most: about what the compute units hold at once (each leaves a row of partial sums).
 inline long long norm_grad_most(long long D, int n_cu)
 {
     const RowShape s = norm_grad_shape(D);
-    return (long long)n_cu * (s.T == 512 ? 1 : s.T == 0 || s.C == 2 ? 2 : 4);
+    if (s.T == 0) return 2ll * n_cu;
+    if (s.T == 64) return (s.C == 1 ? 4ll : 3ll) * n_cu;
+    const int each = 1024 / s.T;                                        // (sixteen wavefronts a compute unit)
+    return (long long)(each < 1 ? 1 : each) * n_cu;
 }
 
 // Rows of an activation's gradient to workgroups: strips of 512 columns times `words` shares of the rows, four rows each at least.
@@ -38,6 +46,9 @@ inline long long act_grad_words(long long M, long long N, int n_cu)
     const long long strips = (N + 511) / 512, all = 8ll * n_cu, words = all / strips, rows = (M + 3) / 4;
     return words < 1 ? 1 : words < rows ? words : rows < 1 ? 1 : rows;
 }
+// ... with their sums: whether one workgroup takes all rows of 128 columns, without a second launch.  In a graph 128 x 11008 takes 7.8 us so; from there on it is bound by the
+// vector ALUs of the few compute units at work (256 x 1531 14.9 us, by two launches 9).
+inline bool act_grad_few(long long M) { return M <= 128; }
 
 // Many tensors: launches of up to `list` of them, and the workgroups of each, which leave a partial sum each.
 inline long long clip_launches(long long count, int list) { return (count + list - 1) / list; }

@@ -55,11 +55,26 @@ template <bool BF16> __device__ __forceinline__ void put_columns(void* y, long l
         for (int i = 0; i < 3; ++i) if (i < left) to[i] = v[i];
     }
 }
-template <int ACT> __device__ __forceinline__ v4f act_four(v4f z)
+template <bool BF16, int ACT, int N> __device__ __forceinline__ void act_all(v4f (&z)[N])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) z[i] = act_of(ACT, z[i]);
-    return z;
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[j][i] = act_of<!BF16>(ACT, z[j][i]);
+}
+template <bool BF16, int N> __device__ __forceinline__ void act_by(int act, v4f (&z)[N])
+{
+    switch (act) {
+    case 1: act_all<BF16, 1>(z); break;
+    case 2: act_all<BF16, 2>(z); break;
+    case 3: act_all<BF16, 3>(z); break;
+    case 4: act_all<BF16, 4>(z);
+    }
+}
+// the residual of column i of four
+template <bool BF16> __device__ __forceinline__ float residual_of(const unsigned int* r, int i)
+{
+    return __uint_as_float(BF16 ? ((i & 1) ? r[i >> 1] & 0xFFFF0000u : r[i >> 1] << 16) : r[i]);
 }
 template <bool BF16, typename P> __device__ __forceinline__ void finish_four(const P& p, int m, int n, v4f v, const EpilogueOperands& o)
 {
@@ -68,23 +83,88 @@ template <bool BF16, typename P> __device__ __forceinline__ void finish_four(con
     const int left = p.N - n;
     v = v + o.bias;
     if (e.z) put_columns<BF16>(e.z, (long long)m * e.ldz + n, left, v);
-    switch (e.act) {
-    case 1: v = act_four<1>(v); break;
-    case 2: v = act_four<2>(v); break;
-    case 3: v = act_four<3>(v); break;
-    case 4: v = act_four<4>(v);
-    }
+    v4f z[1] = {v};
+    act_by<BF16>(e.act, z);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned int h = BF16 ? ((i & 1) ? o.r[i >> 1] & 0xFFFF0000u : o.r[i >> 1] << 16) : o.r[i];
-        v[i] = e.residual ? __builtin_fmaf(v[i], e.scale, __uint_as_float(h)) : v[i] * e.scale;
-    }
+    for (int i = 0; i < 4; ++i) v[i] = e.residual ? __builtin_fmaf(z[0][i], e.scale, residual_of<BF16>(o.r, i)) : z[0][i] * e.scale;
     put_columns<BF16>(p.y, (long long)m * p.ldy + n, left, v);
 }
-// `count` squares of 32 x 32 that a wavefront has put into LDS from `place` on, 4 KB each: the first is square `first` of the wavefront's, FN to a row of squares;
-// the wavefront's rows begin at m0, its columns at n0.
-template <bool BF16, int FN, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
+// Four columns of a lane to or from a matrix in a window: offsets of the lane and of the wavefront, in bytes.
+template <bool BF16> __device__ __forceinline__ void ask_four(unsigned int (&r)[4], const Window& w, unsigned int at, unsigned int uni)
 {
+    if constexpr (BF16) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(resource(w), (int)at, (int)uni, 0);
+        r[0] = (unsigned int)v[0]; r[1] = (unsigned int)v[1];
+    } else {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b128(resource(w), (int)at, (int)uni, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = (unsigned int)v[i];
+    }
+}
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+template <bool BF16> __device__ __forceinline__ void give_four(const Window& w, unsigned int at, unsigned int uni, v4f v)
+{
+    if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b64(v2u{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, resource(w), (int)at, (int)uni, 0);
+    else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), resource(w), (int)at, (int)uni, 0);
+}
+// Whether the part of a matrix of `rows` x `columns` from (m0, n0) on can go by such windows: all of it there, fours on their own alignment, 32-bit offsets.
+template <typename P> __device__ __forceinline__ bool by_windows(const P& p, int m0, int n0, int rows, int columns, unsigned int size)
+{
+    const Epilogue& e = p.e;
+    const unsigned long long on = (reinterpret_cast<unsigned long long>(p.y) | (unsigned long long)p.ldy * size | (e.residual ? reinterpret_cast<unsigned long long>(e.residual) | (unsigned long long)e.ldr * size : 0) |
+                                   (e.z ? reinterpret_cast<unsigned long long>(e.z) | (unsigned long long)e.ldz * size : 0)) & (4 * size - 1);
+    const long long far = (long long)(1 << 30) / (rows * (int)size);
+    return on == 0 && (reinterpret_cast<unsigned long long>(e.bias) & 15) == 0 && m0 + rows <= p.M && n0 + columns <= p.N && p.ldy < far && (!e.residual || e.ldr < far) && (!e.z || e.ldz < far);
+}
+// `count` squares of 32 x 32 that a wavefront has put into LDS from `place` on, 4 KB each: the first is square `first` of the wavefront's, FN to a row of squares;
+// the wavefront's ROWS rows begin at m0, its columns at n0.
+// Where all of the wavefront's part is inside y, everything goes by windows: a matrix that is not there is an empty one, from which zeros come and into which nothing
+// goes, so that no branch stands between loads and stores, and a square's operands, asked for while the one before is finished, are waited for without the
+// stores in between.  (With a branch around each, the wait was for all of them: 4096 x 11008 x 4096 with gelu and z took @FAST@.)
+template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
+{
+    constexpr unsigned int SIZE = BF16 ? 2 : 4;
+    if (by_windows(p, m0, n0, ROWS, 32 * FN, SIZE)) {
+        const Epilogue& e = p.e;
+        auto over = [&](const void* x, long long ld) {
+            return window(x ? reinterpret_cast<const char*>(x) + ((long long)m0 * ld + n0) * SIZE : nullptr, x ? (unsigned int)((ROWS - 1) * ld + 32 * FN) * SIZE : 0u);
+        };
+        const Window wy = over(p.y, p.ldy), wz = over(e.z, e.ldz), wr = over(e.residual, e.ldr), wb = window(e.bias ? e.bias + n0 : nullptr, e.bias ? 32 * FN * 4 : 0);
+        const unsigned int r8 = (unsigned int)(lane >> 3), c4 = 4 * (unsigned int)(lane & 7);
+        const unsigned int aty = (r8 * (unsigned int)p.ldy + c4) * SIZE, atz = (r8 * (unsigned int)e.ldz + c4) * SIZE, atr = (r8 * (unsigned int)e.ldr + c4) * SIZE;
+        struct Operands { unsigned int r[4][4], b[4]; };
+        auto ask = [&](Operands& o, int s) {
+            const unsigned int row = (unsigned int)(s / FN) * 32, column = (unsigned int)(s % FN) * 32;
+            ask_four<false>(o.b, wb, c4 * 4, column * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ask_four<BF16>(o.r[i], wr, atr, ((row + 8 * i) * (unsigned int)e.ldr + column) * SIZE);
+        };
+        Operands next;
+        ask(next, first);
+#pragma unroll 1
+        for (int s = 0; s < count; ++s) {
+            const Operands o = next;
+            ask(next, first + (s + 1 < count ? s + 1 : s));
+            const unsigned int row = (unsigned int)((first + s) / FN) * 32, column = (unsigned int)((first + s) % FN) * 32;
+            v4f v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = place[s * 256 + quarter_slot(i, lane)];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] += __uint_as_float(o.b[j]);
+                give_four<BF16>(wz, atz, ((row + 8 * i) * (unsigned int)e.ldz + column) * SIZE, v[i]);
+            }
+            act_by<BF16>(e.act, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = __builtin_fmaf(v[i][j], e.scale, residual_of<BF16>(o.r[i], j));
+                give_four<BF16>(wy, aty, ((row + 8 * i) * (unsigned int)p.ldy + column) * SIZE, v[i]);
+            }
+        }
+        return;
+    }
     auto row = [&](int q) { return m0 + (first + (q >> 2)) / FN * 32 + 8 * (q & 3) + (lane >> 3); };
     auto column = [&](int q) { return n0 + (first + (q >> 2)) % FN * 32 + 4 * (lane & 7); };
     EpilogueOperands here = epilogue_operands<BF16>(p, row(0), column(0));

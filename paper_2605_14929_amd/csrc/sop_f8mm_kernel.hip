@@ -284,7 +284,7 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
         for (int first = 0; first < SQUARES; first += PART) {
 #pragma unroll
             for (int s = first; s < first + PART && s < SQUARES; ++s) put_square(place + (s - first) * 256, lane, acc[s / FN][s % FN]);
-            finish_squares<!EXACT, FN>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
+            finish_squares<!EXACT, FN, FM * 32>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
         }
     } else {
         v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);

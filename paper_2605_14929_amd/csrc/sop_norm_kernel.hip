@@ -8,7 +8,7 @@
 //
 // Every pass is bound by HBM.  A row stays in the registers of the threads that share it (T threads, C times eight neighbouring elements each), so that it is
 // read once; its sums go over a wavefront by rotations and over a workgroup through LDS.  Threads keep their columns from row to row, so weights, and the
-// backward pass's sums over rows, stay in registers too: a workgroup leaves one row of partial sums, and a second kernel adds those up in a fixed order.
+// backward pass's sums over rows, stay with them: a workgroup leaves one row of partial sums, and a second kernel adds those up in a fixed order.
 // Longer rows (more than 16384 elements, backward 8192) are read several times over instead.
 //
 // Sums of squares are binary32; where one leaves its range (elements beyond 2^63 or so) the row's are formed once more from elements 2^-70 as large.
@@ -22,40 +22,47 @@
 
 namespace sopk {
 
-// The sum over a wavefront, for all lanes
-__device__ __forceinline__ float wave_sum(float x)
+// The sum over sixteen lanes of a wavefront that stand in a row, and over all of it; for all lanes
+__device__ __forceinline__ float sixteen_sum(float x)
 {
-    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));   // row_ror:8, 4, 2, 1: sums of sixteen
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));   // row_ror:8, 4, 2, 1
     x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xF, 0xF, false));
     x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xF, 0xF, false));
     x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xF, 0xF, false));
-    const int b = __float_as_int(x);
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+    const int b = __float_as_int(sixteen_sum(x));
     return (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
            (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
 }
-// Sums over the T threads of a row.  Two places in LDS by turns: whoever writes one has passed the barrier behind the other's reads.
-template <int T> struct RowSums {
-    static constexpr int W = T / 64;
-    float (*slot)[16][4];                                               // [2][wavefronts][sums]
+// Up to four sums over a row's threads: a wavefront's own, or those of a workgroup of up to sixteen, which leave theirs in LDS, where a lane reads the one of its place
+// in a row of sixteen (places without a wavefront hold zeros).  Two sets of places by turns: whoever writes one has passed the barrier behind the other's reads.
+// However they are added, all lanes get the same bits.
+template <bool ONE> struct RowSums {
+    v4f (*slot)[16];                                                    // [2]
     int turn = 0;
+    __device__ __forceinline__ explicit RowSums(v4f (*at)[16]) : slot(at)
+    {
+        if (!ONE && threadIdx.x < 32) slot[threadIdx.x >> 4][threadIdx.x & 15] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!ONE) __syncthreads();
+    }
     template <int N> __device__ __forceinline__ void operator()(float (&v)[N])
     {
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] = wave_sum(v[j]);
-        if constexpr (W > 1) {
-            const int wave = threadIdx.x >> 6;
+        if constexpr (!ONE) {
             if ((threadIdx.x & 63) == 0) {
+                v4f mine = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int j = 0; j < N; ++j) slot[turn][wave][j] = v[j];
+                for (int j = 0; j < N; ++j) mine[j] = v[j];
+                slot[turn][threadIdx.x >> 6] = mine;
             }
             __syncthreads();
+            const v4f its = slot[turn][threadIdx.x & 15];
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                float s = slot[turn][0][j];
-#pragma unroll
-                for (int w = 1; w < W; ++w) s += slot[turn][w][j];
-                v[j] = s;
-            }
+            for (int j = 0; j < N; ++j) v[j] = sixteen_sum(its[j]);
             turn ^= 1;
         }
     }
@@ -68,13 +75,13 @@ __device__ __forceinline__ float unit_of(float sum, float inv_d, float eps) { re
 __device__ __forceinline__ float unit_of_fewer(float sum, float inv_d) { return __builtin_amdgcn_rsqf(sum * inv_d) * SOPK_FEWER; }
 
 // ---- forward, a row in registers
-template <int T, int C, bool YB, bool RB>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormParams p, long long each)
+template <bool ONE, int C, int MOST, bool YB, bool RB>
+__global__ __launch_bounds__(MOST) void norm_kernel(const NormParams p, long long each)
 {
-    constexpr int RW = T < 256 ? 256 / T : 1;
-    __shared__ float slot[2][16][4];
-    RowSums<T> sums{slot};
-    const int t = threadIdx.x & (T - 1), who = RW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / T) : 0;
+    constexpr int RW = ONE ? MOST / 64 : 1;                             // rows at a time
+    __shared__ v4f slot[2][16];
+    RowSums<ONE> sums(slot);
+    const int T = ONE ? 64 : blockDim.x, t = ONE ? threadIdx.x & 63 : threadIdx.x, who = ONE ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const float inv_d = 1.0f / (float)p.D;
     int k[C], left[C];
     float f[C][8], b[C][8];
@@ -174,8 +181,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormParam
 template <bool YB, bool RB>
 __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
 {
-    __shared__ float slot[2][16][4];
-    RowSums<1024> sums{slot};
+    __shared__ v4f slot[2][16];
+    RowSums<false> sums(slot);
     const float inv_d = 1.0f / (float)p.D;
     const int whole = (p.D + 8191) / 8192 * 8192;                       // (all lanes of sixteen take part in a block's maximum)
     for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
@@ -248,16 +255,19 @@ __device__ __forceinline__ Share share_of(const NormGradParams& p, long long w)
 }
 __device__ __forceinline__ long long begin_of(const NormGradParams& p, long long g, int part) { return g * p.per_group + part * p.per_group / p.parts; }
 
-// What sums over rows a thread has when a group ends: t = sum of dr x
-template <int C> __device__ __forceinline__ void end_group(long long w, long long g, const int (&k)[C], const int (&left)[C], float (&t)[C][8], float (&da)[C][8])
+// What sums over rows a thread has when a group ends, t = sum of dr x: a part of it, from which dgate and dafter are joined; or, of a whole group, dgate, and what dafter gets of it
+template <int C> __device__ __forceinline__ void end_group(long long w, long long g, const int (&k)[C], const int (&left)[C], const float (&t)[C][8], float (&da)[C][8])
 {
     const NormGradParams& p = seldom();
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+        if (p.parts > 1) {
+            put<false>(p.part_t + w * p.D, k[c], left[c], t[c]);
+            continue;
+        }
         float gate[8];
         gate8(p.gate, p.ldg, p.gate_bf16, g, k[c], left[c], gate);
-        if (p.dgate && p.parts > 1) put<false>(p.part_t + w * p.D, k[c], left[c], t[c]);
-        else if (p.dgate) {
+        if (p.dgate) {
             float after[8];
             vector8(p.after, k[c], left[c], 1.0f, after);
 #pragma unroll
@@ -265,84 +275,112 @@ template <int C> __device__ __forceinline__ void end_group(long long w, long lon
             put_numbers(p.dgate, g, p.lddg, p.gate_bf16, k[c], left[c], after);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { da[c][i] = __builtin_fmaf(p.scale * gate[i], t[c][i], da[c][i]); t[c][i] = 0.0f; }
+        for (int i = 0; i < 8; ++i) da[c][i] = p.scale * gate[i] * t[c][i];
     }
 }
 
-// ---- backward, a row in registers
-template <int T, int C, bool YB, bool RB>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_grad_kernel(const NormGradParams p)
+// ---- backward, a row in registers.  The next row is on its way while one is worked on.  What a thread keeps of its columns beside the sums of the rows (weights, and dafter's
+// sums, which a group's end adds to) stands in LDS, in places of its own.
+template <bool ONE, int C, int MOST, bool YB, bool RB>
+__global__ __launch_bounds__(MOST) void norm_grad_kernel(const NormGradParams p)
 {
-    constexpr int RW = T < 256 ? 256 / T : 1;
-    __shared__ float slot[2][16][4];
-    __shared__ float joined[RW > 1 ? RW : 1][RW > 1 ? C * T * 8 : 1];
-    RowSums<T> sums{slot};
-    const int t = threadIdx.x & (T - 1), who = RW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / T) : 0;
+    constexpr int RW = ONE ? MOST / 64 : 1;
+    extern __shared__ __align__(16) unsigned char kept[];
+    __shared__ v4f slot[2][16];
+    RowSums<ONE> sums(slot);
+    const int NT = blockDim.x, T = ONE ? 64 : NT, t = ONE ? threadIdx.x & 63 : threadIdx.x, who = ONE ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const float inv_d = 1.0f / (float)p.D;
+    enum { FACTOR, BEFORE, AFTER, JOIN };
+    auto place = [&](int what, int c, int half, int thread) -> v4f& { return reinterpret_cast<v4f*>(kept)[((what * C + c) * 2 + half) * NT + thread]; };
+    auto keep = [&](int what, int c, const float (&v)[8]) {
+        place(what, c, 0, threadIdx.x) = v4f{v[0], v[1], v[2], v[3]};
+        place(what, c, 1, threadIdx.x) = v4f{v[4], v[5], v[6], v[7]};
+    };
+    auto have = [&](int what, int c, float (&v)[8]) {
+        const v4f a = place(what, c, 0, threadIdx.x), b = place(what, c, 1, threadIdx.x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    };
     int k[C], left[C];
-    float f[C][8], b[C][8], st[C][8], sa[C][8], sb[C][8];
+    float st[C][8], sb[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         k[c] = (c * T + t) * 8;
         left[c] = p.D - k[c];
-        vector8(seldom().before, k[c], left[c], 0.0f, b[c]);
+        float b[8], none[8];
+        vector8(seldom().before, k[c], left[c], 0.0f, b);
+        keep(BEFORE, c, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) st[c][i] = sa[c][i] = sb[c][i] = 0.0f;
+        for (int i = 0; i < 8; ++i) st[c][i] = sb[c][i] = none[i] = 0.0f;
+        keep(AFTER, c, none);
+        keep(FACTOR, c, none);
     }
     // the wavefronts of a workgroup that have a row each put their sums together: the first one has them all
     auto join = [&](float (&v)[C][8]) {
-        if constexpr (RW > 1) {
+        if constexpr (ONE) {
             __syncthreads();
+#pragma unroll
+            for (int c = 0; c < C; ++c) keep(JOIN, c, v[c]);
+            __syncthreads();
+            if (who != 0) return;
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) joined[who][(c * 8 + i) * T + t] = v[c][i];
-            __syncthreads();
+                for (int w = 1; w < RW; ++w)
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                    for (int half = 0; half < 2; ++half) {
+                        const v4f a = place(JOIN, c, half, w * 64 + t);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float s = joined[0][(c * 8 + i) * T + t];
+                        for (int i = 0; i < 4; ++i) v[c][4 * half + i] += a[i];
+                    }
+        }
+    };
+    struct Row { Raw<RB> s[C], d[C]; Raw<YB> n[C], y[C]; };
+    auto load = [&](Row& r, long long m) {
 #pragma unroll
-                    for (int w = 1; w < RW; ++w) s += joined[w][(c * 8 + i) * T + t];
-                    v[c][i] = who == 0 ? s : 0.0f;
-                }
+        for (int c = 0; c < C; ++c) {
+            r.s[c] = p.before ? ask<RB>(reinterpret_cast<const char*>(p.s) + m * p.lds * (RB ? 2 : 4), k[c], left[c]) : nothing<RB>();
+            r.n[c] = p.before ? ask<YB>(reinterpret_cast<const char*>(p.dn) + m * p.lddn * (YB ? 2 : 4), k[c], left[c]) : nothing<YB>();
+            r.y[c] = p.y ? ask<YB>(reinterpret_cast<const char*>(p.y) + m * p.ldy * (YB ? 2 : 4), k[c], left[c]) : nothing<YB>();
+            r.d[c] = p.ds ? ask<RB>(reinterpret_cast<const char*>(p.ds) + m * p.ldds * (RB ? 2 : 4), k[c], left[c]) : nothing<RB>();
         }
     };
     const Share z = share_of(seldom(), blockIdx.x);
+    Row row;
+    long long held = -1;                                                // the row that has been asked for
     for (long long g = z.g0; g < z.g1; ++g) {
         if (p.y) {
             const NormGradParams& p = seldom();
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                float after[8];
-                gate8(p.gate, p.ldg, p.gate_bf16, g, k[c], left[c], f[c]);
+                float f[8], after[8];
+                gate8(p.gate, p.ldg, p.gate_bf16, g, k[c], left[c], f);
                 vector8(p.after, k[c], left[c], 1.0f, after);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[c][i] = p.scale * f[c][i] * after[i];
+                for (int i = 0; i < 8; ++i) f[i] = p.scale * f[i] * after[i];
+                keep(FACTOR, c, f);
             }
         }
-        const long long end = begin_of(seldom(), g, z.part + 1);
-        for (long long m = begin_of(seldom(), g, z.part) + who; m < end; m += RW) {
-            Raw<RB> rs[C], rd[C];
-            Raw<YB> rn[C], ry[C];
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                rs[c] = p.before ? ask<RB>(reinterpret_cast<const char*>(p.s) + m * p.lds * (RB ? 2 : 4), k[c], left[c]) : nothing<RB>();
-                rn[c] = p.before ? ask<YB>(reinterpret_cast<const char*>(p.dn) + m * p.lddn * (YB ? 2 : 4), k[c], left[c]) : nothing<YB>();
-                ry[c] = p.y ? ask<YB>(reinterpret_cast<const char*>(p.y) + m * p.ldy * (YB ? 2 : 4), k[c], left[c]) : nothing<YB>();
-                rd[c] = p.ds ? ask<RB>(reinterpret_cast<const char*>(p.ds) + m * p.ldds * (RB ? 2 : 4), k[c], left[c]) : nothing<RB>();
-            }
+        const long long begin = begin_of(seldom(), g, z.part), end = begin_of(seldom(), g, z.part + 1);
+        const long long after_end = g + 1 < z.g1 ? end + who : -1;      // (rows of a workgroup's groups follow each other)
+        for (long long m = begin + who; m < end; m += RW) {
+            if (held != m) load(row, m);
+            const Row now = row;
+            held = m + RW < end ? m + RW : after_end;
+            if (held >= 0 && held < p.M) load(row, held);
             float sum[3] = {0.0f, 0.0f, 0.0f};                          // of s^2, p s and y^2
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c) {
+                float b[8];
+                have(BEFORE, c, b);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float s = at(rs[c], i), y = at(ry[c], i);
+                    const float s = at(now.s[c], i), y = at(now.y[c], i);
                     sum[0] = __builtin_fmaf(s, s, sum[0]);
-                    sum[1] = __builtin_fmaf(b[c][i] * at(rn[c], i), s, sum[1]);
+                    sum[1] = __builtin_fmaf(b[i] * at(now.n[c], i), s, sum[1]);
                     sum[2] = __builtin_fmaf(y, y, sum[2]);
                 }
+            }
             sums(sum);
             float s2 = unit_of(sum[0], inv_d, p.eps), s1 = p.after ? unit_of(sum[2], inv_d, p.eps) : 1.0f, mean = sum[1] * s2 * inv_d;
             if (too_much(sum[0]) || too_much(fabsf(sum[1])) || (p.after && too_much(sum[2]))) {
@@ -351,7 +389,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_grad_kernel(const Norm
                 for (int c = 0; c < C; ++c)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float s = at(rs[c], i) * SOPK_FEWER, y = at(ry[c], i) * SOPK_FEWER;
+                        const float s = at(now.s[c], i) * SOPK_FEWER, y = at(now.y[c], i) * SOPK_FEWER;
                         few[0] = __builtin_fmaf(s, s, few[0]);
                         few[1] = __builtin_fmaf(y, y, few[1]);
                     }
@@ -360,40 +398,50 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_grad_kernel(const Norm
                 if (p.after && too_much(sum[2])) s1 = unit_of_fewer(few[1], inv_d);
                 float ph[1] = {0.0f};
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c) {
+                    float b[8];
+                    have(BEFORE, c, b);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) ph[0] = __builtin_fmaf(b[c][i] * at(rn[c], i), at(rs[c], i) * s2, ph[0]);
+                    for (int i = 0; i < 8; ++i) ph[0] = __builtin_fmaf(b[i] * at(now.n[c], i), at(now.s[c], i) * s2, ph[0]);
+                }
                 sums(ph);
                 mean = ph[0] * inv_d;
             }
             float dr[C][8], qx[1] = {0.0f};
 #pragma unroll
             for (int c = 0; c < C; ++c) {
+                float b[8];
+                have(BEFORE, c, b);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float h = at(rs[c], i) * s2, x = at(ry[c], i) * s1, dn = at(rn[c], i);
-                    dr[c][i] = __builtin_fmaf(s2, __builtin_fmaf(-h, mean, b[c][i] * dn), at(rd[c], i));
+                    const float h = at(now.s[c], i) * s2, x = at(now.y[c], i) * s1, dn = at(now.n[c], i);
+                    dr[c][i] = __builtin_fmaf(s2, __builtin_fmaf(-h, mean, b[i] * dn), at(now.d[c], i));
                     sb[c][i] = __builtin_fmaf(dn, h, sb[c][i]);
                     st[c][i] = __builtin_fmaf(dr[c][i], x, st[c][i]);
                 }
                 put<RB>(reinterpret_cast<char*>(p.dr) + m * p.lddr * (RB ? 2 : 4), k[c], left[c], dr[c]);
             }
             if (!p.y) continue;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {                               // dr becomes q
+                float f[8];
+                have(FACTOR, c, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    dr[c][i] *= f[i];
+                    qx[0] = __builtin_fmaf(dr[c][i], at(now.y[c], i) * s1, qx[0]);
+                }
+            }
             if (p.after) {
+                sums(qx);
+                const float c1 = qx[0] * inv_d;
 #pragma unroll
                 for (int c = 0; c < C; ++c)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) qx[0] = __builtin_fmaf(f[c][i] * dr[c][i], at(ry[c], i) * s1, qx[0]);
-                sums(qx);
+                    for (int i = 0; i < 8; ++i) dr[c][i] = s1 * __builtin_fmaf(-at(now.y[c], i) * s1, c1, dr[c][i]);
             }
-            const float c1 = qx[0] * inv_d;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float q = f[c][i] * dr[c][i];
-                    dr[c][i] = p.after ? s1 * __builtin_fmaf(-at(ry[c], i) * s1, c1, q) : q;
-                }
                 put<YB>(reinterpret_cast<char*>(p.dy) + m * p.lddy * (YB ? 2 : 4), k[c], left[c], dr[c]);
                 if (p.q.codes) put_codes(p.q, p.e5m2, dr[c], m, k[c], left[c]);
             }
@@ -401,7 +449,17 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_grad_kernel(const Norm
         const NormGradParams& r = seldom();
         if (r.dafter || r.dgate) {
             join(st);
-            if (who == 0) end_group<C>(blockIdx.x, g, k, left, st, sa);
+            if (who == 0) {
+                float da[C][8], had[8];
+                end_group<C>(blockIdx.x, g, k, left, st, da);
+#pragma unroll
+                for (int c = 0; c < C && r.parts == 1; ++c) {
+                    have(AFTER, c, had);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) had[i] += da[c][i];
+                    keep(AFTER, c, had);
+                }
+            }
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -413,7 +471,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_grad_kernel(const Norm
     if (who != 0) return;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        if (r.dafter) put<false>(r.part_a + (long long)blockIdx.x * r.D, k[c], left[c], sa[c]);
+        float da[8];
+        have(AFTER, c, da);
+        if (r.dafter && r.parts == 1) put<false>(r.part_a + (long long)blockIdx.x * r.D, k[c], left[c], da);
         if (r.dbefore) put<false>(r.part_b + (long long)blockIdx.x * r.D, k[c], left[c], sb[c]);
     }
 }
@@ -451,8 +511,8 @@ template <bool YB, bool RB> struct LongRow {
 template <bool YB, bool RB>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradParams p)
 {
-    __shared__ float slot[2][16][4];
-    RowSums<1024> sums{slot};
+    __shared__ v4f slot[2][16];
+    RowSums<false> sums(slot);
     const float inv_d = 1.0f / (float)p.D;
     const int whole = (p.D + 8191) / 8192 * 8192;
     for (long long m = blockIdx.x; m < p.M; m += gridDim.x) {
@@ -550,18 +610,24 @@ __global__ __launch_bounds__(256) void norm_grad_columns_kernel(const NormGradPa
         }
         if (p.dafter || p.dgate) {
             join(st);
-            if (wave == 0) end_group<1>(word, g, k, left, st, sa);
+            if (wave == 0) {
+                float da[1][8];
+                end_group<1>(word, g, k, left, st, da);
+#pragma unroll
+                for (int i = 0; i < 8 && p.parts == 1; ++i) sa[0][i] += da[0][i];
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) st[0][i] = 0.0f;
         }
     }
     if (p.dbefore) join(sb);
     if (wave != 0) return;
-    if (p.dafter) put<false>(p.part_a + word * p.D, k[0], left[0], sa[0]);
+    if (p.dafter && p.parts == 1) put<false>(p.part_a + word * p.D, k[0], left[0], sa[0]);
     if (p.dbefore) put<false>(p.part_b + word * p.D, k[0], left[0], sb[0]);
 }
 
-// ---- the rows of partial sums added up, in binary64, in a fixed order: 32 columns a workgroup, its 32 half-wavefronts share the rows
+// ---- the rows of partial sums added up, in binary64, in a fixed order: 32 columns a workgroup, its 32 half-wavefronts share the rows.  Row i of the first set has the
+// weight of its gate's row, i / share.
 __global__ __launch_bounds__(1024) void join_kernel(const JoinParams p)
 {
     __shared__ double part[32][33];
@@ -569,16 +635,38 @@ __global__ __launch_bounds__(1024) void join_kernel(const JoinParams p)
     long long set = blockIdx.y;
     int j = 0;
     while (j < 2 && set >= p.sets[j]) { set -= p.sets[j]; ++j; }
-    const long long rows = p.rows[j];
-    const float* from = p.part[j] + set * rows * p.D + d;
+    const int rows = (int)p.rows[j], at = d < p.D ? d : p.D - 1;
+    const float* from = p.part[j] + set * rows * p.D + at;
+    const bool weighted = j == 0 && p.gate;
+    auto weight = [&](int i) {
+        const long long k = (unsigned int)i / (unsigned int)p.share * p.ldg + at;
+        return (double)(p.gate_bf16 ? __uint_as_float((unsigned int)reinterpret_cast<const uint16_t*>(p.gate)[k] << 16) : reinterpret_cast<const float*>(p.gate)[k]);
+    };
     double s = 0.0;
-    if (d < p.D) {
-        long long i = row;
-        for (; i + 96 < rows; i += 128) {
-            const float a = from[i * p.D], b = from[(i + 32) * p.D], c = from[(i + 64) * p.D], e = from[(i + 96) * p.D];
-            s += ((double)a + (double)b) + ((double)c + (double)e);
+    const long long step = 32ll * p.D;
+    const float* q = from + (long long)row * p.D;
+    int i = row;
+    for (; i + 224 < rows; i += 256, q += 8 * step) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = q[u * step];
+        if (weighted) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s = __builtin_fma((double)v[u], weight(i + 32 * u), s);
+        } else {
+            s += (((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3])) + (((double)v[4] + (double)v[5]) + ((double)v[6] + (double)v[7]));
         }
-        for (; i < rows; i += 32) s += (double)from[i * p.D];
+    }
+    if (i < rows) {                                                     // the last ones, asked for together too
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = from[(long long)(i + 32 * u < rows ? i + 32 * u : rows - 1) * p.D];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const bool in = i + 32 * u < rows;
+            if (weighted) s = in ? __builtin_fma((double)v[u], weight(in ? i + 32 * u : i), s) : s;
+            else s += in ? (double)v[u] : 0.0;
+        }
     }
     part[row][col] = s;
     __syncthreads();
@@ -586,21 +674,28 @@ __global__ __launch_bounds__(1024) void join_kernel(const JoinParams p)
     s = 0.0;
 #pragma unroll
     for (int i = 0; i < 32; ++i) s += part[i][col];
-    if (j == 2) s *= (double)p.factor * (p.after ? (double)p.after[d] : 1.0);
+    if (j != 1) s *= (double)p.factor;
+    if (j == 2 && p.after) s *= (double)p.after[d];
     if (p.out_bf16[j]) reinterpret_cast<uint16_t*>(p.out[j])[set * p.ldo[j] + d] = (uint16_t)bf16_bits((float)s);
     else reinterpret_cast<float*>(p.out[j])[set * p.ldo[j] + d] = (float)s;
 }
 
-template <int T, int C, bool YB, bool RB> static hipError_t norm_go(const NormParams& p, int n_cu, hipStream_t st)
+template <bool ONE, int C, int MOST, bool YB, bool RB> static hipError_t norm_go(const NormParams& p, int T, int n_cu, hipStream_t st)
 {
-    constexpr int RW = T < 256 ? 256 / T : 1, NT = T < 256 ? 256 : T;
-    const long long most = (long long)n_cu * 2048 / NT * RW, each = (p.M + most - 1) / most, units = (p.M + each - 1) / each;
-    hipLaunchKernelGGL((norm_kernel<T, C, YB, RB>), dim3((unsigned)((units + RW - 1) / RW)), dim3(NT), 0, st, p, each);
+    const int RW = ONE ? MOST / 64 : 1, NT = ONE ? MOST : T;
+    const long long most = (long long)n_cu * (2048 / NT) * RW, each = (p.M + most - 1) / most, units = (p.M + each - 1) / each;
+    hipLaunchKernelGGL((norm_kernel<ONE, C, MOST, YB, RB>), dim3((unsigned)((units + RW - 1) / RW)), dim3(NT), 0, st, p, each);
     return hipGetLastError();
 }
-template <int T, int C, bool YB, bool RB> static hipError_t norm_grad_go(const NormGradParams& p, hipStream_t st)
+template <bool ONE, int C, int MOST, bool YB, bool RB> static hipError_t norm_grad_go(const NormGradParams& p, int T, hipStream_t st)
 {
-    hipLaunchKernelGGL((norm_grad_kernel<T, C, YB, RB>), dim3((unsigned)p.words), dim3(T < 256 ? 256 : T), 0, st, p);
+    const int NT = ONE ? MOST : T, bytes = (ONE ? 4 : 3) * C * 32 * NT;
+    auto fn = &norm_grad_kernel<ONE, C, MOST, YB, RB>;
+    if (bytes > 64 * 1024 - 512) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(fn, dim3((unsigned)p.words), dim3(NT), bytes, st, p);
     return hipGetLastError();
 }
 static long long grid_of(long long n, long long most) { return n < most ? n : most; }
@@ -608,28 +703,18 @@ static long long grid_of(long long n, long long most) { return n < most ? n : mo
 template <bool YB, bool RB> static hipError_t norm_shape_go(const NormParams& p, int n_cu, hipStream_t st)
 {
     const sopr::RowShape s = sopr::norm_shape(p.D);
-    switch (s.T * 16 + s.C) {
-    case 64 * 16 + 1: return norm_go<64, 1, YB, RB>(p, n_cu, st);
-    case 64 * 16 + 2: return norm_go<64, 2, YB, RB>(p, n_cu, st);
-    case 256 * 16 + 1: return norm_go<256, 1, YB, RB>(p, n_cu, st);
-    case 256 * 16 + 2: return norm_go<256, 2, YB, RB>(p, n_cu, st);
-    case 512 * 16 + 2: return norm_go<512, 2, YB, RB>(p, n_cu, st);
-    case 512 * 16 + 3: return norm_go<512, 3, YB, RB>(p, n_cu, st);
-    case 512 * 16 + 4: return norm_go<512, 4, YB, RB>(p, n_cu, st);
-    }
+    if (s.T == 64) return s.C == 1 ? norm_go<true, 1, 256, YB, RB>(p, s.T, n_cu, st) : norm_go<true, 2, 256, YB, RB>(p, s.T, n_cu, st);
+    if (s.C == 1) return norm_go<false, 1, 256, YB, RB>(p, s.T, n_cu, st);
+    if (s.C == 2) return norm_go<false, 2, 512, YB, RB>(p, s.T, n_cu, st);
+    if (s.C == 4) return norm_go<false, 4, 512, YB, RB>(p, s.T, n_cu, st);
     hipLaunchKernelGGL((norm_long_kernel<YB, RB>), dim3((unsigned)grid_of(p.M, 2 * n_cu)), dim3(1024), 0, st, p);
     return hipGetLastError();
 }
 template <bool YB, bool RB> static hipError_t norm_grad_shape_go(const NormGradParams& p, int n_cu, hipStream_t st)
 {
     const sopr::RowShape s = sopr::norm_grad_shape(p.D);
-    switch (s.T * 16 + s.C) {
-    case 64 * 16 + 1: return norm_grad_go<64, 1, YB, RB>(p, st);
-    case 64 * 16 + 2: return norm_grad_go<64, 2, YB, RB>(p, st);
-    case 256 * 16 + 1: return norm_grad_go<256, 1, YB, RB>(p, st);
-    case 256 * 16 + 2: return norm_grad_go<256, 2, YB, RB>(p, st);
-    case 512 * 16 + 2: return norm_grad_go<512, 2, YB, RB>(p, st);
-    }
+    if (s.T == 64) return s.C == 1 ? norm_grad_go<true, 1, 256, YB, RB>(p, s.T, st) : norm_grad_go<true, 2, 256, YB, RB>(p, s.T, st);
+    if (s.C == 1) return norm_grad_go<false, 1, 1024, YB, RB>(p, s.T, st);
     hipLaunchKernelGGL((norm_grad_long_kernel<YB, RB>), dim3((unsigned)grid_of(p.M, 2 * n_cu)), dim3(1024), 0, st, p);
     if (p.dafter || p.dbefore || p.dgate) hipLaunchKernelGGL((norm_grad_columns_kernel<YB, RB>), dim3((unsigned)((p.D + 511) / 512), (unsigned)p.words), dim3(256), 0, st, p);
     return hipGetLastError();

@@ -584,7 +584,7 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
         for (int first = 0; first < SQUARES; first += PART) {
 #pragma unroll
             for (int s = first; s < first + PART && s < SQUARES; ++s) put_square(place + (s - first) * 256, lane, acc[s / F][s % F]);
-            finish_squares<true, F>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
+            finish_squares<true, F, E * 32>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
         }
     } else {
         v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);

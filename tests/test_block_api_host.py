@@ -78,7 +78,7 @@ def test_packed_product_with_an_epilogue_in_two_launches(lib):
     assert lib.sop_packed_linear(lib.ctx, AT, 8, _packed(1, 8, 8), 4, e, AT, 1, None) == EINVAL
 
 
-def _act_grad(lib, M=100, N=600, dy=AT, lddy=None, z=AT, ldz=None, dtype=B.F32, act=3, dz=AT + 4, lddz=None, dz8=None, db=AT, ws=1 << 30, size=None):
+def _act_grad(lib, M=1000, N=600, dy=AT, lddy=None, z=AT, ldz=None, dtype=B.F32, act=3, dz=AT + 4, lddz=None, dz8=None, db=AT, ws=1 << 30, size=None):
     n = C.c_size_t()
     assert lib.sop_fp8_linear_grad_workspace(lib.ctx, M, N, C.byref(n)) == OK
     return lib.sop_fp8_linear_grad(lib.ctx, dy, N if lddy is None else lddy, z, N if ldz is None else ldz, dtype, M, N, act, 1.0, dz, N if lddz is None else lddz,
@@ -86,22 +86,22 @@ def _act_grad(lib, M=100, N=600, dy=AT, lddy=None, z=AT, ldz=None, dtype=B.F32, 
 
 
 def test_gradient_of_an_epilogue(lib):
-    for M in (1, 4, 5, 100, 8192, 100000):
+    for M in (1, 4, 5, 100, 128, 129, 8192, 100000):
         for N in (1, 512, 513, 11008, 1 << 20):
             status, size = _act_grad(lib, M, N)
             assert status == OK
             said = {s[0]: [int(v) for v in s[1:]] for s in _said(lib)}
             m, n, words, strips, part = said["act_grad"]
             assert (m, n, strips) == (M, N, -(-N // 512)) and words * strips <= max(strips, 2048) and 1 <= words <= -(-M // 4)
-            assert size == (words * N * 4 if words > 1 else 0) and part == ((1 << 30) if words > 1 else 0)
-            assert ("join" in said) == (words > 1)
-            if words > 1:
+            assert size == (words * N * 4 if M > 128 else 0) and part == ((1 << 30) if M > 128 else 0)
+            assert ("join" in said) == (M > 128)                       # few rows: a workgroup has all of a column
+            if M > 128:
                 assert said["join"] == [0, 1, words, 1 << 30, AT]
     assert _act_grad(lib, 0)[0] == OK and _said(lib) == [["join", "0", "1", "0", "0", str(AT)]]   # no rows: zeros
     assert _act_grad(lib, 0, db=None)[0] == OK and _said(lib) == []
     assert _act_grad(lib, act=0, z=None, dz=None)[0] == OK
-    for more in (dict(dtype=2), dict(act=5), dict(dy=None), dict(dy=AT + 2), dict(z=None), dict(lddy=599), dict(lddz=599), dict(ldz=1), dict(db=AT + 1), dict(dz8=_f8(100, 600, 128)),
-                 dict(dz8=_f8(100, 600, fmt=3)), dict(dz8=_f8(100, 600, ld=592)), dict(dz8=_f8(100, 600, ld=600))):
+    for more in (dict(dtype=2), dict(act=5), dict(dy=None), dict(dy=AT + 2), dict(z=None), dict(lddy=599), dict(lddz=599), dict(ldz=1), dict(db=AT + 1), dict(dz8=_f8(1000, 600, 128)),
+                 dict(dz8=_f8(1000, 600, fmt=3)), dict(dz8=_f8(1000, 600, ld=592)), dict(dz8=_f8(1000, 600, ld=600))):
         assert _act_grad(lib, **more)[0] == EINVAL, more
     for more in (dict(ws=None), dict(ws=(1 << 30) + 8), dict(size=0)):
         assert _act_grad(lib, **more)[0] == ENOMEM, more
@@ -152,7 +152,7 @@ def _norm_grad(lib, M=6, D=300, o=None, ws=1 << 32, size=None, fmt=True, **kw):
 
 def test_norm_gradients(lib):
     """Every row of a group is somebody's; partial sums, and what long rows keep, lie in the workspace; every sum has its rows joined."""
-    for D in (1, 300, 512, 600, 2048, 4096, 8192, 8193, 20000):
+    for D in (1, 300, 512, 600, 1025, 2048, 4096, 8192, 8193, 16384, 16385, 20000):
         for M, G in ((1, 1), (6, 3), (777, 3), (5000, 1), (4096, 4096), (1200, 600), (2000, 1000), (3000, 1500), (100000, 2)):
             status, size = _norm_grad(lib, M, D, _opts(gate=AT, ld_gate=D, groups=G, gate_dtype=G % 2), dgate=1 << 62)
             assert status == OK, lib.stub_error()
@@ -165,9 +165,8 @@ def test_norm_gradients(lib):
                 assert [p * each // parts for p in range(parts + 1)][-1] == each
             else:
                 assert words <= G and [w * G // words for w in range(words + 1)][-1] == G and all((w + 1) * G // words > w * G // words for w in range(words))
-            assert words <= 1024 and (a, b) == (base, base + row)
-            end = base + (3 if parts > 1 else 2) * row
-            assert parts == 1 or t == end - row
+            assert words <= 2048 and (a, t, b) == (base, base, base + row)
+            end = base + 2 * row
             assert size == end - base + (12 * M if D > 8192 else 0) and (D <= 8192 or st == end)
             joins = {int(s[1]): [int(v) for v in s[2:]] for s in said[1:]}
             assert joins[0][:3] == [1, words, a] and joins[1][:3] == [1, words, b] and (2 in joins) == (parts > 1)
