@@ -13,10 +13,11 @@ inline RowShape norm_shape(long long D)
     const int C = D <= 512 ? 1 : D <= 1024 ? 2 : D <= 2048 ? 1 : D <= 8192 ? 2 : 4;
     return D > 16384 ? RowShape{0, 0} : RowShape{threads_for(D, C), C};
 }
-// Backward, where a thread holds four times as much: eight elements up to 8192 (8192 x 4096 bf16 105 us, sixteen 108; 777 x 5024 fp32 32 and 34).
+// Backward, where a thread holds four times as much: eight elements up to 8192 (8192 x 4096 bf16 105 us, sixteen 108; 777 x 5024 fp32 32 and 34), then
+// sixteen of a row that it does not keep (4096 x 12288 bf16 224 us, by the way of still longer rows 330).
 inline RowShape norm_grad_shape(long long D)
 {
-    return D <= 1024 ? norm_shape(D) : D <= 8192 ? RowShape{threads_for(D, 1), 1} : RowShape{0, 0};
+    return D <= 1024 ? norm_shape(D) : D <= 8192 ? RowShape{threads_for(D, 1), 1} : D <= 16384 ? RowShape{1024, 2} : RowShape{0, 0};
 }
 
 // Rows in G groups of `each` (a group shares a row of the gate), to `words` workgroups: as many groups as there are workgroups and more are dealt out whole

@@ -121,7 +121,8 @@ template <typename P> __device__ __forceinline__ bool by_windows(const P& p, int
 // the wavefront's ROWS rows begin at m0, its columns at n0.
 // Where all of the wavefront's part is inside y, everything goes by windows: a matrix that is not there is an empty one, from which zeros come and into which nothing
 // goes, so that no branch stands between loads and stores, and a square's operands, asked for while the one before is finished, are waited for without the
-// stores in between.  (With a branch around each, the wait was for all of them: 4096 x 11008 x 4096 with gelu and z took @FAST@.)
+// stores in between.  (With a branch around each, the wait was for all of them: 4096 x 11008 x 4096 with gelu and z took 269 us, by windows 217; without an
+// epilogue the product takes 198.)
 template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
 {
     constexpr unsigned int SIZE = BF16 ? 2 : 4;

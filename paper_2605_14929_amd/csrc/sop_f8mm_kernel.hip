@@ -108,10 +108,16 @@ __device__ __forceinline__ void store_y(const F8MmParams& p, int m, int n, v4f v
 }
 
 // ... as they are, or through the epilogue (BF16: the type of y)
-template <bool EPI, bool BF16> __device__ __forceinline__ void leave(const F8MmParams& p, int m, int n, v4f v)
+template <bool EPI, bool BF16> __device__ __forceinline__ void leave(const F8MmParams& p, int m, int n, v4f v, const EpilogueOperands& o)
 {
-    if constexpr (EPI) finish_four<BF16>(p, m, n, v, epilogue_operands<BF16>(p, m, n));
+    if constexpr (EPI) finish_four<BF16>(p, m, n, v, o);
     else store_y(p, m, n, v);
+}
+// what an epilogue reads for the first results of a wavefront, asked for before the steps along K
+template <bool EPI, bool BF16> __device__ __forceinline__ EpilogueOperands asked(const F8MmParams& p, int m, int n, bool any)
+{
+    if constexpr (EPI) if (any) return epilogue_operands<BF16>(p, m, n);
+    return EpilogueOperands{};
 }
 
 // The last step of a K that is no multiple of 128: a row is read up to a multiple of 16, and what lies beyond K becomes zeros in LDS, `rows` rows
@@ -310,6 +316,9 @@ __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, i
     int tm, tn;
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
     const int m0 = tm * (FM * 16), n0 = tn * (FN * 16), KF = p.K >> 7, KB = (p.K + 127) >> 7;
+    auto row = [&](int t) { return m0 + t / FN * 16 + r16; };
+    auto column = [&](int t) { return n0 + t % FN * 16 + 4 * q; };
+    const EpilogueOperands first = asked<EPI, !EXACT>(p, row(wave), column(wave), wave < FM * FN);
     const unsigned char* xr[FM];
     const unsigned char* xsr[FM];
     const unsigned char* wr[FN];
@@ -395,7 +404,7 @@ __global__ __launch_bounds__(W * 64) void f8mm_rows_kernel(const F8MmParams p, i
         v4f s = part[0][a][b][lane];
 #pragma unroll
         for (int i = 1; i < W; ++i) s += part[i][a][b][lane];
-        leave<EPI, !EXACT>(p, m0 + a * 16 + r16, n0 + b * 16 + 4 * q, s);
+        leave<EPI, !EXACT>(p, row(t), column(t), s, t == wave ? first : asked<EPI, !EXACT>(p, row(t), column(t), true));
     }
 }
 
@@ -414,6 +423,9 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
     int tm, tn;
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
     const int m0 = tm * (32 * FM), n0 = tn * (32 * FN), KF = p.K >> 7, KB = (p.K + 127) >> 7;
+    auto row = [&](int t) { return m0 + (t >> 2) / FN * 32 + 8 * (t & 3) + (lane >> 3); };
+    auto column = [&](int t) { return n0 + (t >> 2) % FN * 32 + 4 * (lane & 7); };
+    const EpilogueOperands first = asked<EPI, !EXACT>(p, row(wave), column(wave), wave < FM * FN * 4);
     const unsigned char* xb = p.x + (long long)m0 * p.ldx;
     const unsigned char* wb = p.w + (long long)n0 * p.ldw;
     unsigned char* own = lds + wave * OWN;
@@ -503,11 +515,11 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
         for (int b = 0; b < FN; ++b) put_square(reinterpret_cast<v4f*>(own) + (a * FN + b) * 256, lane, acc[a][b]);
     __syncthreads();
     for (int t = wave; t < FM * FN * 4; t += W) {                         // a quarter of a square
-        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3, at = (t >> 2) * 256 + quarter_slot(i, lane);
+        const int at = (t >> 2) * 256 + quarter_slot(t & 3, lane);
         v4f s = reinterpret_cast<const v4f*>(lds)[at];
 #pragma unroll
         for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[at];
-        leave<EPI, !EXACT>(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
+        leave<EPI, !EXACT>(p, row(t), column(t), s, t == wave ? first : asked<EPI, !EXACT>(p, row(t), column(t), true));
     }
 }
 

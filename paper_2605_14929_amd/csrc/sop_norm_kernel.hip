@@ -9,7 +9,7 @@
 // Every pass is bound by HBM.  A row stays in the registers of the threads that share it (T threads, C times eight neighbouring elements each), so that it is
 // read once; its sums go over a wavefront by rotations and over a workgroup through LDS.  Threads keep their columns from row to row, so weights, and the
 // backward pass's sums over rows, stay with them: a workgroup leaves one row of partial sums, and a second kernel adds those up in a fixed order.
-// Longer rows (more than 16384 elements, backward 8192) are read several times over instead.
+// Backward, rows of more than 8192 elements are read three times over instead, two of them out of L2; so are those of more than 16384, which leave their sums to a pass over columns.
 //
 // Sums of squares are binary32; where one leaves its range (elements beyond 2^63 or so) the row's are formed once more from elements 2^-70 as large.
 #include <hip/hip_runtime.h>
@@ -478,7 +478,7 @@ __global__ __launch_bounds__(MOST) void norm_grad_kernel(const NormGradParams p)
     }
 }
 
-// ---- backward, rows of any length: first the rows (dr, dy, and what the sums need of a row), then strips of 512 columns
+// Rows that no thread keeps: eight elements of their operands at a time.
 template <bool YB, bool RB> struct LongRow {
     const NormGradParams& p;
     long long m, g;
@@ -508,6 +508,134 @@ template <bool YB, bool RB> struct LongRow {
         for (int i = 0; i < 8; ++i) f[i] = p.scale * f[i] * after[i];
     }
 };
+
+// ---- backward, rows of up to 16384 elements: 1024 threads with sixteen columns each.  Their sums over rows stay in registers and LDS, a row does not: it is read once
+// from HBM and, one workgroup a compute unit, twice more out of L2.
+template <bool YB, bool RB>
+__global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradParams p)
+{
+    constexpr int C = 2;
+    extern __shared__ __align__(16) unsigned char kept[];               // dafter's sums, and t
+    __shared__ v4f slot[2][16];
+    RowSums<false> sums(slot);
+    const float inv_d = 1.0f / (float)p.D;
+    auto after_sum = [&](int c, int half) -> v4f& { return reinterpret_cast<v4f*>(kept)[(c * 2 + half) * 1024 + threadIdx.x]; };
+    auto t_sum = [&](int c, int half) -> v4f& { return reinterpret_cast<v4f*>(kept)[(4 + c * 2 + half) * 1024 + threadIdx.x]; };
+    int k[C], left[C];
+    float sb[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        k[c] = (c * 1024 + (int)threadIdx.x) * 8;
+        left[c] = p.D - k[c];
+        after_sum(c, 0) = after_sum(c, 1) = t_sum(c, 0) = t_sum(c, 1) = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sb[c][i] = 0.0f;
+    }
+    const Share z = share_of(seldom(), blockIdx.x);
+    for (long long g = z.g0; g < z.g1; ++g) {
+        const long long begin = begin_of(seldom(), g, z.part), end = begin_of(seldom(), g, z.part + 1);
+        for (long long m = begin; m < end; ++m) {
+            const LongRow<YB, RB> w{p, m, g};
+            auto squares = [&](float by, float (&sum)[3]) {             // of s and y, and p s
+                sum[0] = sum[1] = sum[2] = 0.0f;
+#pragma unroll 1
+                for (int c = 0; c < C; ++c) {
+                    float s[8], dn[8], y[8], b[8];
+                    w.read((c * 1024 + (int)threadIdx.x) * 8, s, dn, y, b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float u = s[i] * by, v = y[i] * by;
+                        sum[0] = __builtin_fmaf(u, u, sum[0]);
+                        sum[1] = __builtin_fmaf(b[i] * dn[i], s[i], sum[1]);
+                        sum[2] = __builtin_fmaf(v, v, sum[2]);
+                    }
+                }
+                sums(sum);
+            };
+            float sum[3];
+            squares(1.0f, sum);
+            float s2 = unit_of(sum[0], inv_d, p.eps), s1 = p.after ? unit_of(sum[2], inv_d, p.eps) : 1.0f, mean = sum[1] * s2 * inv_d;
+            if (too_much(sum[0]) || too_much(fabsf(sum[1])) || (p.after && too_much(sum[2]))) {
+                float few[3], ph[1] = {0.0f};
+                squares(SOPK_FEWER, few);
+                if (too_much(sum[0])) s2 = unit_of_fewer(few[0], inv_d);
+                if (p.after && too_much(sum[2])) s1 = unit_of_fewer(few[2], inv_d);
+#pragma unroll 1
+                for (int c = 0; c < C; ++c) {
+                    float s[8], dn[8], y[8], b[8];
+                    w.read((c * 1024 + (int)threadIdx.x) * 8, s, dn, y, b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ph[0] = __builtin_fmaf(b[i] * dn[i], s[i] * s2, ph[0]);
+                }
+                sums(ph);
+                mean = ph[0] * inv_d;
+            }
+            float q[C][8], qx[1] = {0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float s[8], dn[8], y[8], b[8], f[8];
+                w.read(k[c], s, dn, y, b);
+                w.sum_grad(k[c], s, dn, b, s2, mean, q[c]);
+                put<RB>(reinterpret_cast<char*>(p.dr) + m * p.lddr * (RB ? 2 : 4), k[c], left[c], q[c]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sb[c][i] = __builtin_fmaf(dn[i], s[i] * s2, sb[c][i]);
+                if (!p.y) continue;
+                w.factors(k[c], f);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    v4f t = t_sum(c, half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t[i] = __builtin_fmaf(q[c][4 * half + i], y[4 * half + i] * s1, t[i]);
+                    t_sum(c, half) = t;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    q[c][i] *= f[i];
+                    qx[0] = __builtin_fmaf(q[c][i], y[i] * s1, qx[0]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!p.y) continue;
+            if (p.after) sums(qx);
+            const float c1 = qx[0] * inv_d;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (p.after) {
+                    const Raw<YB> y = ask<YB>(w.row(p.y, p.ldy, YB), k[c], left[c]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) q[c][i] = s1 * __builtin_fmaf(-at(y, i) * s1, c1, q[c][i]);
+                }
+                put<YB>(reinterpret_cast<char*>(p.dy) + m * p.lddy * (YB ? 2 : 4), k[c], left[c], q[c]);
+                if (p.q.codes) put_codes(p.q, p.e5m2, q[c], m, k[c], left[c]);
+            }
+        }
+        const NormGradParams& r = seldom();
+        if (r.dafter || r.dgate) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int kc[1] = {k[c]}, lc[1] = {left[c]};
+                const v4f lo = t_sum(c, 0), hi = t_sum(c, 1);
+                const float tc[1][8] = {{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
+                float da[1][8];
+                t_sum(c, 0) = t_sum(c, 1) = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                end_group<1>(blockIdx.x, g, kc, lc, tc, da);
+                if (r.parts > 1) continue;
+                after_sum(c, 0) += v4f{da[0][0], da[0][1], da[0][2], da[0][3]};
+                after_sum(c, 1) += v4f{da[0][4], da[0][5], da[0][6], da[0][7]};
+            }
+        }
+    }
+    const NormGradParams& r = seldom();
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const v4f a = after_sum(c, 0), b = after_sum(c, 1);
+        const float da[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        if (r.dafter && r.parts == 1) put<false>(r.part_a + (long long)blockIdx.x * r.D, k[c], left[c], da);
+        if (r.dbefore) put<false>(r.part_b + (long long)blockIdx.x * r.D, k[c], left[c], sb[c]);
+    }
+}
+
+// ---- backward, longer rows: first the rows (dr, dy, and what the sums need of a row), then strips of 512 columns
 template <bool YB, bool RB>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradParams p)
 {
@@ -715,6 +843,13 @@ template <bool YB, bool RB> static hipError_t norm_grad_shape_go(const NormGradP
     const sopr::RowShape s = sopr::norm_grad_shape(p.D);
     if (s.T == 64) return s.C == 1 ? norm_grad_go<true, 1, 256, YB, RB>(p, s.T, st) : norm_grad_go<true, 2, 256, YB, RB>(p, s.T, st);
     if (s.C == 1) return norm_grad_go<false, 1, 1024, YB, RB>(p, s.T, st);
+    if (s.T == 1024) {
+        auto fn = &norm_grad_wide_kernel<YB, RB>;
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(fn, dim3((unsigned)p.words), dim3(1024), 128 * 1024, st, p);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL((norm_grad_long_kernel<YB, RB>), dim3((unsigned)grid_of(p.M, 2 * n_cu)), dim3(1024), 0, st, p);
     if (p.dafter || p.dbefore || p.dgate) hipLaunchKernelGGL((norm_grad_columns_kernel<YB, RB>), dim3((unsigned)((p.D + 511) / 512), (unsigned)p.words), dim3(256), 0, st, p);
     return hipGetLastError();

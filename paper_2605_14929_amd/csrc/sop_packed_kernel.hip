@@ -90,10 +90,16 @@ __device__ __forceinline__ void store_y(const PackedMmParams& p, int m, int n, v
 }
 
 // ... as they are, or through the epilogue
-template <bool EPI> __device__ __forceinline__ void leave(const PackedMmParams& p, int m, int n, v4f v)
+template <bool EPI> __device__ __forceinline__ void leave(const PackedMmParams& p, int m, int n, v4f v, const EpilogueOperands& o)
 {
-    if constexpr (EPI) finish_four<true>(p, m, n, v, epilogue_operands<true>(p, m, n));
+    if constexpr (EPI) finish_four<true>(p, m, n, v, o);
     else store_y(p, m, n, v);
+}
+// what an epilogue reads for the first results of a wavefront, asked for before the steps along K
+template <bool EPI> __device__ __forceinline__ EpilogueOperands asked(const PackedMmParams& p, int m, int n, bool any)
+{
+    if constexpr (EPI) if (any) return epilogue_operands<true>(p, m, n);
+    return EpilogueOperands{};
 }
 
 // ---- few rows of x: FM x 16 of them by 16 columns a workgroup, K dealt out to its W wavefronts, 128 elements a step, U steps of a
@@ -109,6 +115,7 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
     __shared__ v4f part[W][FM][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, q = lane >> 4;
     const int n0 = blockIdx.x * 16, n = min(n0 + r16, p.N - 1), lg = 31 - __builtin_clz(p.g);
+    const EpilogueOperands first = asked<EPI>(p, wave * 16 + r16, n0 + 4 * q, wave < FM);
     const uint16_t* words = p.words + (long long)n * (p.K >> lg);
     const unsigned char* pay = p.payload + (long long)n * (p.K / 8) * NB;
     const uint16_t* xr[FM];
@@ -192,7 +199,7 @@ __global__ __launch_bounds__(W * 64) void packed_rows_kernel(const PackedMmParam
         v4f s = part[0][a][lane];
 #pragma unroll
         for (int i = 1; i < W; ++i) s += part[i][a][lane];
-        leave<EPI>(p, a * 16 + r16, n0 + 4 * q, s);
+        leave<EPI>(p, a * 16 + r16, n0 + 4 * q, s, a == wave ? first : asked<EPI>(p, a * 16 + r16, n0 + 4 * q, true));
     }
 }
 
@@ -211,6 +218,9 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
     int tm, tn;
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
     const int m0 = tm * (32 * FM), n0 = tn * (32 * FN), whole = p.K / (64 * S);
+    auto row = [&](int t) { return m0 + (t >> 2) / FN * 32 + 8 * (t & 3) + (lane >> 3); };
+    auto column = [&](int t) { return n0 + (t >> 2) % FN * 32 + 4 * (lane & 7); };
+    const EpilogueOperands first = asked<EPI>(p, row(wave), column(wave), wave < FM * FN * 4);
     unsigned char* own = lds + wave * OWN;
     const unsigned int own0 = lds_address(own);
     const Window xw = window(p.x + (long long)m0 * p.ldx, ((unsigned int)(min(32 * FM, p.M - m0) - 1) * (unsigned int)p.ldx + (unsigned int)p.K) * 2);
@@ -326,11 +336,11 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
         for (int b = 0; b < FN; ++b) put_square(reinterpret_cast<v4f*>(own) + (a * FN + b) * 256, lane, acc[a][b]);
     __syncthreads();
     for (int t = wave; t < FM * FN * 4; t += W) {                         // a quarter of a square
-        const int a = (t >> 2) / FN, b = (t >> 2) % FN, i = t & 3, at = (t >> 2) * 256 + quarter_slot(i, lane);
+        const int at = (t >> 2) * 256 + quarter_slot(t & 3, lane);
         v4f s = reinterpret_cast<const v4f*>(lds)[at];
 #pragma unroll
         for (int q = 1; q < W; ++q) s += reinterpret_cast<const v4f*>(lds + q * OWN)[at];
-        leave<EPI>(p, m0 + a * 32 + 8 * i + (lane >> 3), n0 + b * 32 + 4 * (lane & 7), s);
+        leave<EPI>(p, row(t), column(t), s, t == wave ? first : asked<EPI>(p, row(t), column(t), true));
     }
 }
 

@@ -167,7 +167,7 @@ def test_norm_gradients(lib):
                 assert words <= G and [w * G // words for w in range(words + 1)][-1] == G and all((w + 1) * G // words > w * G // words for w in range(words))
             assert words <= 2048 and (a, t, b) == (base, base, base + row)
             end = base + 2 * row
-            assert size == end - base + (12 * M if D > 8192 else 0) and (D <= 8192 or st == end)
+            assert size == end - base + (12 * M if D > 16384 else 0) and (D <= 16384 or st == end)
             joins = {int(s[1]): [int(v) for v in s[2:]] for s in said[1:]}
             assert joins[0][:3] == [1, words, a] and joins[1][:3] == [1, words, b] and (2 in joins) == (parts > 1)
             if parts > 1:
