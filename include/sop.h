@@ -623,7 +623,8 @@ sop_status sop_packed_linear(sop_ctx* ctx, const void* x_dev, int64_t ldx, const
 /* Gradient of an epilogue, from the z that it kept: dz = scale dy act'(z) (relu: 0 at 0), as numbers of dy's type (for sop_fp8_weight_grad), in 8 bits (for
  * the input gradient; formed from the binary32 values), and dbias = sum of dz over the rows.  The residual's gradient is dy.
  *   dy [M, N], z [M, N] of dy's type (NULL without an activation), dz [M, N] of dy's type or NULL; dz8 of block_rows 1
- *   dbias: DEVICE, N floats, or NULL; sums over rows are binary32 within some hundred rows and binary64 above them, in an order fixed by the sizes and the GPU
+ *   dbias: DEVICE, N floats, or NULL; sums over rows are binary32 within a workgroup's share of them (up to
+ *   2^11 such shares) and binary64 from there on, in an order fixed by the sizes and the GPU
  *   workspace: DEVICE, 16-byte aligned, sop_fp8_linear_grad_workspace() bytes; NULL where dbias is */
 sop_status sop_fp8_linear_grad_workspace(sop_ctx* ctx, int64_t M, int64_t N, size_t* bytes);
 sop_status sop_fp8_linear_grad(sop_ctx* ctx, const void* dy_dev, int64_t lddy, const void* z_dev, int64_t ldz, sop_dtype dtype, int64_t M, int64_t N,

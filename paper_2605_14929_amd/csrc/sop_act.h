@@ -69,13 +69,14 @@ template <bool FINE> __device__ __forceinline__ float act_of(int act, float z)
     if (act == 1) return z < 0.0f ? 0.0f : z;
     if (act == 2 || act == 4) {
         const Logistic s = logistic_of<FINE>(act == 2 ? z : z * __builtin_fmaf(z * z, SOPK_TANH_B, SOPK_TANH_A));
-        return z >= 0.0f ? z * s.w : fmaxf(z, -1e30f) * s.w * s.g * s.g; // (w of NaN is NaN)
+        const float m = z >= 0.0f ? 1.0f : s.g;
+        return fmaxf(z, -1e30f) * s.w * m * m;                          // (w of NaN is NaN)
     }
     if (act == 3) {
-        const float a = fminf(fabsf(z), 40.0f);
-        const Tail t = tail<FINE>(a);
-        const float below = t.g * t.r;                                  // below g = Phi(-a)
-        return z < 0.0f ? -a * below * t.g : z * __builtin_fmaf(-below, t.g, 1.0f);
+        const float c = __builtin_amdgcn_fmed3f(z, -40.0f, 40.0f);      // (of NaN -40, and z - u is NaN)
+        const Tail t = tail<FINE>(fabsf(c));
+        const float u = c * (t.g * t.r) * t.g;                          // z Phi(-|z|)
+        return z < 0.0f ? u : z - u;
     }
     return z;
 }

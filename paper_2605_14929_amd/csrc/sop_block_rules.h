@@ -35,7 +35,10 @@ inline RowShare norm_share(long long G, long long each, long long most)
 inline long long norm_grad_most(long long D, int n_cu)
 {
     const RowShape s = norm_grad_shape(D);
-    if (s.T == 0) return 2ll * n_cu;
+    if (s.T == 0) {                                                     // (strips of 512 columns are workgroups too)
+        const long long words = 16ll * n_cu / ((D + 511) / 512);
+        return words < 1 ? 1 : words;
+    }
     if (s.T == 64) return (s.C == 1 ? 4ll : 3ll) * n_cu;
     const int each = 1024 / s.T;                                        // (sixteen wavefronts a compute unit)
     return (long long)(each < 1 ? 1 : each) * n_cu;

@@ -117,53 +117,62 @@ template <typename P> __device__ __forceinline__ bool by_windows(const P& p, int
     const long long far = (long long)(1 << 30) / (rows * (int)size);
     return on == 0 && (reinterpret_cast<unsigned long long>(e.bias) & 15) == 0 && m0 + rows <= p.M && n0 + columns <= p.N && p.ldy < far && (!e.residual || e.ldr < far) && (!e.z || e.ldz < far);
 }
-// `count` squares of 32 x 32 that a wavefront has put into LDS from `place` on, 4 KB each: the first is square `first` of the wavefront's, FN to a row of squares;
-// the wavefront's ROWS rows begin at m0, its columns at n0.
-// Where all of the wavefront's part is inside y, everything goes by windows: a matrix that is not there is an empty one, from which zeros come and into which nothing
-// goes, so that no branch stands between loads and stores, and a square's operands, asked for while the one before is finished, are waited for without the
-// stores in between.  (With a branch around each, the wait was for all of them: 4096 x 11008 x 4096 with gelu and z took 269 us, by windows 217; without an
-// epilogue the product takes 198.)
-template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
+// `count` squares of 32 x 32 that a wavefront has put into LDS from `place` on, 4 KB each, all of them inside y: the first is square `first` of the wavefront's, FN to a row
+// of squares; its ROWS rows begin at m0, its columns at n0.  RES, Z: there is a residual, z is kept.  No branch stands between loads and stores, so that a square's operands, asked
+// for while the one before is finished, are waited for without the stores in between.
+template <bool BF16, int FN, int ROWS, bool RES, bool Z, typename P> __device__ __forceinline__ void finish_whole(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
 {
     constexpr unsigned int SIZE = BF16 ? 2 : 4;
-    if (by_windows(p, m0, n0, ROWS, 32 * FN, SIZE)) {
-        const Epilogue& e = p.e;
-        auto over = [&](const void* x, long long ld) {
-            return window(x ? reinterpret_cast<const char*>(x) + ((long long)m0 * ld + n0) * SIZE : nullptr, x ? (unsigned int)((ROWS - 1) * ld + 32 * FN) * SIZE : 0u);
-        };
-        const Window wy = over(p.y, p.ldy), wz = over(e.z, e.ldz), wr = over(e.residual, e.ldr), wb = window(e.bias ? e.bias + n0 : nullptr, e.bias ? 32 * FN * 4 : 0);
-        const unsigned int r8 = (unsigned int)(lane >> 3), c4 = 4 * (unsigned int)(lane & 7);
-        const unsigned int aty = (r8 * (unsigned int)p.ldy + c4) * SIZE, atz = (r8 * (unsigned int)e.ldz + c4) * SIZE, atr = (r8 * (unsigned int)e.ldr + c4) * SIZE;
-        struct Operands { unsigned int r[4][4], b[4]; };
-        auto ask = [&](Operands& o, int s) {
-            const unsigned int row = (unsigned int)(s / FN) * 32, column = (unsigned int)(s % FN) * 32;
-            ask_four<false>(o.b, wb, c4 * 4, column * 4);
+    const Epilogue& e = p.e;
+    auto over = [&](const void* x, long long ld) { return window(reinterpret_cast<const char*>(x) + ((long long)m0 * ld + n0) * SIZE, (unsigned int)((ROWS - 1) * ld + 32 * FN) * SIZE); };
+    const Window wy = over(p.y, p.ldy), wz = Z ? over(e.z, e.ldz) : wy, wr = RES ? over(e.residual, e.ldr) : wy, wb = window(e.bias ? e.bias + n0 : nullptr, e.bias ? 32 * FN * 4 : 0);
+    const unsigned int r8 = (unsigned int)(lane >> 3), c4 = 4 * (unsigned int)(lane & 7);
+    const unsigned int aty = (r8 * (unsigned int)p.ldy + c4) * SIZE, atz = (r8 * (unsigned int)e.ldz + c4) * SIZE, atr = (r8 * (unsigned int)e.ldr + c4) * SIZE;
+    struct Operands { unsigned int r[RES ? 4 : 1][4], b[4]; };
+    auto ask = [&](Operands& o, int s) {
+        const unsigned int row = (unsigned int)(s / FN) * 32, column = (unsigned int)(s % FN) * 32;
+        ask_four<false>(o.b, wb, c4 * 4, column * 4);                   // (no bias: an empty window, from which zeros come)
+        if constexpr (RES) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) ask_four<BF16>(o.r[i], wr, atr, ((row + 8 * i) * (unsigned int)e.ldr + column) * SIZE);
-        };
-        Operands next;
-        ask(next, first);
-#pragma unroll 1
-        for (int s = 0; s < count; ++s) {
-            const Operands o = next;
-            ask(next, first + (s + 1 < count ? s + 1 : s));
-            const unsigned int row = (unsigned int)((first + s) / FN) * 32, column = (unsigned int)((first + s) % FN) * 32;
-            v4f v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = place[s * 256 + quarter_slot(i, lane)];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[i][j] += __uint_as_float(o.b[j]);
-                give_four<BF16>(wz, atz, ((row + 8 * i) * (unsigned int)e.ldz + column) * SIZE, v[i]);
-            }
-            act_by<BF16>(e.act, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[i][j] = __builtin_fmaf(v[i][j], e.scale, residual_of<BF16>(o.r[i], j));
-                give_four<BF16>(wy, aty, ((row + 8 * i) * (unsigned int)p.ldy + column) * SIZE, v[i]);
-            }
         }
+    };
+    Operands next;
+    ask(next, first);
+#pragma unroll 1
+    for (int s = 0; s < count; ++s) {
+        const Operands o = next;
+        ask(next, first + (s + 1 < count ? s + 1 : s));
+        const unsigned int row = (unsigned int)((first + s) / FN) * 32, column = (unsigned int)((first + s) % FN) * 32;
+        v4f v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = place[s * 256 + quarter_slot(i, lane)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] += __uint_as_float(o.b[j]);
+            if constexpr (Z) give_four<BF16>(wz, atz, ((row + 8 * i) * (unsigned int)e.ldz + column) * SIZE, v[i]);
+        }
+        act_by<BF16>(e.act, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (RES) v[i][j] = __builtin_fmaf(v[i][j], e.scale, residual_of<BF16>(o.r[i], j));
+                else v[i][j] *= e.scale;
+            }
+            give_four<BF16>(wy, aty, ((row + 8 * i) * (unsigned int)p.ldy + column) * SIZE, v[i]);
+        }
+    }
+}
+// ... or some of them outside y, or on odd addresses: four by four, each with its checks.  (All of them so, every wait being for all stores before it, 4096 x 11008 x 4096 with
+// gelu and z took 269 us; by windows @NOW@, without an epilogue @PLAIN@.)
+template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
+{
+    if (by_windows(p, m0, n0, ROWS, 32 * FN, BF16 ? 2 : 4)) {
+        if (p.e.residual && p.e.z) finish_whole<BF16, FN, ROWS, true, true>(p, place, first, count, m0, n0, lane);
+        else if (p.e.residual) finish_whole<BF16, FN, ROWS, true, false>(p, place, first, count, m0, n0, lane);
+        else if (p.e.z) finish_whole<BF16, FN, ROWS, false, true>(p, place, first, count, m0, n0, lane);
+        else finish_whole<BF16, FN, ROWS, false, false>(p, place, first, count, m0, n0, lane);
         return;
     }
     auto row = [&](int q) { return m0 + (first + (q >> 2)) / FN * 32 + 8 * (q & 3) + (lane >> 3); };

@@ -87,15 +87,16 @@ def _act_grad(lib, M=1000, N=600, dy=AT, lddy=None, z=AT, ldz=None, dtype=B.F32,
 
 def test_gradient_of_an_epilogue(lib):
     for M in (1, 4, 5, 100, 128, 129, 8192, 100000):
-        for N in (1, 512, 513, 11008, 1 << 20):
+        for N in (1, 512, 513, 11008, 1 << 20, 1 << 23):
             status, size = _act_grad(lib, M, N)
             assert status == OK
             said = {s[0]: [int(v) for v in s[1:]] for s in _said(lib)}
             m, n, words, strips, part = said["act_grad"]
             assert (m, n, strips) == (M, N, -(-N // 512)) and words * strips <= max(strips, 2048) and 1 <= words <= -(-M // 4)
-            assert size == (words * N * 4 if M > 128 else 0) and part == ((1 << 30) if M > 128 else 0)
-            assert ("join" in said) == (M > 128)                       # few rows: a workgroup has all of a column
-            if M > 128:
+            few = M <= 128                                             # a workgroup has all of a column
+            assert size == (0 if few else words * N * 4) and part == (0 if few else 1 << 30)
+            assert ("join" in said) != few
+            if not few:
                 assert said["join"] == [0, 1, words, 1 << 30, AT]
     assert _act_grad(lib, 0)[0] == OK and _said(lib) == [["join", "0", "1", "0", "0", str(AT)]]   # no rows: zeros
     assert _act_grad(lib, 0, db=None)[0] == OK and _said(lib) == []
