@@ -101,12 +101,14 @@ template <bool BF16> __device__ __forceinline__ void ask_four(unsigned int (&r)[
         for (int i = 0; i < 4; ++i) r[i] = (unsigned int)v[i];
     }
 }
+// (A store of 16 bytes takes its data registers a moment after it has been issued.  Without a scalar offset the compiler keeps the next instruction from writing them that
+// soon; with one it does not, and the first of the four arrived as what came after it.  So the sum of both offsets is the lane's.)
 typedef unsigned int v2u __attribute__((ext_vector_type(2)));
 typedef unsigned int v4u __attribute__((ext_vector_type(4)));
 template <bool BF16> __device__ __forceinline__ void give_four(const Window& w, unsigned int at, unsigned int uni, v4f v)
 {
     if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b64(v2u{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, resource(w), (int)at, (int)uni, 0);
-    else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), resource(w), (int)at, (int)uni, 0);
+    else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), resource(w), (int)(at + uni), 0, 0);
 }
 // Whether the part of a matrix of `rows` x `columns` from (m0, n0) on can go by such windows: all of it there, fours on their own alignment, 32-bit offsets.
 template <typename P> __device__ __forceinline__ bool by_windows(const P& p, int m0, int n0, int rows, int columns, unsigned int size)

@@ -611,9 +611,9 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradPara
         }
         const NormGradParams& r = seldom();
         if (r.dafter || r.dgate) {
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < C; ++c) {
-                const int kc[1] = {k[c]}, lc[1] = {left[c]};
+                const int kc[1] = {(c * 1024 + (int)threadIdx.x) * 8}, lc[1] = {r.D - kc[0]};
                 const v4f lo = t_sum(c, 0), hi = t_sum(c, 1);
                 const float tc[1][8] = {{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
                 float da[1][8];
