@@ -611,7 +611,7 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradPara
         }
         const NormGradParams& r = seldom();
         if (r.dafter || r.dgate) {
-#pragma unroll 1
+#pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int kc[1] = {(c * 1024 + (int)threadIdx.x) * 8}, lc[1] = {r.D - kc[0]};
                 const v4f lo = t_sum(c, 0), hi = t_sum(c, 1);
@@ -759,58 +759,53 @@ __global__ __launch_bounds__(256) void norm_grad_columns_kernel(const NormGradPa
 __global__ __launch_bounds__(1024) void join_kernel(const JoinParams p)
 {
     __shared__ double part[32][33];
-    const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int col = threadIdx.x & 31, row = threadIdx.x >> 5, d = blockIdx.x * 32 + col;
     long long set = blockIdx.y;
     int j = 0;
     while (j < 2 && set >= p.sets[j]) { set -= p.sets[j]; ++j; }
-    const int rows = (int)p.rows[j];
+    const int rows = (int)p.rows[j], at = d < p.D ? d : p.D - 1;
+    const float* from = p.part[j] + set * rows * p.D + at;
     const bool weighted = j == 0 && p.gate;
+    auto weight = [&](int i) {
+        const long long k = (unsigned int)i / (unsigned int)p.share * p.ldg + at;
+        return (double)(p.gate_bf16 ? __uint_as_float((unsigned int)reinterpret_cast<const uint16_t*>(p.gate)[k] << 16) : reinterpret_cast<const float*>(p.gate)[k]);
+    };
+    double s = 0.0;
     const long long step = 32ll * p.D;
-    for (int first = (int)blockIdx.x * 32; first < p.D; first += (int)gridDim.x * 32) {
-        const int d = first + col, at = d < p.D ? d : p.D - 1;
-        auto weight = [&](int i) {
-            const long long k = (unsigned int)i / (unsigned int)p.share * p.ldg + at;
-            return (double)(p.gate_bf16 ? __uint_as_float((unsigned int)reinterpret_cast<const uint16_t*>(p.gate)[k] << 16) : reinterpret_cast<const float*>(p.gate)[k]);
-        };
-        const float* from = p.part[j] + set * rows * p.D + at;
-        const float* q = from + (long long)row * p.D;
-        double s = 0.0;
-        int i = row;
-        for (; i + 224 < rows; i += 256, q += 8 * step) {
-            float v[8];
+    const float* q = from + (long long)row * p.D;
+    int i = row;
+    for (; i + 224 < rows; i += 256, q += 8 * step) {
+        float v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = q[u * step];
-            if (weighted) {
+        for (int u = 0; u < 8; ++u) v[u] = q[u * step];
+        if (weighted) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) s = __builtin_fma((double)v[u], weight(i + 32 * u), s);
-            } else {
-                s += (((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3])) + (((double)v[4] + (double)v[5]) + ((double)v[6] + (double)v[7]));
-            }
+            for (int u = 0; u < 8; ++u) s = __builtin_fma((double)v[u], weight(i + 32 * u), s);
+        } else {
+            s += (((double)v[0] + (double)v[1]) + ((double)v[2] + (double)v[3])) + (((double)v[4] + (double)v[5]) + ((double)v[6] + (double)v[7]));
         }
-        if (i < rows) {                                                 // the last ones, asked for together too
-            float v[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = from[(long long)(i + 32 * u < rows ? i + 32 * u : rows - 1) * p.D];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const bool in = i + 32 * u < rows;
-                if (weighted) s = in ? __builtin_fma((double)v[u], weight(in ? i + 32 * u : i), s) : s;
-                else s += in ? (double)v[u] : 0.0;
-            }
-        }
-        part[row][col] = s;
-        __syncthreads();
-        if (row == 0 && d < p.D) {
-            s = 0.0;
-#pragma unroll
-            for (int u = 0; u < 32; ++u) s += part[u][col];
-            if (rows > 0 && j != 1) s *= (double)p.factor;              // (sums of no rows are zero, whatever the weights are)
-            if (rows > 0 && j == 2 && p.after) s *= (double)p.after[d];
-            if (p.out_bf16[j]) reinterpret_cast<uint16_t*>(p.out[j])[set * p.ldo[j] + d] = (uint16_t)bf16_bits((float)s);
-            else reinterpret_cast<float*>(p.out[j])[set * p.ldo[j] + d] = (float)s;
-        }
-        __syncthreads();
     }
+    if (i < rows) {                                                     // the last ones, asked for together too
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = from[(long long)(i + 32 * u < rows ? i + 32 * u : rows - 1) * p.D];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const bool in = i + 32 * u < rows;
+            if (weighted) s = in ? __builtin_fma((double)v[u], weight(in ? i + 32 * u : i), s) : s;
+            else s += in ? (double)v[u] : 0.0;
+        }
+    }
+    part[row][col] = s;
+    __syncthreads();
+    if (row != 0 || d >= p.D) return;
+    s = 0.0;
+#pragma unroll
+    for (int u = 0; u < 32; ++u) s += part[u][col];
+    if (rows > 0 && j != 1) s *= (double)p.factor;                      // (sums of no rows are zero, whatever the weights are)
+    if (rows > 0 && j == 2 && p.after) s *= (double)p.after[d];
+    if (p.out_bf16[j]) reinterpret_cast<uint16_t*>(p.out[j])[set * p.ldo[j] + d] = (uint16_t)bf16_bits((float)s);
+    else reinterpret_cast<float*>(p.out[j])[set * p.ldo[j] + d] = (float)s;
 }
 
 template <bool ONE, int C, int MOST, bool YB, bool RB> static hipError_t norm_go(const NormParams& p, int T, int n_cu, hipStream_t st)
@@ -877,7 +872,6 @@ extern "C" hipError_t sopk_norm_grad_launch(const NormGradParams* p, int y_bf16,
 extern "C" hipError_t sopk_join_launch(const JoinParams* p, void* stream)
 {
     const long long sets = p->sets[0] + p->sets[1] + p->sets[2];
-    const int strips = (p->D + 31) / 32, most = 1 << 16;               // (with 32768 sets at most, fewer than 2^32 threads along either dimension)
-    hipLaunchKernelGGL(sopk::join_kernel, dim3((unsigned)(strips < most ? strips : most), (unsigned)sets), dim3(1024), 0, (hipStream_t)stream, *p);
+    hipLaunchKernelGGL(sopk::join_kernel, dim3((unsigned)((p->D + 31) / 32), (unsigned)sets), dim3(1024), 0, (hipStream_t)stream, *p);   // (D at most 2^23)
     return hipGetLastError();
 }
