@@ -7,7 +7,7 @@
 //   gelu           z Phi(z), Phi the normal distribution.  Phi(-a) = phi(a) R(a), phi its density, R the Mills ratio, which is smooth: with t = 1 / (1 + 0.3 a),
 //                  R = t P(t), P of degree 7 fitted here to R in 64 bits at 400 Chebyshev nodes of a in [0, 14.5] for the least relative error (1.7e-7).
 //                  Slope Phi(z) + z phi(z): from -a, phi (R - a).
-// FINE: with the exponent h = a log2 e in two parts, so that the error of g is that of the hardware's 2^t.  Otherwise, for results that are rounded to bf16, without:
+// FINE: with the exponent h = a log2 e in two parts, so that the error of g is that of the hardware's 2^t.  Otherwise, for bf16 numbers, without:
 // 1.4 h 2^-24 of the value more.
 // Far out the arguments are clamped where the function has long been 0 or z: infinities give the limits, NaN stays.
 #ifndef SOP_ACT_H
@@ -93,11 +93,10 @@ template <bool FINE> __device__ __forceinline__ float act_slope(int act, float z
         return up ? dw : dw * s.g * s.g;
     }
     if (act == 3) {
-        const float a = fminf(fabsf(z), 40.0f);
+        const float b = fabsf(z), a = b > 40.0f ? 40.0f : b;            // (NaN stays)
         const Tail t = tail<FINE>(a);
-        const float down = t.g * __builtin_fmaf(-a, SOPK_PHI0, t.r);    // down g = Phi(-a) - a phi(a)
-        const float r = z < 0.0f ? d * down * t.g : d * __builtin_fmaf(-down, t.g, 1.0f);
-        return z != z ? z : r;
+        const float u = d * (t.g * __builtin_fmaf(-a, SOPK_PHI0, t.r)) * t.g;   // d (Phi(-a) - a phi(a))
+        return z < 0.0f ? u : d - u;
     }
     return d;
 }

@@ -19,19 +19,19 @@ template <bool BF16> __device__ __forceinline__ void slopes(int act, const Raw<B
     switch (act) {
     case 1:
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(1, at(z, i), d[i]);
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<!BF16>(1, at(z, i), d[i]);
         break;
     case 2:
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(2, at(z, i), d[i]);
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<!BF16>(2, at(z, i), d[i]);
         break;
     case 3:
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(3, at(z, i), d[i]);
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<!BF16>(3, at(z, i), d[i]);
         break;
     case 4:
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] = act_slope<true>(4, at(z, i), d[i]);
+        for (int i = 0; i < 8; ++i) d[i] = act_slope<!BF16>(4, at(z, i), d[i]);
     }
 }
 template <bool BF16> struct GradRow { Raw<BF16> d, z; };
