@@ -167,7 +167,8 @@ template <bool BF16, int FN, int ROWS, bool RES, bool Z, typename P> __device__ 
     }
 }
 // ... or some of them outside y, or on odd addresses: four by four, each with its checks.  (All of them so, every wait being for all stores before it, 4096 x 11008 x 4096 with
-// gelu and z took 269 us; by windows @NOW@, without an epilogue @PLAIN@.)
+// gelu and z took 269 us.  By windows 210; without an epilogue 179, with a bias 181, and a residual 204 (its 90 MB come in bursts, when all tiles end), with silu 195, with
+// gelu 205: the vector ALUs, eight wavefronts a compute unit doing nothing else.)
 template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
 {
     if (by_windows(p, m0, n0, ROWS, 32 * FN, BF16 ? 2 : 4)) {
