@@ -40,6 +40,7 @@ struct JoinParams {
     long long sets[3]; long long ldo[3]; int out_bf16[3];
     const float* after; float factor;
     const void* gate; long long ldg; int gate_bf16, share;             // gate null: weights of 1
+    int also;                                                     // out[0] comes of set 2, the only one, times factor and gate
     int D;
 };
 

@@ -239,6 +239,7 @@ extern "C" sop_status sop_residual_norm_grad(sop_ctx* c, const sop_residual_norm
     if (t->dbefore) one_sum(j, 1, p.part_b, words, 1, t->dbefore, 0, false);
     if (t->dgate && (M == 0 || shared)) one_sum(j, 2, p.part_t, M > 0 ? g.share.parts : 0, o->groups, t->dgate, t->ld_dgate, o->gate_dtype == SOP_BF16);
     if (shared && o->gate) { j.gate = o->gate; j.ldg = o->ld_gate; j.gate_bf16 = o->gate_dtype == SOP_BF16; j.share = g.share.parts; }
+    if (shared && t->dafter && t->dgate && o->groups == 1) { j.sets[0] = 0; j.also = 1; }
     j.factor = shared ? o->scale : 1.0f;                                // (whole groups: workgroups have put scale and gate on their sums)
     return launched(c, call, join(j, stream));
 }

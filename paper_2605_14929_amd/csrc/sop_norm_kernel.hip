@@ -759,7 +759,7 @@ __global__ __launch_bounds__(256) void norm_grad_columns_kernel(const NormGradPa
 }
 
 // ---- the rows of partial sums added up, in binary64, in a fixed order: 32 columns a workgroup, its 32 half-wavefronts share the rows.  Row i of the first set has the
-// weight of its gate's row, i / share.
+// weight of its gate's row, i / share.  A gate of one row: its own set's sum, weighted, is the first set's too.
 __global__ __launch_bounds__(1024) void join_kernel(const JoinParams p)
 {
     __shared__ double part[32][33];
@@ -806,6 +806,7 @@ __global__ __launch_bounds__(1024) void join_kernel(const JoinParams p)
     s = 0.0;
 #pragma unroll
     for (int u = 0; u < 32; ++u) s += part[u][col];
+    if (j == 2 && p.also) reinterpret_cast<float*>(p.out[0])[d] = (float)(s * (double)p.factor * weight(0));
     if (rows > 0 && j != 1) s *= (double)p.factor;                      // (sums of no rows are zero, whatever the weights are)
     if (rows > 0 && j == 2 && p.after) s *= (double)p.after[d];
     if (p.out_bf16[j]) reinterpret_cast<uint16_t*>(p.out[j])[set * p.ldo[j] + d] = (uint16_t)bf16_bits((float)s);
