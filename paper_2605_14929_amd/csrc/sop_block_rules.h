@@ -13,11 +13,12 @@ inline RowShape norm_shape(long long D)
     const int C = D <= 512 ? 1 : D <= 1024 ? 2 : D <= 2048 ? 1 : D <= 8192 ? 2 : 4;
     return D > 16384 ? RowShape{0, 0} : RowShape{threads_for(D, C), C};
 }
-// Backward, where a thread holds four times as much: eight elements up to 8192 (8192 x 4096 bf16 105 us, sixteen 108; 777 x 5024 fp32 32 and 34), then
+// Backward, where a thread holds four times as much: eight elements up to 8192 (8192 x 4096 bf16 105 us, sixteen 108; 777 x 5024 fp32 32 and 34; 8192 x 1024 fp32 49, sixteen a
+// wavefront's thread 58), then
 // sixteen of a row that it does not keep (4096 x 12288 bf16 224 us, by the way of still longer rows 330).
 inline RowShape norm_grad_shape(long long D)
 {
-    return D <= 1024 ? norm_shape(D) : D <= 8192 ? RowShape{threads_for(D, 1), 1} : D <= 16384 ? RowShape{1024, 2} : RowShape{0, 0};
+    return D <= 512 ? norm_shape(D) : D <= 8192 ? RowShape{threads_for(D, 1), 1} : D <= 16384 ? RowShape{1024, 2} : RowShape{0, 0};
 }
 
 // Rows in G groups of `each` (a group shares a row of the gate), to `words` workgroups: as many groups as there are workgroups and more are dealt out whole
@@ -39,9 +40,7 @@ inline long long norm_grad_most(long long D, int n_cu)
         const long long words = 16ll * n_cu / ((D + 511) / 512);
         return words < 1 ? 1 : words;
     }
-    if (s.T == 64) return (s.C == 1 ? 4ll : 3ll) * n_cu;
-    const int each = 1024 / s.T;                                        // (sixteen wavefronts a compute unit)
-    return (long long)(each < 1 ? 1 : each) * n_cu;
+    return (s.T < 256 ? 4ll : 1024ll / s.T) * n_cu;                     // (sixteen wavefronts a compute unit, but four workgroups at most)
 }
 
 // Rows of an activation's gradient to workgroups: strips of 512 columns times `words` shares of the rows, four rows each at least.

@@ -846,7 +846,7 @@ template <bool YB, bool RB> static hipError_t norm_shape_go(const NormParams& p,
 template <bool YB, bool RB> static hipError_t norm_grad_shape_go(const NormGradParams& p, int n_cu, hipStream_t st)
 {
     const sopr::RowShape s = sopr::norm_grad_shape(p.D);
-    if (s.T == 64) return s.C == 1 ? norm_grad_go<true, 1, 256, YB, RB>(p, s.T, st) : norm_grad_go<true, 2, 256, YB, RB>(p, s.T, st);
+    if (s.T == 64) return norm_grad_go<true, 1, 256, YB, RB>(p, s.T, st);
     if (s.C == 1) return norm_grad_go<false, 1, 1024, YB, RB>(p, s.T, st);
     if (s.T == 1024) {
         auto fn = &norm_grad_wide_kernel<YB, RB>;

@@ -51,13 +51,13 @@ def test_a_row_fits_the_threads_that_share_it(ask):
                 assert (T, C) == (0, 0)
                 continue
             assert T % 64 == 0 and 64 <= T <= most[C] and T * C * 8 >= D
-            assert (T == 64) == (D <= 1024)                            # a wavefront, four of them a workgroup
+            assert (T == 64) == (D <= (1024 if op == "norm" else 512))     # a wavefront, four of them a workgroup
 
 
 def test_every_shape_of_a_row_is_compared_at_some_width(ask):
     for op in ("norm", "grad"):
         got = ask(op, *[(D,) for D in G.WIDTHS])
-        assert {(T == 64, T == 0, C) for T, C in got} == {(True, False, 1), (True, False, 2), (False, False, 1), (False, False, 2), (False, True, 0)} | ({(False, False, 4)} if op == "norm" else set())
+        assert {(T == 64, T == 0, C) for T, C in got} == {(True, False, 1), (False, False, 1), (False, False, 2), (False, True, 0)} | ({(True, False, 2), (False, False, 4)} if op == "norm" else set())
         assert len({T for T, _ in got}) >= 8
 
 
