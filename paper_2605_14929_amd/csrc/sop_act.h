@@ -70,7 +70,7 @@ template <bool FINE> __device__ __forceinline__ float act_of(int act, float z)
     if (act == 2 || act == 4) {
         const Logistic s = logistic_of<FINE>(act == 2 ? z : z * __builtin_fmaf(z * z, SOPK_TANH_B, SOPK_TANH_A));
         const float m = z >= 0.0f ? 1.0f : s.g;
-        return fmaxf(z, -1e30f) * s.w * m * m;                          // (w of NaN is NaN)
+        return __builtin_amdgcn_fmed3f(z, -1e30f, __builtin_inff()) * s.w * m * m;   // (w of NaN is NaN)
     }
     if (act == 3) {
         const float c = __builtin_amdgcn_fmed3f(z, -40.0f, 40.0f);      // (of NaN -40, and z - u is NaN)

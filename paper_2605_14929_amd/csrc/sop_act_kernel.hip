@@ -2,7 +2,7 @@
 //
 // One pass, bound by HBM.  A wavefront takes a strip of 512 columns, eight a lane, and goes down its share of the rows, so that the sums of a column stay in
 // registers; the four wavefronts of a workgroup take rows by turns and join their sums in LDS, and workgroups leave a row of partial sums each, which a
-// second kernel adds up in a fixed order.  8192 x 11008 bf16 with gelu: 133 us and 5, 4.75 TB/s (relu as fast: bound by HBM; rows asked for ahead change nothing).  Few rows go without it: a workgroup takes 128 columns of all of them, 64 rows at a time.
+// second kernel adds up in a fixed order.  8192 x 11008 bf16 with gelu: 132 us and 5, 4.8 TB/s (relu as fast: bound by HBM; rows asked for ahead change nothing).  Few rows go without it: a workgroup takes 128 columns of all of them, 64 rows at a time.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -4,7 +4,7 @@
 // arguments, and the tensors in chunks of 8192 elements, which workgroups take in turn.  Squares are formed and added in binary64: exact squares, and nothing
 // overflows.  Each workgroup leaves one partial sum, and every workgroup of the second pass adds them all up for itself, in one order, so that no third
 // launch stands between.  The second pass goes through the tensors from their end, what the first has read last being in the last-level cache.
-// 1.08 G fp32 gradients into bf16: 722 us (6.0 TB/s) and 1236 (5.3); 9.4 M in their fp32 8.5 and 15.
+// 1.08 G fp32 gradients into bf16: 724 us (6.0 TB/s) and 1238 (5.2); 9.4 M in their fp32 8.6 and 15.
 #include <hip/hip_runtime.h>
 
 #include "sop_block.h"

@@ -1,5 +1,5 @@
 // Epilogue of a product: z = v + bias (kept where wanted), y = residual + scale act(z), all in binary32, each of z and y rounded once.  Results come by four
-// neighbouring columns of a row a lane; what an epilogue reads for the next four is on its way while these are finished.
+// neighbouring columns of a row a lane; what an epilogue reads is asked for ahead.
 #ifndef SOP_EPILOGUE_H
 #define SOP_EPILOGUE_H
 #include "sop_act.h"
@@ -117,41 +117,50 @@ template <typename P> __device__ __forceinline__ bool by_windows(const P& p, int
     const unsigned long long on = (reinterpret_cast<unsigned long long>(p.y) | (unsigned long long)p.ldy * size | (e.residual ? reinterpret_cast<unsigned long long>(e.residual) | (unsigned long long)e.ldr * size : 0) |
                                    (e.z ? reinterpret_cast<unsigned long long>(e.z) | (unsigned long long)e.ldz * size : 0)) & (4 * size - 1);
     const long long far = (long long)(1 << 30) / (rows * (int)size);
-    return on == 0 && (reinterpret_cast<unsigned long long>(e.bias) & 15) == 0 && m0 + rows <= p.M && n0 + columns <= p.N && p.ldy < far && (!e.residual || e.ldr < far) && (!e.z || e.ldz < far);
+    return on == 0 && m0 + rows <= p.M && n0 + columns <= p.N && p.ldy < far && (!e.residual || e.ldr < far) && (!e.z || e.ldz < far);
+}
+// The bias of a wavefront's 32 FN columns, in a place of its own in LDS: zeros where there is none
+template <int FN, typename P> __device__ __forceinline__ void put_bias(const P& p, float* to, int n0, int lane)
+{
+#pragma unroll
+    for (int c = 0; c < 32 * FN; c += 64) {
+        const int n = n0 + c + lane;
+        if (32 * FN - c >= 64 || lane < 32) to[c + lane] = p.e.bias && n < p.N ? p.e.bias[n] : 0.0f;
+    }
 }
 // `count` squares of 32 x 32 that a wavefront has put into LDS from `place` on, 4 KB each, all of them inside y: the first is square `first` of the wavefront's, FN to a row
-// of squares; its ROWS rows begin at m0, its columns at n0.  RES, Z: there is a residual, z is kept.  No branch stands between loads and stores, so that a square's operands, asked
-// for while the one before is finished, are waited for without the stores in between.
-template <bool BF16, int FN, int ROWS, bool RES, bool Z, typename P> __device__ __forceinline__ void finish_whole(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
+// of squares; its ROWS rows begin at m0, its columns at n0.  RES, Z: there is a residual, z is kept.  No branch stands between loads and stores, so that a square's residual, asked
+// for two squares ahead, is waited for without the stores in between.
+template <bool BF16, int FN, int ROWS, bool RES, bool Z, typename P> __device__ __forceinline__ void finish_whole(const P& p, const v4f* place, const float* bias, int first, int count, int m0, int n0, int lane)
 {
     constexpr unsigned int SIZE = BF16 ? 2 : 4;
     const Epilogue& e = p.e;
     auto over = [&](const void* x, long long ld) { return window(reinterpret_cast<const char*>(x) + ((long long)m0 * ld + n0) * SIZE, (unsigned int)((ROWS - 1) * ld + 32 * FN) * SIZE); };
-    const Window wy = over(p.y, p.ldy), wz = Z ? over(e.z, e.ldz) : wy, wr = RES ? over(e.residual, e.ldr) : wy, wb = window(e.bias ? e.bias + n0 : nullptr, e.bias ? 32 * FN * 4 : 0);
+    const Window wy = over(p.y, p.ldy), wz = Z ? over(e.z, e.ldz) : wy, wr = RES ? over(e.residual, e.ldr) : wy;
     const unsigned int r8 = (unsigned int)(lane >> 3), c4 = 4 * (unsigned int)(lane & 7);
     const unsigned int aty = (r8 * (unsigned int)p.ldy + c4) * SIZE, atz = (r8 * (unsigned int)e.ldz + c4) * SIZE, atr = (r8 * (unsigned int)e.ldr + c4) * SIZE;
-    struct Operands { unsigned int r[RES ? 4 : 1][4], b[4]; };
-    auto ask = [&](Operands& o, int s) {
-        const unsigned int row = (unsigned int)(s / FN) * 32, column = (unsigned int)(s % FN) * 32;
-        ask_four<false>(o.b, wb, c4 * 4, column * 4);                   // (no bias: an empty window, from which zeros come)
+    struct Residual { unsigned int r[RES ? 4 : 1][4]; };
+    auto ask = [&](Residual& o, int s) {
         if constexpr (RES) {
+            const unsigned int q = (unsigned int)(first + (s < count ? s : count - 1)), row = q / FN * 32, column = q % FN * 32;
 #pragma unroll
             for (int i = 0; i < 4; ++i) ask_four<BF16>(o.r[i], wr, atr, ((row + 8 * i) * (unsigned int)e.ldr + column) * SIZE);
         }
     };
-    Operands next;
-    ask(next, first);
+    Residual next, after;
+    ask(next, 0);
+    ask(after, 1);
 #pragma unroll 1
     for (int s = 0; s < count; ++s) {
-        const Operands o = next;
-        ask(next, first + (s + 1 < count ? s + 1 : s));
+        const Residual o = next;
+        next = after;
+        ask(after, s + 2);
         const unsigned int row = (unsigned int)((first + s) / FN) * 32, column = (unsigned int)((first + s) % FN) * 32;
+        const v4f b = *reinterpret_cast<const v4f*>(bias + column + c4);
         v4f v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[i] = place[s * 256 + quarter_slot(i, lane)];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[i][j] += __uint_as_float(o.b[j]);
+            v[i] = place[s * 256 + quarter_slot(i, lane)] + b;
             if constexpr (Z) give_four<BF16>(wz, atz, ((row + 8 * i) * (unsigned int)e.ldz + column) * SIZE, v[i]);
         }
         act_by<BF16>(e.act, v);
@@ -167,15 +176,15 @@ template <bool BF16, int FN, int ROWS, bool RES, bool Z, typename P> __device__ 
     }
 }
 // ... or some of them outside y, or on odd addresses: four by four, each with its checks.  (All of them so, every wait being for all stores before it, 4096 x 11008 x 4096 with
-// gelu and z took 269 us.  By windows 210; without an epilogue 179, with a bias 181, and a residual 204 (its 90 MB come in bursts, when all tiles end), with silu 195, with
+// gelu and z took 269 us.  By windows 210; without an epilogue 179, with a bias 180, and a residual 201 (its 90 MB come in bursts, when all tiles end), with silu 194, with
 // gelu 205: the vector ALUs, eight wavefronts a compute unit doing nothing else.)
-template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, int first, int count, int m0, int n0, int lane)
+template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, const float* bias, int first, int count, int m0, int n0, int lane)
 {
     if (by_windows(p, m0, n0, ROWS, 32 * FN, BF16 ? 2 : 4)) {
-        if (p.e.residual && p.e.z) finish_whole<BF16, FN, ROWS, true, true>(p, place, first, count, m0, n0, lane);
-        else if (p.e.residual) finish_whole<BF16, FN, ROWS, true, false>(p, place, first, count, m0, n0, lane);
-        else if (p.e.z) finish_whole<BF16, FN, ROWS, false, true>(p, place, first, count, m0, n0, lane);
-        else finish_whole<BF16, FN, ROWS, false, false>(p, place, first, count, m0, n0, lane);
+        if (p.e.residual && p.e.z) finish_whole<BF16, FN, ROWS, true, true>(p, place, bias, first, count, m0, n0, lane);
+        else if (p.e.residual) finish_whole<BF16, FN, ROWS, true, false>(p, place, bias, first, count, m0, n0, lane);
+        else if (p.e.z) finish_whole<BF16, FN, ROWS, false, true>(p, place, bias, first, count, m0, n0, lane);
+        else finish_whole<BF16, FN, ROWS, false, false>(p, place, bias, first, count, m0, n0, lane);
         return;
     }
     auto row = [&](int q) { return m0 + (first + (q >> 2)) / FN * 32 + 8 * (q & 3) + (lane >> 3); };

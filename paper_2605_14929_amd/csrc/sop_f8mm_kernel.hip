@@ -153,6 +153,8 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
     tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, group, tm, tn);
     const int m0 = tm * BM, n0 = tn * BN, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WC * (BM / WR), wn = wave % WC * (BN / WC);
+    float* bias = reinterpret_cast<float*>(lds + 2 * STAGE) + wave * (32 * FN);   // (with an epilogue)
+    if constexpr (EPI) put_bias<FN>(p, bias, n0 + wn, lane);
     const unsigned char* xb = p.x + (long long)m0 * p.ldx;
     const unsigned char* wb = p.w + (long long)n0 * p.ldw;
     const int KF = p.K >> 7, KB = (p.K + 127) >> 7;                     // whole steps, all steps
@@ -283,14 +285,16 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
     }
     __syncthreads();                                                    // (LDS is free for the results)
     if constexpr (EPI) {
-        // as many of the wavefront's squares at once as find room, so that the epilogue's code stands there once or twice, in a loop over quarters of them
+        // as many of the wavefront's squares at once as find room, and the epilogue's code once: it is fetched by the few wavefronts that run it
+        // (2048 x 11008 x 4096 packed takes 208 us with the code there once or twice, 252 with six copies, 196 without an epilogue)
         constexpr int SQUARES = FM * FN, ROOM = 2 * STAGE / (WR * WC) / 4096, PART = ROOM < SQUARES ? ROOM : SQUARES;
         v4f* place = reinterpret_cast<v4f*>(lds + wave * (PART * 4096));
-#pragma unroll
+#pragma unroll 1
         for (int first = 0; first < SQUARES; first += PART) {
 #pragma unroll
-            for (int s = first; s < first + PART && s < SQUARES; ++s) put_square(place + (s - first) * 256, lane, acc[s / FN][s % FN]);
-            finish_squares<!EXACT, FN, FM * 32>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
+            for (int s = 0; s < SQUARES; ++s)
+                if (first == s / PART * PART) put_square(place + (s % PART) * 256, lane, acc[s / FN][s % FN]);
+            finish_squares<!EXACT, FN, FM * 32>(p, place, bias, first, min(PART, SQUARES - first), m0 + wm, n0 + wn, lane);
         }
     } else {
         v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
@@ -525,7 +529,7 @@ __global__ __launch_bounds__(512) void f8mm_split_kernel(const F8MmParams p, int
 
 template <int BM, int BN, int WR, int WC, int XF, bool EXACT, bool EPI> static hipError_t tile_go(const F8MmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128;
+    const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN, bytes = 2 * (BM + BN) * 128 + (EPI ? WR * BN * 4 : 0);
     auto fn = &f8mm_tile_kernel<BM, BN, WR, WC, XF, EXACT, EPI>;
     if (bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);

@@ -11,9 +11,9 @@
 // backward pass's sums over rows, stay with them: a workgroup leaves one row of partial sums, and a second kernel adds those up in a fixed order.
 // Backward, rows of more than 8192 elements are read three times over instead, two of them out of L2; so are those of more than 16384, which leave their sums to a pass over columns.
 //
-// Measured, kernel times (a large copy moves 5.1 TB/s): forward 8192 x 8192, y bf16 and stream fp32, 147 us, 5.0 TB/s, one token of 4096 4.0 us; backward 8192 x 4096 bf16 with a
-// gate of one row 94 us, 4.8 TB/s with the partial sums, and 7 us to add those up (512 rows of 4096, twice); 777 x 5024 fp32 with three gates 25 and 7; 4096 x 12288 bf16 224 us in all.
-// Backward, the next row is asked for while one is worked on (8192 x 4096 105 us in all, without that 123).
+// Measured, kernel times (a large copy moves 5.1 TB/s): forward 8192 x 8192, y bf16 and stream fp32, 145 us, 5.1 TB/s, one token of 4096 4.1 us; backward 8192 x 4096 bf16 with a
+// gate of one row 95 us, 4.8 TB/s with the partial sums, and 6 us to add those up (512 rows of 4096, twice); 777 x 5024 fp32 with three gates 25 and 7; 4096 x 12288 bf16 224 us in all.
+// Backward, the next row is asked for while one is worked on (8192 x 4096 102 us in all, without that some 20 more).
 //
 // Sums of squares are binary32; where one leaves its range (elements beyond 2^63 or so) the row's are formed once more from elements 2^-70 as large.
 #include <hip/hip_runtime.h>

@@ -344,6 +344,9 @@ __global__ __launch_bounds__(512) void packed_split_kernel(const PackedMmParams 
     }
 }
 
+// The squares of 32 x 32 that a wavefront's epilogue finishes at once, in wide tiles; the bias stands behind them
+template <int E, int F> constexpr int wide_part(int bytes) { return bytes / 4 / 4096 < E * F ? bytes / 4 / 4096 : E * F; }
+
 // ---- wide tiles: 64 E x 64 F of y (4 x 4, 4 x 3, 2 x 2) by four wavefronts, each 32 E x 32 F of it; 64 elements along K a step,
 // two steps in LDS.  While sixteen elements are multiplied (E F matrix instructions), the next sixteen's operands are read, and between
 // two barriers (4 E F matrix instructions) every thread forms 16 F weights of the step after the next, eight by eight: behind each matrix
@@ -587,14 +590,18 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
     wait_loads();
     __syncthreads();                                                    // (LDS is free for the results)
     if constexpr (EPI) {
-        // as many of the wavefront's squares at once as find room, so that the epilogue's code stands there twice at most, in a loop over quarters of them
-        constexpr int SQUARES = E * F, ROOM = (TAB + 2 * STAGE) / 4 / 4096, PART = ROOM < SQUARES ? ROOM : SQUARES;
+        // as many of the wavefront's squares at once as find room, and the epilogue's code once: it is fetched by the few wavefronts that run it
+        // (2048 x 11008 x 4096 packed takes 208 us with the code there once or twice, 252 with six copies, 196 without an epilogue)
+        constexpr int SQUARES = E * F, PART = wide_part<E, F>(TAB + 2 * STAGE);
         v4f* place = reinterpret_cast<v4f*>(lds + wave * (PART * 4096));
-#pragma unroll
+        float* bias = reinterpret_cast<float*>(lds + 4 * PART * 4096) + wave * (32 * F);
+        put_bias<F>(p, bias, n0 + wn, lane);
+#pragma unroll 1
         for (int first = 0; first < SQUARES; first += PART) {
 #pragma unroll
-            for (int s = first; s < first + PART && s < SQUARES; ++s) put_square(place + (s - first) * 256, lane, acc[s / F][s % F]);
-            finish_squares<true, F, E * 32>(p, place, first, SQUARES - first < PART ? SQUARES - first : PART, m0 + wm, n0 + wn, lane);
+            for (int s = 0; s < SQUARES; ++s)
+                if (first == s / PART * PART) put_square(place + (s % PART) * 256, lane, acc[s / F][s % F]);
+            finish_squares<true, F, E * 32>(p, place, bias, first, min(PART, SQUARES - first), m0 + wm, n0 + wn, lane);
         }
     } else {
         v4f* place = reinterpret_cast<v4f*>(lds + wave * 4096);
@@ -626,8 +633,9 @@ template <int NB, int FM, int FN, int S, bool EPI> static hipError_t split_go(co
 }
 template <int NB, int E, int F, bool EPI> static hipError_t wide_go(const PackedMmParams& p, hipStream_t st)
 {
-    const int tm = (p.M + 64 * E - 1) / (64 * E), tn = (p.N + 64 * F - 1) / (64 * F), bytes = (16 << 2 * NB) + 2 * (64 * E + 64 * F) * 128;
-    static_assert((16 << 2 * NB) + 2 * (64 * E + 64 * F) * 128 <= 160 * 1024, "the tables and two steps fit into LDS");
+    constexpr int STEPS = (16 << 2 * NB) + 2 * (64 * E + 64 * F) * 128, SQUARES = 4 * wide_part<E, F>(STEPS) * 4096 + 512 * F, bytes = EPI && SQUARES > STEPS ? SQUARES : STEPS;
+    const int tm = (p.M + 64 * E - 1) / (64 * E), tn = (p.N + 64 * F - 1) / (64 * F);
+    static_assert(bytes <= 160 * 1024, "the tables and two steps fit into LDS");
     auto fn = p.g == 8 ? &packed_wide_kernel<NB, E, F, true, EPI> : &packed_wide_kernel<NB, E, F, false, EPI>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
