@@ -647,6 +647,56 @@ def test_clip_takes_elements_beyond_four_gigabytes():
     assert float(x[n - 1]) == 1.5 and float(x[5]) == 2 and float(x[1 << 31]) == 6 and int((x != 0).sum()) == 3
 
 
+# ---- rows far apart
+
+def _apart(buf, stride, *mats):
+    """Copies of matrices side by side in one buffer, their rows `stride` elements apart."""
+    wide, at, out = buf.view(-1, stride), 3, []
+    for x in mats:
+        v = wide[:x.shape[0], at:at + x.shape[1]]
+        v.copy_(x)
+        out.append(v)
+        at += x.shape[1] + 5
+    return out
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [100, 1000, 4096, 8200, 16392])
+def test_norms_of_rows_far_apart(D, t):
+    """Five rows 2^30 elements apart, beyond what 32 bits address, give the bits of rows that follow each other."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    new = lambda *z: torch.randn(z, generator=gen, device="cuda").to(_type(t))  # noqa: E731
+    buf = torch.empty(5 << 30, dtype=_type(t), device="cuda")
+    r, y, ds, dn, gate, w = new(5, D), new(5, D), new(5, D), new(5, D), new(5, D), new(D).float()
+    fr, fy, fds, fdn, fgate, out = _apart(buf, 1 << 30, r, y, ds, dn, gate, r)
+    near = ctx().residual_norm(r, y, after=w, gate=gate, scale=0.5, before=w, dtype=_type(t), fmt=sop.E4M3)
+    far = ctx().residual_norm(fr, fy, after=w, gate=fgate, scale=0.5, before=w, dtype=_type(t), fmt=sop.E4M3, out=out)
+    assert far[0] is out and torch.equal(near[0], out) and torch.equal(near[1], far[1])
+    assert torch.equal(near[2].codes, far[2].codes) and torch.equal(near[2].scales, far[2].scales)
+    g = ctx().residual_norm_grad(ds, dn, near[0], before=w, y=y, after=w, gate=gate, scale=0.5, fmt=sop.E5M2)
+    h = ctx().residual_norm_grad(fds, fdn, out, before=w, y=fy, after=w, gate=fgate, scale=0.5, fmt=sop.E5M2)
+    assert all(torch.equal(a, b) for a, b in ((g.dr, h.dr), (g.dy, h.dy), (g.dy8.codes, h.dy8.codes), (g.dbefore, h.dbefore), (g.dafter, h.dafter), (g.dgate, h.dgate)))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("M, N, K, apart", [(5, 300, 200, 30), (300, 1531, 300, 23), (2300, 4700, 150, 21)])
+def test_epilogue_of_rows_far_apart(M, N, K, apart, t):
+    """... and so do residual, y, z and dy of a product with an epilogue, where their offsets pass 32 bits."""
+    import torch
+    x, w, bias, z = _z_case(np.random.default_rng(11), M, N, K)
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    res, dy = (torch.randn((M, N), generator=gen, device="cuda").to(_type(t)) for _ in range(2))
+    fres, fy, fz, fdy = _apart(torch.empty(M << apart, dtype=_type(t), device="cuda"), 1 << apart, res, res, res, dy)
+    kw = dict(bias=_vec(bias), act=sop.GELU, scale=0.5, dtype=_type(t))
+    y, kept = ctx().fp8_linear(x, w, residual=res, keep=True, **kw)
+    assert torch.equal(y, ctx().fp8_linear(x, w, residual=fres, out=fy, **kw))
+    assert torch.equal(y, ctx().fp8_linear(x, w, residual=fres, out=fres, **kw))
+    fz.copy_(kept)
+    a, b = ctx().fp8_linear_grad(dy, kept, act=sop.GELU), ctx().fp8_linear_grad(fdy, fz, act=sop.GELU)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1].codes, b[1].codes) and torch.equal(a[2], b[2])
+
+
 # ---- all of it together
 
 def _block(cx, v, x, ds):
