@@ -1003,6 +1003,8 @@ class Context:
 
     def _matrix(self, x, shape, dt, what):
         """(address, row stride) of a matrix of numbers of one shape and sop_dtype."""
+        if shape[0] > 1 and x.shape == shape and x.is_contiguous() and self._dtypes.get(x.dtype) == dt and x.get_device() == self.device:
+            return x.data_ptr(), shape[1]                                   # (the usual one, sooner)
         xt, ld = self._numbers(x, what)
         if x.shape != shape:
             raise SopError(2, f"{what} must be {shape[0]} x {shape[1]}")
@@ -1055,13 +1057,15 @@ class Context:
 
     def _workspace(self, size, like, *sizes):
         """(address, bytes, what keeps it) of what a call named by its _workspace entry point needs."""
-        import torch
         n = C.c_size_t()
-        _check(size(self._h, *sizes, C.byref(n)), self._h)
-        if n.value == 0:
+        st = size(self._h, *sizes, C.byref(n))
+        if st:
+            _check(st, self._h)
+        n = n.value
+        if n == 0:
             return None, 0, None
-        ws = torch.empty(n.value, dtype=torch.uint8, device=like.device)
-        return ws.data_ptr(), n.value, ws
+        ws = like.new_empty((n + 3) // 4, dtype=self._f32)
+        return ws.data_ptr(), n, ws
 
     def fp8_linear_grad(self, dy, z=None, act=None, scale: float = 1.0, bias: bool = True, fmt=E5M2, stream=None):
         """sop_fp8_linear_grad: (dz, dz8, dbias) of the epilogue act / scale from dy [M, N] and the z that fp8_linear kept: numbers of dy's type (for fp8_weight_grad; dy
@@ -1139,29 +1143,28 @@ class Context:
         o = self._norm_opts(M, D, after, gate, scale, before, eps)
         of_y = y if y is not None else dn
         dty = dt if of_y is None else self._numbers(of_y, "y or dn")[0]
-        t = _NormGrads(r_dtype=dt, y_dtype=dty)
+        dsp = sp = dnp = yp = dyp = None
+        lds = ls = ldn = ldy = 0
         if ds is not None:
-            t.ds, t.ld_ds = self._matrix(ds, shape, dt, "ds")
+            dsp, lds = self._matrix(ds, shape, dt, "ds")
         if before is not None:
-            t.s, t.ld_s = self._matrix(s, shape, dt, "s")
-            t.dn, t.ld_dn = self._matrix(dn, shape, dty, "dn")
-        dr, dy, dy8 = like.new_empty(shape), None, None
-        t.dr, t.ld_dr = dr.data_ptr(), D
+            sp, ls = self._matrix(s, shape, dt, "s")
+            dnp, ldn = self._matrix(dn, shape, dty, "dn")
+        dr, dy, dy8, m8 = like.new_empty(shape), None, None, None
         if y is not None:
-            t.y, t.ld_y = self._matrix(y, shape, dty, "y")
+            yp, ldy = self._matrix(y, shape, dty, "y")
             dy = y.new_empty(shape)
-            t.dy, t.ld_dy = dy.data_ptr(), D
+            dyp = dy.data_ptr()
             if fmt is not None:
                 dy8 = Fp8Blocks.empty(M, D, fmt, like.device)
-                t.dy8 = C.pointer(dy8._m)
+                m8 = C.pointer(dy8._m)
         elif fmt is not None:
             raise SopError(1, "without y there is no dy8")
         db = None if before is None else before.new_empty(D)
         da = None if after is None else after.new_empty(D)
         dg = None if gate is None else gate.new_empty(gate.shape)
-        t.dbefore, t.dafter = None if db is None else db.data_ptr(), None if da is None else da.data_ptr()
-        if dg is not None:
-            t.dgate, t.ld_dgate = dg.data_ptr(), D
+        t = _NormGrads(dsp, lds, dnp, ldn, sp, ls, yp, ldy, dr.data_ptr(), D, dyp, D, m8, None if db is None else db.data_ptr(),
+                       None if da is None else da.data_ptr(), None if dg is None else dg.data_ptr(), D, dt, dty)
         at, size, ws = self._workspace(self._lib.sop_residual_norm_grad_workspace, like, M, D, o.groups)
         st = self._lib.sop_residual_norm_grad(self._h, o, M, D, t, at, size, self._raw_stream(self.device))
         if st:
