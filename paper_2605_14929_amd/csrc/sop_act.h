@@ -1,6 +1,7 @@
 // Activations and their slopes in binary32, over all of its range: 0 none, 1 relu, 2 silu, 3 gelu, 4 gelu by tanh (SOP_ACT_*).
 //
 // exp(-a), a >= 0, is kept as its root g = exp(-a / 2): what is small because of it leaves binary32's normal numbers only in the last step, a second multiplication by g.
+// What grows (z, the inner derivative) meets the first g before it meets anything else, so that nothing overflows beside a result that does not.
 //   logistic(u)    w = 1 / (1 + exp(-|u|)); u >= 0: w, else w exp(-|u|)
 //   silu           z logistic(z);             slope s + z s (1 - s)
 //   gelu by tanh   z logistic(2 v), v = sqrt(2 / pi) (z + 0.044715 z^3): (1 + tanh v) / 2 = logistic(2 v)
@@ -89,8 +90,8 @@ template <bool FINE> __device__ __forceinline__ float act_slope(int act, float z
         const Logistic s = logistic_of<FINE>(act == 2 ? c : c * __builtin_fmaf(q, SOPK_TANH_B, SOPK_TANH_A));
         const float inner = act == 2 ? c : c * __builtin_fmaf(q, 3.0f * SOPK_TANH_B, SOPK_TANH_A);
         const bool up = z >= 0.0f;
-        const float dw = d * s.w * __builtin_fmaf(inner, up ? s.g * s.g * s.w : s.w, 1.0f);
-        return up ? dw : dw * s.g * s.g;
+        const float m = up ? 1.0f : s.g;
+        return m * __builtin_fmaf(inner, up ? s.g * s.g * s.w : s.w, 1.0f) * (d * s.w) * m;   // (m (1 + inner w) is at most 1.3 whatever z is)
     }
     if (act == 3) {
         const float b = fabsf(z), a = b > 40.0f ? 40.0f : b;            // (NaN stays)
