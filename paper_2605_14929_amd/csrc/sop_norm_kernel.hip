@@ -15,7 +15,8 @@
 // gate of one row 95 us, 4.8 TB/s with the partial sums, and 6 us to add those up (512 rows of 4096, twice); 777 x 5024 fp32 with three gates 25 and 7; 4096 x 12288 bf16 224 us in all.
 // Backward, the next row is asked for while one is worked on (8192 x 4096 102 us in all, without that some 20 more).
 //
-// Sums of squares are binary32; where one leaves its range (elements beyond 2^63 or so) the row's are formed once more from elements 2^-70 as large.
+// Sums of squares are binary32; where one leaves its range (elements beyond 2^51 to 2^61, by how many there are) the row's are formed once more from elements 2^-96 as large: 2^20 of the
+// largest, 2^128, then add up to 2^84, and the smallest sum that is formed again, 2^20 elements of 2^51, to 2^-69.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -73,9 +74,10 @@ template <bool ONE> struct RowSums {
 };
 // 1 / sqrt(mean + eps) of a row whose sum of squares is `sum`; where that is beyond SOPK_MUCH, what `again` says: the sum of squares of elements times FEWER
 #define SOPK_MUCH 1e37f
-#define SOPK_FEWER 8.470329473e-22f                                     // 2^-70
+#define SOPK_FEWER 1.262177448e-29f                                     // 2^-96
 __device__ __forceinline__ bool too_much(float sum) { return !(sum <= SOPK_MUCH); }
 __device__ __forceinline__ float unit_of(float sum, float inv_d, float eps) { return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_d, eps)); }
+// (beyond an rms of 2^126 it is no normal number, and known to 2^-150)
 __device__ __forceinline__ float unit_of_fewer(float sum, float inv_d) { return __builtin_amdgcn_rsqf(sum * inv_d) * SOPK_FEWER; }
 
 // ---- forward, a row in registers

@@ -6,7 +6,7 @@ import pytest
 import paper_2605_14929_amd as sop
 from oracle import block as OB
 from gpu_util import ctx
-from test_gpu_block import ACT, U, _near_codes_within, _slope_error, _t, _to
+from test_gpu_block import ACT, U, _forward_errors, _grad_errors, _near_codes_within, _norm_case, _slope_error, _t, _to, _vec
 from test_gpu_block import _close as _near, _np
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +39,50 @@ def test_large_gradients_under_any_slope(name, dtype, M):
         _close(dz, want, err, dtype)
         _near_codes_within(dz8, want, "E5M2", err)
         _close(db, want[at], err[at] + 2 * U * np.abs(want[at]), "f32")
+
+
+def _large_rows(rng, M, D):
+    """Rows of one size each, from where their squares leave binary32 to where they all but do themselves; the last has a single such element."""
+    x = np.where(rng.random((M, D)) < 0.5, -1.0, 1.0) * rng.uniform(0.5, 1, (M, D)) * np.resize([1e19, 2e18, 1e25, 1e36, 2e37, 1e38, BIG, BIG], M)[:, None]
+    x[M - 2] = np.where(x[M - 2] < 0, -BIG, BIG)
+    x[M - 1, : D - 1] *= 1e-25
+    return x.astype(np.float32)
+
+
+def _of_unit(unit):
+    """What 1 / rms is rounded by where it is no normal number (rms beyond 2^126), of itself: half of 2^-149."""
+    return 2.0 ** -150 / unit
+
+
+@pytest.mark.parametrize("D", [96, 1000, 4096, 8192, 8200, 16384, 20000, 1 << 20])
+def test_norm_of_rows_of_large_numbers(D):
+    """x after and before h are of size 1 however large the row is."""
+    import torch
+    rng = np.random.default_rng(21)
+    c = _norm_case(rng, 8, D, "f32", "f32", 0, True, True, scale=0.25)
+    c["y"] = _large_rows(rng, 8, D)
+    want, es, wn, en = _forward_errors(c)
+    u = _of_unit(OB.unit(c["y"].astype(np.float64), c["eps"]))
+    s, n, n8 = ctx().residual_norm(_t(c["r"]), _t(c["y"]), after=_vec(c["after"]), scale=c["scale"], before=_vec(c["before"]), dtype=torch.float32, fmt=sop.E4M3)
+    _close(s, want, es + u * np.abs(want - c["r"]), "f32")
+    c["r"], c["y"], c["after"] = c["y"], None, None
+    want, es, wn, en = _forward_errors(c)
+    s, n, n8 = ctx().residual_norm(_t(c["r"]), before=_vec(c["before"]), dtype=torch.float32, fmt=sop.E4M3)
+    en = en + u * np.abs(wn)
+    _close(n, wn, en, "f32")
+    _near_codes_within(n8, wn, "E4M3", en)
+
+
+@pytest.mark.parametrize("D", [96, 1000, 4096, 8192, 8200, 16384, 20000])
+def test_norm_gradients_of_rows_of_large_numbers(D):
+    """... and so the weights' gradients are; those of the rows themselves vanish.  Errors are those of rows of any size, whose k is 60 U at least, and twice a rounding of 1 / rms (4.3 U)
+    more: a quarter of them covers that."""
+    rng = np.random.default_rng(22)
+    for what in ("s", "y"):
+        c = _norm_case(rng, 8, D, "f32", "f32", 2, True, True)
+        c["r" if what == "s" else "y"] = _large_rows(rng, 8, D)
+        ds, dn = (rng.standard_normal((8, D)).astype(np.float32) for _ in range(2))
+        want, err = _grad_errors(c, ds, dn, c["r"])
+        got = ctx().residual_norm_grad(_t(ds), _t(dn), _t(c["r"]), before=_vec(c["before"]), y=_t(c["y"]), after=_vec(c["after"]), gate=_t(c["gate"]), scale=c["scale"], fmt=sop.E5M2)
+        for k in ("dr", "dy", "dbefore", "dafter", "dgate"):
+            _close(getattr(got, k), want[k], 1.25 * err[k], "f32")
