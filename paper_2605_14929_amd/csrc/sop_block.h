@@ -3,13 +3,15 @@
 #define SOP_BLOCK_H
 #include "sop_linear.h"
 
+#define SOPK_FEWER 1.262177448e-29f                                     // 2^-96: what elements are multiplied by whose squares' sum leaves binary32
+
 /* s = r + scale gate after y / rms(y), n = before s / rms(s) */
 struct NormParams {
     const void* y; long long ldy;            // null: s = r
     const void* r; long long ldr;
     const float* after; const float* before; // null: no such norm
     const void* gate; long long ldg; int gate_bf16; long long per_group;   // row m takes row m / per_group
-    float scale, eps;
+    float scale, eps, eps_fewer;             // eps_fewer: eps SOPK_FEWER^2
     long long M; int D;
     void* out; long long ldo;                // of r's type, null: not written
     void* n; long long ldn; int n_bf16;
@@ -23,7 +25,7 @@ struct NormGradParams {
     const void* y; long long ldy;            // null: no dy
     const float* after; const float* before;
     const void* gate; long long ldg; int gate_bf16; long long groups, per_group;
-    float scale, eps;
+    float scale, eps, eps_fewer;             // eps_fewer: eps SOPK_FEWER^2
     long long M; int D;
     void* dr; long long lddr;
     void* dy; long long lddy;

@@ -157,7 +157,7 @@ extern "C" sop_status sop_residual_norm(sop_ctx* c, const sop_residual_norm_opts
     std::memset(&p, 0, sizeof(p));
     p.y = y; p.ldy = ld_y; p.r = r; p.ldr = ld_r; p.after = o->after; p.before = o->before;
     p.gate = o->gate; p.ldg = o->ld_gate; p.gate_bf16 = o->gate && o->gate_dtype == SOP_BF16; p.per_group = o->gate ? M / o->groups : M;
-    p.scale = o->scale; p.eps = o->eps; p.M = M; p.D = (int)D;
+    p.scale = o->scale; p.eps = o->eps; p.eps_fewer = o->eps * SOPK_FEWER * SOPK_FEWER; p.M = M; p.D = (int)D;
     p.out = s; p.ldo = ld_s; p.n = n; p.ldn = ld_n; p.n_bf16 = n && n_dtype == SOP_BF16;
     if (n8) { p.q = out_of(n8); p.e5m2 = n8->format == SOP_E5M2; }
     OnDevice on(sopc::device(c));
@@ -220,7 +220,7 @@ extern "C" sop_status sop_residual_norm_grad(sop_ctx* c, const sop_residual_norm
     if (M > 0) {
         p.ds = t->ds; p.ldds = t->ld_ds; p.dn = t->dn; p.lddn = t->ld_dn; p.s = t->s; p.lds = t->ld_s; p.y = t->y; p.ldy = t->ld_y;
         p.after = o->after; p.before = o->before; p.gate = o->gate; p.ldg = o->ld_gate; p.gate_bf16 = o->gate && o->gate_dtype == SOP_BF16;
-        p.groups = g.groups; p.per_group = g.each; p.scale = o->scale; p.eps = o->eps; p.M = M; p.D = (int)D;
+        p.groups = g.groups; p.per_group = g.each; p.scale = o->scale; p.eps = o->eps; p.eps_fewer = o->eps * SOPK_FEWER * SOPK_FEWER; p.M = M; p.D = (int)D;
         p.dr = t->dr; p.lddr = t->ld_dr; p.dy = t->dy; p.lddy = t->ld_dy;
         if (t->dy8) { p.q = out_of(t->dy8); p.e5m2 = t->dy8->format == SOP_E5M2; }
         p.dafter = t->dafter; p.dbefore = t->dbefore; p.dgate = t->dgate; p.lddg = t->ld_dgate;

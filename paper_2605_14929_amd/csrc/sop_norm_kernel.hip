@@ -72,13 +72,12 @@ template <bool ONE> struct RowSums {
         }
     }
 };
-// 1 / sqrt(mean + eps) of a row whose sum of squares is `sum`; where that is beyond SOPK_MUCH, what `again` says: the sum of squares of elements times FEWER
+// 1 / sqrt(mean + eps) of a row whose sum of squares is `sum`; where that is beyond SOPK_MUCH, that of elements times SOPK_FEWER instead, and eps times its square
 #define SOPK_MUCH 1e37f
-#define SOPK_FEWER 1.262177448e-29f                                     // 2^-96
 __device__ __forceinline__ bool too_much(float sum) { return !(sum <= SOPK_MUCH); }
 __device__ __forceinline__ float unit_of(float sum, float inv_d, float eps) { return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_d, eps)); }
 // (beyond an rms of 2^126 it is no normal number, and known to 2^-150)
-__device__ __forceinline__ float unit_of_fewer(float sum, float inv_d) { return __builtin_amdgcn_rsqf(sum * inv_d) * SOPK_FEWER; }
+__device__ __forceinline__ float unit_of_fewer(float sum, float inv_d, float eps_fewer) { return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_d, eps_fewer)) * SOPK_FEWER; }
 
 // ---- forward, a row in registers
 template <bool ONE, int C, int MOST, bool YB, bool RB>
@@ -140,7 +139,7 @@ __global__ __launch_bounds__(MOST) void norm_kernel(const NormParams p, long lon
 #pragma unroll
                         for (int i = 0; i < 8; ++i) { const float z = at(y[c], i) * SOPK_FEWER; sum[0] = __builtin_fmaf(z, z, sum[0]); }
                     sums(sum);
-                    s1 = unit_of_fewer(sum[0], inv_d);
+                    s1 = unit_of_fewer(sum[0], inv_d, p.eps_fewer);
                 }
             }
             char* out = reinterpret_cast<char*>(p.out) + m * p.ldo * (RB ? 2 : 4);
@@ -171,7 +170,7 @@ __global__ __launch_bounds__(MOST) void norm_kernel(const NormParams p, long lon
 #pragma unroll
                 for (int i = 0; i < 8; ++i) { const float z = s[c][i] * SOPK_FEWER; sum[0] = __builtin_fmaf(z, z, sum[0]); }
             sums(sum);
-            s2 = unit_of_fewer(sum[0], inv_d);
+            s2 = unit_of_fewer(sum[0], inv_d, p.eps_fewer);
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -226,7 +225,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
         };
         auto unit = [&](bool of_y) {
             const float sum = squares(of_y, 1.0f);
-            return too_much(sum) ? unit_of_fewer(squares(of_y, SOPK_FEWER), inv_d) : unit_of(sum, inv_d, p.eps);
+            return too_much(sum) ? unit_of_fewer(squares(of_y, SOPK_FEWER), inv_d, p.eps_fewer) : unit_of(sum, inv_d, p.eps);
         };
         if (p.y && p.after) s1 = unit(true);
         if (p.before) s2 = unit(false);
@@ -400,8 +399,8 @@ __global__ __launch_bounds__(MOST) void norm_grad_kernel(const NormGradParams p)
                         few[1] = __builtin_fmaf(y, y, few[1]);
                     }
                 sums(few);
-                if (too_much(sum[0])) s2 = unit_of_fewer(few[0], inv_d);
-                if (p.after && too_much(sum[2])) s1 = unit_of_fewer(few[1], inv_d);
+                if (too_much(sum[0])) s2 = unit_of_fewer(few[0], inv_d, p.eps_fewer);
+                if (p.after && too_much(sum[2])) s1 = unit_of_fewer(few[1], inv_d, p.eps_fewer);
                 float ph[1] = {0.0f};
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
@@ -564,8 +563,8 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradPara
             if (too_much(sum[0]) || too_much(fabsf(sum[1])) || (p.after && too_much(sum[2]))) {
                 float few[3], ph[1] = {0.0f};
                 squares(SOPK_FEWER, few);
-                if (too_much(sum[0])) s2 = unit_of_fewer(few[0], inv_d);
-                if (p.after && too_much(sum[2])) s1 = unit_of_fewer(few[2], inv_d);
+                if (too_much(sum[0])) s2 = unit_of_fewer(few[0], inv_d, p.eps_fewer);
+                if (p.after && too_much(sum[2])) s1 = unit_of_fewer(few[2], inv_d, p.eps_fewer);
 #pragma unroll 1
                 for (int c = 0; c < C; ++c) {
                     float s[8], dn[8], y[8], b[8];
@@ -668,8 +667,8 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradPara
         float s2 = unit_of(sq[0], inv_d, p.eps), s1 = p.after ? unit_of(sq[1], inv_d, p.eps) : 1.0f;
         if (too_much(sq[0]) || (p.after && too_much(sq[1]))) {
             const v2f few = squares(SOPK_FEWER);
-            if (too_much(sq[0])) s2 = unit_of_fewer(few[0], inv_d);
-            if (p.after && too_much(sq[1])) s1 = unit_of_fewer(few[1], inv_d);
+            if (too_much(sq[0])) s2 = unit_of_fewer(few[0], inv_d, p.eps_fewer);
+            if (p.after && too_much(sq[1])) s1 = unit_of_fewer(few[1], inv_d, p.eps_fewer);
         }
         float sum[1] = {0.0f};
         if (p.before) {

@@ -86,3 +86,20 @@ def test_norm_gradients_of_rows_of_large_numbers(D):
         got = ctx().residual_norm_grad(_t(ds), _t(dn), _t(c["r"]), before=_vec(c["before"]), y=_t(c["y"]), after=_vec(c["after"]), gate=_t(c["gate"]), scale=c["scale"], fmt=sop.E5M2)
         for k in ("dr", "dy", "dbefore", "dafter", "dgate"):
             _close(getattr(got, k), want[k], 1.25 * err[k], "f32")
+
+
+@pytest.mark.parametrize("D", [96, 4096, 12000, 20000])
+def test_norm_under_a_large_eps(D):
+    """eps beside a sum of squares that leaves binary32."""
+    import torch
+    rng = np.random.default_rng(23)
+    c = _norm_case(rng, 4, D, "f32", "f32", 0, False, True)
+    c.update(r=(1e18 * rng.standard_normal((4, D))).astype(np.float32), y=None, eps=float(np.float32(3e36)))
+    c["r"][1:] *= np.float32(10)
+    want, es, wn, en = _forward_errors(c)
+    _close(ctx().residual_norm(_t(c["r"]), before=_vec(c["before"]), dtype=torch.float32, eps=c["eps"])[1], wn, en, "f32")
+    dn = rng.standard_normal((4, D)).astype(np.float32)
+    want, err = _grad_errors(c, None, dn, c["r"])
+    got = ctx().residual_norm_grad(None, _t(dn), _t(c["r"]), before=_vec(c["before"]), eps=c["eps"])
+    _close(got.dr, want["dr"], err["dr"], "f32")
+    _close(got.dbefore, want["dbefore"], err["dbefore"], "f32")
