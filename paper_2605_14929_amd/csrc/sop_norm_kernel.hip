@@ -17,6 +17,7 @@
 //
 // Sums of squares are binary32; where one leaves its range (elements beyond 2^51 to 2^61, by how many there are) the row's are formed once more from elements 2^-96 as large: 2^20 of the
 // largest, 2^128, then add up to 2^84, and the smallest sum that is formed again, 2^20 elements of 2^51, to 2^-69.
+// The means of p h and q x are no larger than what they are means of: a thread's part of the sum is divided by D before the parts meet.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -386,8 +387,9 @@ __global__ __launch_bounds__(MOST) void norm_grad_kernel(const NormGradParams p)
                     sum[2] = __builtin_fmaf(y, y, sum[2]);
                 }
             }
+            sum[1] *= inv_d;
             sums(sum);
-            float s2 = unit_of(sum[0], inv_d, p.eps), s1 = p.after ? unit_of(sum[2], inv_d, p.eps) : 1.0f, mean = sum[1] * s2 * inv_d;
+            float s2 = unit_of(sum[0], inv_d, p.eps), s1 = p.after ? unit_of(sum[2], inv_d, p.eps) : 1.0f, mean = sum[1] * s2;
             if (too_much(sum[0]) || too_much(fabsf(sum[1])) || (p.after && too_much(sum[2]))) {
                 float few[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -409,8 +411,9 @@ __global__ __launch_bounds__(MOST) void norm_grad_kernel(const NormGradParams p)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) ph[0] = __builtin_fmaf(b[i] * at(now.n[c], i), at(now.s[c], i) * s2, ph[0]);
                 }
+                ph[0] *= inv_d;
                 sums(ph);
-                mean = ph[0] * inv_d;
+                mean = ph[0];
             }
             float dr[C][8], qx[1] = {0.0f};
 #pragma unroll
@@ -438,8 +441,9 @@ __global__ __launch_bounds__(MOST) void norm_grad_kernel(const NormGradParams p)
                 }
             }
             if (p.after) {
+                qx[0] *= inv_d;
                 sums(qx);
-                const float c1 = qx[0] * inv_d;
+                const float c1 = qx[0];
 #pragma unroll
                 for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -555,11 +559,12 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradPara
                         sum[2] = __builtin_fmaf(v, v, sum[2]);
                     }
                 }
+                sum[1] *= inv_d;
                 sums(sum);
             };
             float sum[3];
             squares(1.0f, sum);
-            float s2 = unit_of(sum[0], inv_d, p.eps), s1 = p.after ? unit_of(sum[2], inv_d, p.eps) : 1.0f, mean = sum[1] * s2 * inv_d;
+            float s2 = unit_of(sum[0], inv_d, p.eps), s1 = p.after ? unit_of(sum[2], inv_d, p.eps) : 1.0f, mean = sum[1] * s2;
             if (too_much(sum[0]) || too_much(fabsf(sum[1])) || (p.after && too_much(sum[2]))) {
                 float few[3], ph[1] = {0.0f};
                 squares(SOPK_FEWER, few);
@@ -572,8 +577,9 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradPara
 #pragma unroll
                     for (int i = 0; i < 8; ++i) ph[0] = __builtin_fmaf(b[i] * dn[i], s[i] * s2, ph[0]);
                 }
+                ph[0] *= inv_d;
                 sums(ph);
-                mean = ph[0] * inv_d;
+                mean = ph[0];
             }
             float q[C][8], qx[1] = {0.0f};
 #pragma unroll
@@ -601,8 +607,9 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradPara
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (!p.y) continue;
+            qx[0] *= inv_d;
             if (p.after) sums(qx);
-            const float c1 = qx[0] * inv_d;
+            const float c1 = qx[0];
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 if (p.after) {
@@ -677,9 +684,10 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradPara
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(b[i] * dn[i], s[i] * s2, sum[0]);
             }
+            sum[0] *= inv_d;
             sums(sum);
         }
-        const float mean = sum[0] * inv_d;
+        const float mean = sum[0];
         sum[0] = 0.0f;
         if (p.y && p.after) {
             for (int k = threadIdx.x * 8; k < p.D; k += 8192) {
@@ -689,9 +697,10 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const NormGradPara
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(f[i] * dr[i], y[i] * s1, sum[0]);
             }
+            sum[0] *= inv_d;
             sums(sum);
         }
-        const float c1 = sum[0] * inv_d;
+        const float c1 = sum[0];
         for (int k = threadIdx.x * 8; k < whole; k += 8192) {
             const int left = p.D - k;
             w.read(k, s, dn, y, b);

@@ -103,3 +103,24 @@ def test_norm_under_a_large_eps(D):
     got = ctx().residual_norm_grad(None, _t(dn), _t(c["r"]), before=_vec(c["before"]), eps=c["eps"])
     _close(got.dr, want["dr"], err["dr"], "f32")
     _close(got.dbefore, want["dbefore"], err["dbefore"], "f32")
+
+
+@pytest.mark.parametrize("D", [96, 1000, 2050, 4096, 8192, 8200, 16384, 20000])
+def test_norm_gradients_from_large_gradients(D):
+    """The means of p h and q x are no larger than what they are means of: gradients of 1e35 to 1e37, all of one sign beside h or x, have sums that leave binary32 and means that do not.
+    By rows: small s under a large 1 / rms, s of size 1, s and its gradient beside it, y of size 1, y small."""
+    rng = np.random.default_rng(24)
+    c = _norm_case(rng, 5, D, "f32", "f32", 0, True, True, scale=0.5)
+    c.update(after=rng.uniform(0.5, 1, D).astype(np.float32), before=rng.uniform(0.5, 1, D).astype(np.float32))
+    s, y, a = rng.standard_normal((5, D)), rng.standard_normal((5, D)), rng.uniform(0.5, 1, (5, D))
+    s[0] *= 1e-3
+    y[4] *= 1e-3
+    c.update(r=s.astype(np.float32), y=y.astype(np.float32))
+    dn, ds = a * np.sign(s) * np.array([1e35, 1e37, 1e37, 0, 0])[:, None], a * np.sign(y) * np.array([0, 0, 1e37, 1e37, 1e34])[:, None]
+    ds, dn = ds.astype(np.float32), dn.astype(np.float32)
+    want, err = _grad_errors(c, ds, dn, c["r"])
+    got = ctx().residual_norm_grad(_t(ds), _t(dn), _t(c["r"]), before=_vec(c["before"]), y=_t(c["y"]), after=_vec(c["after"]), scale=c["scale"], fmt=sop.E5M2)
+    assert max(np.abs(want[k]).max() for k in want) < 2e38
+    for k in ("dr", "dy", "dbefore", "dafter"):
+        _close(getattr(got, k), want[k], err[k], "f32")
+    _near_codes_within(got.dy8, want["dy"], "E5M2", err["dy"])
