@@ -622,7 +622,7 @@ sop_status sop_packed_linear(sop_ctx* ctx, const void* x_dev, int64_t ldx, const
 
 /* Gradient of an epilogue, from the z that it kept: dz = scale dy act'(z) (relu: 0 at 0), as numbers of dy's type (for sop_fp8_weight_grad), in 8 bits (for
  * the input gradient; formed from the binary32 values), and dbias = sum of dz over the rows.  The residual's gradient is dy.
- *   dy [M, N], z [M, N] of dy's type (NULL without an activation), dz [M, N] of dy's type or NULL; dz8 of block_rows 1
+ *   dy [M, N], z [M, N] of dy's type (NULL without an activation), dz [M, N] of dy's type or NULL; it may be dy or z itself (then with its row stride); dz8 of block_rows 1
  *   dbias: DEVICE, N floats, or NULL; sums over rows are binary32 within a workgroup's share of them (up to
  *   2^11 such shares) and binary64 from there on, in an order fixed by the sizes and the GPU
  *   workspace: DEVICE, 16-byte aligned, sop_fp8_linear_grad_workspace() bytes; NULL where dbias is */
@@ -654,7 +654,7 @@ sop_status sop_residual_norm(sop_ctx* ctx, const sop_residual_norm_opts* opts, i
  *   dbefore = sum of dn h, dafter = sum of scale gate dr u, over all rows; dgate[j] = sum of scale after dr u over the rows of gate row j
  * formed from the binary32 dr.  Types: s, ds and dr of r_dtype; y, dn and dy of y_dtype; dgate of gate_dtype, row stride ld_dgate; dbefore, dafter: D floats.
  * s and dn are not looked at without `before`; y NULL: nothing of y is.  dy8 (NULL or block_rows 1): dy in 8 bits, formed from the binary32 values.  dbefore, dafter and
- * dgate are NULL where they are not wanted (dafter without `after`, dgate without a gate).  Sums over rows as in sop_fp8_linear_grad.
+ * dgate are NULL where they are not wanted (dafter without `after`, dgate without a gate).  All that is written has memory of its own.  Sums over rows as in sop_fp8_linear_grad.
  *   workspace: DEVICE, 16-byte aligned, sop_residual_norm_grad_workspace() bytes */
 typedef struct {
     const void* ds; int64_t ld_ds;

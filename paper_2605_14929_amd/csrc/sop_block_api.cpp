@@ -103,6 +103,7 @@ extern "C" sop_status sop_fp8_linear_grad(sop_ctx* c, const void* dy, int64_t ld
         if (const char* why = plain_fault(dy, N, lddy, size)) return bad(c, call, SOP_EINVAL, why);
         if (act != SOP_ACT_NONE) if (const char* why = plain_fault(z, N, ldz, size)) return bad(c, call, SOP_EINVAL, why);
         if (dz) if (const char* why = plain_fault(dz, N, lddz, size)) return bad(c, call, SOP_EINVAL, why);
+        if (dz && M > 1 && ((dz == dy && lddz != lddy) || (act != SOP_ACT_NONE && dz == z && lddz != ldz))) return bad(c, call, SOP_EINVAL, "a dz in dy's or z's place has its row stride");
         if (const char* why = f8_fault(dz8, N, blocks(N), 1)) return bad(c, call, SOP_EINVAL, why);
         p.q = out_of(dz8);
     }
@@ -188,6 +189,8 @@ extern "C" sop_status sop_residual_norm_grad(sop_ctx* c, const sop_residual_norm
     if (!has_y && (o->after || o->gate)) return bad(c, call, SOP_EINVAL, "without y there is no `after` and no gate");
     if ((t->dbefore && !o->before) || (t->dafter && !o->after) || (t->dgate && !o->gate)) return bad(c, call, SOP_EINVAL, "a gradient is asked for that there is nothing to have");
     if (off(t->dbefore, 4) || off(t->dafter, 4)) return bad(c, call, SOP_EINVAL, "dbefore or dafter is not aligned to its elements");
+    if ((t->dbefore && t->dbefore == o->before) || (t->dafter && t->dafter == o->after) || (t->dgate && t->dgate == o->gate))   // (which other workgroups still read)
+        return bad(c, call, SOP_EINVAL, "the gradients of weights and gate have memory of their own");
     const int64_t zr = size_of(t->r_dtype), zy = size_of(t->y_dtype);
     if (t->dgate) if (const char* why = plain_fault(t->dgate, D, t->ld_dgate, size_of(o->gate_dtype))) return bad(c, call, SOP_EINVAL, why);
     if (M > 0) {
