@@ -592,14 +592,15 @@ sop_status sop_packed_matmul(sop_ctx* ctx, const void* x_dev, int64_t ldx, const
 
 /* ---- what stands around such a layer in a block of a model: products with an epilogue, norms with the residual stream, gradients clipped together.
  * Under the same rules as the calls above: nothing is kept in the context, calls may overlap, all are asynchronous on hip_stream, allocate nothing, may be
- * captured into a graph, and take workspace from the caller where they need any.  All arithmetic is binary32 (sums over rows and tensors: see there);
- * results are rounded once.  Infinities and NaN go the way of the formulas.  Matrices of numbers are fp32 or bf16 on any alignment of an element, row strides in elements. */
+ * captured into a graph, and take workspace from the caller where they need any.  All arithmetic is binary32 (sums over rows and tensors: see there; a product's
+ * sums v are those of the product without an epilogue, with bf16 weights in sop_packed_linear and, for bf16 results, the grid of sop_fp8_matmul); results are rounded once.  Infinities and NaN go the way of the formulas.  Matrices of numbers are fp32 or bf16 on any alignment of an element, row strides in elements. */
 
 /* Epilogue of a product with sums v: z = v + bias, y = residual + scale act(z).
  *   SOP_ACT_RELU       max(z, 0)                SOP_ACT_SILU       z / (1 + exp(-z))
  *   SOP_ACT_GELU       z Phi(z), Phi the normal distribution
  *   SOP_ACT_GELU_TANH  z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
- * An activation of -infinity is its limit, 0.
+ * An activation of -infinity is its limit, 0.  Activations, and the two terms that a slope is the sum of, are within 2^-19 of themselves; gelu by tanh, whose exponent is a rounded polynomial,
+ * within 2^-22 of that exponent more.  For bf16 matrices exponents (z^2 / 2 of gelu, |z| of silu) have 24 bits: 2.5 2^-24 of the exponent more, which dbias and dz8 have too.
  *   bias      DEVICE, N floats, or NULL
  *   residual  DEVICE, [M, N] of y's type, row stride ldr, or NULL; it may be y itself (then with y's row stride)
  *   z         DEVICE, [M, N] of y's type, row stride ldz, or NULL: z is kept for sop_fp8_linear_grad */
@@ -616,7 +617,7 @@ typedef struct {
 sop_status sop_fp8_linear(sop_ctx* ctx, const sop_f8_matrix* x, const sop_f8_matrix* w, int w_transposed, int64_t M, int64_t N, int64_t K,
                           const sop_epilogue* epilogue, void* y, sop_dtype dtype, int64_t ldy, void* hip_stream);
 
-/* sop_packed_matmul with an epilogue; y, residual and z are bf16. */
+/* sop_packed_matmul with an epilogue; y, residual and z are bf16.  As there, w = s * L[code] is rounded to bf16, which takes the error of z and y from 1.7e-3 (their own rounding) to 2.2e-3. */
 sop_status sop_packed_linear(sop_ctx* ctx, const void* x_dev, int64_t ldx, const sop_packed_weights* w, int64_t M, const sop_epilogue* epilogue,
                              void* y_dev, int64_t ldy, void* hip_stream);
 

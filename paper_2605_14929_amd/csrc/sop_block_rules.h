@@ -5,7 +5,10 @@
 namespace sopr {
 
 // A row of D elements by T threads, C times eight elements each, which keep it in registers (T = 64: a wavefront, four of them a workgroup); D beyond 16384 is
-// read several times instead (T = 0).  Measured, by eight and by sixteen elements: 8192 x 4096 bf16 46 and 42 us, 4096 x 5024 fp32 57 and 67, 8192 x 8192 with the stream in fp32 145 and 148.
+// read several times instead (T = 0).  Measured, by eight and by sixteen elements, 2^25 elements in bf16 (and in fp32): rows of 512 45 and 54 us (87 and 95), of 768 57 and 53 (90 and 93), of 1024
+// 49 and 50 (84 and 87), of 1536 47 and 51 (93 and 92), of 2048 48 and 52 (83 and 86), of 2560 55 and 54 (90 and 95), of 3000 55 and 50 (94 and 95), of 4096 48 and 46 (86 and 87);
+// 2^26 elements: of 4104 128 and 138 (180 and 200), of 5024 123 and 125 (186 and 211), of 6144 103 and 108 (177 and 180), of 8192 115 and 100 (175 and 173; y in bf16, stream in fp32 146 and 149).
+// Beyond 512 and up to 4096 the two are within a tenth of each other; in bf16 alone, rows of 7168 to 8192 would gain by sixteen (132 and 100, 115 and 100), which has not been taken.
 struct RowShape { int T, C; };
 inline int threads_for(long long D, int C) { return (int)((D + 512 * C - 1) / (512 * C)) * 64; }
 inline RowShape norm_shape(long long D)
@@ -15,7 +18,7 @@ inline RowShape norm_shape(long long D)
 }
 // Backward, where a thread holds four times as much: eight elements up to 8192 (8192 x 4096 bf16 105 us, sixteen 108; 777 x 5024 fp32 32 and 34; 8192 x 1024 fp32 49, sixteen a
 // wavefront's thread 58), then
-// sixteen of a row that it does not keep (4096 x 12288 bf16 224 us, by the way of still longer rows 330).
+// sixteen of a row that it does not keep (4096 x 12288 bf16 209 us, by the way of still longer rows 330).
 inline RowShape norm_grad_shape(long long D)
 {
     return D <= 512 ? norm_shape(D) : D <= 8192 ? RowShape{threads_for(D, 1), 1} : D <= 16384 ? RowShape{1024, 2} : RowShape{0, 0};

@@ -175,9 +175,9 @@ template <bool BF16, int FN, int ROWS, bool RES, bool Z, typename P> __device__ 
         }
     }
 }
-// ... or some of them outside y, or on odd addresses: four by four, each with its checks.  (All of them so, every wait being for all stores before it, 4096 x 11008 x 4096 with
-// gelu and z took 269 us.  By windows 210; without an epilogue 179, with a bias 180, and a residual 201 (its 90 MB come in bursts, when all tiles end), with silu 194, with
-// gelu 205: the vector ALUs, eight wavefronts a compute unit doing nothing else.)
+// ... or some of them outside y, or on odd addresses: four by four, each with its checks.  (From an odd address, every wait being for all stores before it, 4096 x 11008 x 4096 with
+// gelu and z takes 253 us.  By windows 213, and with a residual 245; without an epilogue 182, with a bias 182, and a residual 205 (its 90 MB come in bursts, when all tiles end), with
+// silu 197, with gelu 207: the vector ALUs, which are busy for 64 k of the 77 k cycles that gelu and z add.)
 template <bool BF16, int FN, int ROWS, typename P> __device__ __forceinline__ void finish_squares(const P& p, const v4f* place, const float* bias, int first, int count, int m0, int n0, int lane)
 {
     if (by_windows(p, m0, n0, ROWS, 32 * FN, BF16 ? 2 : 4)) {

@@ -285,8 +285,8 @@ __global__ __launch_bounds__(WR * WC * 64) void f8mm_tile_kernel(const F8MmParam
     }
     __syncthreads();                                                    // (LDS is free for the results)
     if constexpr (EPI) {
-        // as many of the wavefront's squares at once as find room, and the epilogue's code once: it is fetched by the few wavefronts that run it
-        // (2048 x 11008 x 4096 packed takes 208 us with the code there once or twice, 252 with six copies, 196 without an epilogue)
+        // as many of the wavefront's squares at once as find room, and the epilogue's code once: it is fetched by the few wavefronts that run it (six copies of it
+        // cost the packed product, whose tiles leave the same way, a fifth)
         constexpr int SQUARES = FM * FN, ROOM = 2 * STAGE / (WR * WC) / 4096, PART = ROOM < SQUARES ? ROOM : SQUARES;
         v4f* place = reinterpret_cast<v4f*>(lds + wave * (PART * 4096));
 #pragma unroll 1

@@ -9,10 +9,12 @@
 // Every pass is bound by HBM.  A row stays in the registers of the threads that share it (T threads, C times eight neighbouring elements each), so that it is
 // read once; its sums go over a wavefront by rotations and over a workgroup through LDS.  Threads keep their columns from row to row, so weights, and the
 // backward pass's sums over rows, stay with them: a workgroup leaves one row of partial sums, and a second kernel adds those up in a fixed order.
-// Backward, rows of more than 8192 elements are read three times over instead, two of them out of L2; so are those of more than 16384, which leave their sums to a pass over columns.
+// Backward, rows of 8193 to 16384 elements are read twice over, y a third time: 4096 x 12288 fetches 1.3 times one read from beyond L2 in bf16, 1.9 times in fp32.  Longer ones are read four
+// times by a pass over rows (2.3 times one read from beyond L2 at 4096 x 20000 bf16) and once more by a pass over columns, which has their sums.
 //
 // Measured, kernel times (a large copy moves 5.1 TB/s): forward 8192 x 8192, y bf16 and stream fp32, 145 us, 5.1 TB/s, one token of 4096 4.1 us; backward 8192 x 4096 bf16 with a
-// gate of one row 95 us, 4.8 TB/s with the partial sums, and 6 us to add those up (512 rows of 4096, twice); 777 x 5024 fp32 with three gates 25 and 7; 4096 x 12288 bf16 224 us in all.
+// gate of one row 95 us, 4.8 TB/s with the partial sums, and 6 us to add those up (512 rows of 4096, twice); 777 x 5024 fp32 with three gates 25 and 7; 4096 x 12288 bf16 209 us in all,
+// fp32 338; 4096 x 20000 bf16 forward 189, backward 506; a gate row for each of y, 8192 x 4096 bf16 134, 32768 x 512 148 (a gate of one row: 48).
 // Backward, the next row is asked for while one is worked on (8192 x 4096 102 us in all, without that some 20 more).
 //
 // Sums of squares are binary32; where one leaves its range (elements beyond 2^51 to 2^61, by how many there are) the row's are formed once more from elements 2^-96 as large: 2^20 of the
@@ -518,8 +520,9 @@ template <bool YB, bool RB> struct LongRow {
     }
 };
 
-// ---- backward, rows of up to 16384 elements: 1024 threads with sixteen columns each.  Their sums over rows stay in registers and LDS, a row does not: it is read once
-// from HBM and, one workgroup a compute unit, twice more out of L2.
+// ---- backward, rows of up to 16384 elements: 1024 threads with sixteen columns each.  Their sums over rows stay in registers and LDS, a row does not: it is read again, and, one
+// workgroup a compute unit, mostly out of L2.  (Raw, a row of bf16 would take 32 of a thread's 128 registers, one of fp32 64; that has not been built.)  The compiler keeps some 40 registers
+// of a thread in scratch memory: 31 of the 309 MB written at 4096 x 12288 bf16.
 template <bool YB, bool RB>
 __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const NormGradParams p)
 {

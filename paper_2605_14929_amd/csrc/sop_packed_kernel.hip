@@ -591,7 +591,7 @@ __global__ __launch_bounds__(256, E == 2 ? 2 : 1) void packed_wide_kernel(const 
     __syncthreads();                                                    // (LDS is free for the results)
     if constexpr (EPI) {
         // as many of the wavefront's squares at once as find room, and the epilogue's code once: it is fetched by the few wavefronts that run it
-        // (2048 x 11008 x 4096 packed takes 208 us with the code there once or twice, 252 with six copies, 196 without an epilogue)
+        // (2048 x 11008 x 4096 with silu took 252 us with six copies of it where it took 208 with one or two; by windows, as it is now, 213 to 221, and 194 to 200 without an epilogue)
         constexpr int SQUARES = E * F, PART = wide_part<E, F>(TAB + 2 * STAGE);
         v4f* place = reinterpret_cast<v4f*>(lds + wave * (PART * 4096));
         float* bias = reinterpret_cast<float*>(lds + 4 * PART * 4096) + wave * (32 * F);
